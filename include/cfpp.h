@@ -358,6 +358,144 @@ cfpp_status cfpp_generate_capture(cfpp_ctx *ctx, const void *const *packed_layer
                                   int32_t *pos_dev, void *x_buf, void *hidden_buf,
                                   cfpp_stream stream);
 
+/* ---- drafted trees over a paged cache ------------------------------------------
+ * Several requests share one pool of pages per layer, and a step checks a tree of
+ * drafted tokens of each in one pass.  Five operators, in the order of a step:
+ *
+ *   cfpp_page_tables     pages for the new rows; block tables and slots
+ *   cfpp_tree_plan       ancestor masks and positions from the nodes' parents
+ *   cfpp_page_append     a layer's new K and V rows into their slots
+ *   cfpp_tree_attention  every node over its request's cached positions and its
+ *                        ancestors
+ *   cfpp_tree_accept     the path that agrees with the model's picks; its rows move
+ *                        to the front, in all layers
+ *
+ * cfpp_stack_tree runs a model's blocks for the rows of all trees with them.
+ *
+ * Everything that varies from step to step is device memory, read by the kernels:
+ * a captured graph follows it.  Nothing here raises the device error flag
+ * (cfpp_stack_tree's positions apart): a request that cannot be served has
+ * granted[r] = 0 and slots of -1, and its rows are left out by the calls behind.
+ * No call may overlap in time with another one that writes what it uses.
+ *
+ * One layer's pool (DEVICE, cfpp_page_pool_bytes(pages) bytes):
+ *     fp16 [2 (K, V)][n_pages][n_kv_heads][head_dim/16][page_len][16]
+ * - a KV layer above whose sequences are pages: n_pages its max_batch, page_len its
+ * max_seq.  So a layer's contiguous cache whose max_seq is a multiple of 16 is a
+ * pool too, with sequence b as page b.  Slot page * page_len + offset names a
+ * position of the pool. */
+typedef struct cfpp_pages {
+    int32_t n_pages;      /* pages of a layer's pool; n_pages * page_len < 2^31    */
+    int32_t page_len;     /* positions to a page, a multiple of 16                 */
+    int32_t n_kv_heads;   /* heads that have K and V                               */
+    int32_t head_dim;     /* 64, 80 or 128                                         */
+} cfpp_pages;
+
+/* The requests of a step (HOST struct of DEVICE pointers, 4-byte aligned).  Request r
+ * has lens[r] cached positions and count_r = row_start[r + 1] - row_start[r] rows, its
+ * nodes: rows row_start[r] ... of everything that has a row per node.  Node i is row i of them and
+ * stands at cache index lens[r] + i, whatever its place in the tree.  parents[row] is
+ * the parent's node number, below the node's own; -1 (or any other number that is no
+ * earlier node's): a node right behind the cached positions.  One row without parent
+ * is the plain decode step, a chain a piece of a prompt.
+ * Rows from row_start[n_requests] to max_rows - 1 are nobody's: what belongs to them is
+ * left as it was, but for slots, which are -1 there. */
+typedef struct cfpp_tree_batch {
+    int32_t n_requests;         /* 1 .. 4096                                               */
+    int32_t max_rows;           /* rows that the arrays hold, 1 .. 2^20                    */
+    int32_t max_nodes;          /* most nodes of a request, 1 .. 256                       */
+    int32_t table_stride;       /* entries of a request's block table; times page_len < 2^31 */
+    const int32_t *lens;        /* [n_requests]                                            */
+    int32_t *row_start;         /* [n_requests + 1]         written by cfpp_page_tables    */
+    int32_t *block_table;       /* [n_requests][table_stride]  pages, by position / page_len */
+    int32_t *slots;             /* [max_rows]               written by cfpp_page_tables    */
+    const int32_t *parents;     /* [max_rows]                                              */
+    uint32_t *masks;            /* [max_rows][(max_nodes + 31) / 32]  written by cfpp_tree_plan:
+                                   bit j of a node's words: it sees node j                 */
+    int32_t *positions;         /* [max_rows]               written by cfpp_tree_plan      */
+    void *plan;                 /* cfpp_tree_plan_bytes bytes, 256-byte aligned            */
+    size_t plan_bytes;
+} cfpp_tree_batch;
+
+/* CFPP_OK if `pages` is a shape this build supports, else EINVAL / EUNSUPPORTED. */
+cfpp_status cfpp_validate_pages(const cfpp_pages *pages);
+/* Bytes of one layer's pool; 0 if `pages` is invalid. */
+size_t cfpp_page_pool_bytes(const cfpp_pages *pages);
+/* Bytes of a batch's plan: the attention's launch plan, its counters and the sums that
+ * workgroups hand over.  0 for invalid arguments.  n_heads: query heads, a multiple of
+ * n_kv_heads, at most 256 to each of them. */
+size_t cfpp_tree_plan_bytes(const cfpp_pages *pages, int32_t n_heads, int32_t n_requests,
+                            int32_t max_rows, int32_t max_nodes);
+
+/* Pages for counts[r] new rows behind the lens[r] cached positions of every request.
+ * With target_r = ceil((lens[r] + counts[r]) / page_len) and held[r] pages at entries
+ * 0 .. held[r] - 1 of its block table, a request takes target_r - held[r] pages or
+ * gives back the last held[r] - target_r: lens = counts = 0 gives back all.
+ *   held       : DEVICE int32 [n_requests], updated
+ *   free_pages : DEVICE int32 [n_pages], *free_count of them free.  Pages are taken from the end of the list, for requests in
+ *                order; those given back follow what is left, in order, and can be
+ *                taken from the next call on
+ *   granted    : DEVICE int32 [n_requests]: 1, or 0 where the pages that this request
+ *                and those before it need are more than the free ones (and it needs any),
+ *                the block table is too short, lens or counts negative, or the rows pass
+ *                max_rows: such a request neither takes nor gives, and its slots are -1
+ * Uses lens; writes block_table (taken pages; -1 in place of those given back),
+ * row_start (the sums of counts, up to max_rows; a negative one counts as 0) and slots.
+ * The batch's other pointers may be NULL.  Asynchronous on `stream`, as the calls below. */
+cfpp_status cfpp_page_tables(const cfpp_pages *pages, const cfpp_tree_batch *batch,
+                             const int32_t *counts, int32_t *held, int32_t *free_pages,
+                             int32_t *free_count, int32_t *granted, cfpp_stream stream);
+
+/* masks and positions of every node from parents: bit j of node i is set where j is i or
+ * an ancestor of i, and position = lens[r] + the number of i's ancestors.  Prepares the
+ * batch's plan for cfpp_tree_attention with n_heads query heads: once for all layers,
+ * and again whenever lens, row_start or slots have changed.  The caller may change masks
+ * behind it (any set of the request's nodes, none among them).  Requests with more
+ * than max_nodes nodes, a first slot of -1, negative lengths or more positions than
+ * their block table holds are left out.  slots may be NULL (every request counts),
+ * block_table is not read. */
+cfpp_status cfpp_tree_plan(const cfpp_pages *pages, const cfpp_tree_batch *batch, int32_t n_heads,
+                           cfpp_stream stream);
+
+/* Row i of k_rows and v_rows (DEVICE fp16 [n_rows][row_stride], head n's values at
+ * n * head_dim; row_stride in elements, a multiple of 8) into slots[i] of a layer's
+ * pool.  Slots outside the pool are skipped; of equal slots one row wins, piece by piece. */
+cfpp_status cfpp_page_append(const cfpp_pages *pages, void *kv_pool, const void *k_rows,
+                             const void *v_rows, int64_t row_stride, const int32_t *slots,
+                             int32_t n_rows, cfpp_stream stream);
+
+/* out[row] = softmax(q[row] K^T / sqrt(head_dim)) V over the positions that the node sees:
+ * the lens[r] cached ones, and those of its request's nodes whose bit is set in its masks.
+ * A node that sees none gives zeros.  What lies in unseen positions, infinite or NaN, does not
+ * matter.  A block-table entry outside the pool makes the
+ * rows that see its positions NaN.
+ *   q, out  : DEVICE fp16 [max_rows][stride], head n's values at n * head_dim; strides in
+ *             elements, multiples of 8.  out must not overlap q
+ *   n_heads : query heads; n_heads / n_kv_heads consecutive ones share a key head
+ * Reads lens, row_start, block_table, masks and the plan, which must have been made with
+ * the same pages, n_heads and batch sizes; uses the plan's memory, so calls with one
+ * plan belong on one stream. */
+cfpp_status cfpp_tree_attention(const cfpp_pages *pages, const void *kv_pool,
+                                const cfpp_tree_batch *batch, const void *q, int64_t q_stride,
+                                int32_t n_heads, void *out, int64_t out_stride, cfpp_stream stream);
+
+/* The path that agrees with the model: node 0 (the token that the step before picked),
+ * then the lowest-numbered child whose token is the pick behind its parent, as long as
+ * there is one.  Its K and V rows move to cache indices lens[r] .. in all n_layers
+ * pools (kv_pools: HOST array of DEVICE pointers, at most 64; n_layers 0: nothing moves); other
+ * rows of the request stay or are overwritten.
+ *   tokens, picks : DEVICE int32 [max_rows]: a node's token; the model's pick behind it
+ *   accepted      : DEVICE int32 [n_requests]: length of the path; 0 for a request that has
+ *                   no node, more than max_nodes, or a first slot of -1
+ *   path          : DEVICE int32 [n_requests][max_nodes]: its nodes, then -1
+ *   next_tokens   : DEVICE int32 [n_requests]: the pick behind its last node, or -1
+ *   lens_out      : DEVICE int32 [n_requests]: lens + accepted; may be the same memory as lens
+ * Reads lens, row_start, slots and parents. */
+cfpp_status cfpp_tree_accept(const cfpp_pages *pages, void *const *kv_pools, int32_t n_layers,
+                             const cfpp_tree_batch *batch, const int32_t *tokens,
+                             const int32_t *picks, int32_t *accepted, int32_t *path,
+                             int32_t *next_tokens, int32_t *lens_out, cfpp_stream stream);
+
 /* The whole-stack kernel marks the words its workgroups exchange with a 32-bit
  * epoch that every launch advances by n_layers + 1; the library counts the
  * epochs on the host and, before they could wrap (after about 2^32 / (n_layers + 1)

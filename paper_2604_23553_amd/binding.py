@@ -68,6 +68,7 @@ def _load(kind: str) -> C.CDLL:
         for n in ("cfpp_packed_layer_bytes", "cfpp_kv_layer_bytes", "cfpp_workspace_bytes"):
             getattr(L, n).restype = C.c_size_t
             getattr(L, n).argtypes = [C.POINTER(Config)]
+        L.cfpp_page_pool_bytes.restype = L.cfpp_tree_plan_bytes.restype = C.c_size_t
         L.cfpp_prefill_scratch_bytes.restype = C.c_size_t
         L.cfpp_prefill_scratch_bytes.argtypes = [C.POINTER(Config), C.c_int32]
         L.cfpp_destroy.restype = None
@@ -259,6 +260,72 @@ def cfpp_block_decode_static(cfg: Config, packed_layer, kv_layer, x, pos_dev, ba
     _check(lib().cfpp_block_decode_static(C.byref(cfg), _ptr(packed_layer), _ptr(kv_layer), _ptr(x),
                                           _ptr(pos_dev), C.c_int32(batch), _ptr(out), _ptr(stream)),
            "cfpp_block_decode_static")
+
+
+# ---- drafted trees over a paged cache ------------------------------------------
+class Pages(C.Structure):
+    """Mirror of `cfpp_pages`: a layer's pool of pages."""
+    _fields_ = [("n_pages", C.c_int32), ("page_len", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32)]
+
+
+class TreeBatch(C.Structure):
+    """Mirror of `cfpp_tree_batch`: the requests of a step (device pointers; keep the tensors alive)."""
+    _fields_ = [("n_requests", C.c_int32), ("max_rows", C.c_int32), ("max_nodes", C.c_int32), ("table_stride", C.c_int32),
+                ("lens", C.c_void_p), ("row_start", C.c_void_p), ("block_table", C.c_void_p), ("slots", C.c_void_p),
+                ("parents", C.c_void_p), ("masks", C.c_void_p), ("positions", C.c_void_p), ("plan", C.c_void_p),
+                ("plan_bytes", C.c_size_t)]
+
+    @classmethod
+    def of(cls, max_nodes: int, lens, row_start, block_table, slots, parents=None, masks=None, positions=None, plan=None):
+        """From int32 tensors lens [R], row_start [R + 1], block_table [R, stride], slots [rows], ...; plan: uint8 tensor."""
+        return cls(lens.numel(), slots.numel(), int(max_nodes), block_table.shape[1],
+                   *[_ptr(t).value for t in (lens, row_start, block_table, slots, parents, masks, positions, plan)],
+                   0 if plan is None else plan.numel())
+
+
+def cfpp_validate_pages(pages: Pages) -> int:
+    """Returns the status code (0 = supported); does not raise."""
+    return int(lib().cfpp_validate_pages(C.byref(pages)))
+
+
+def cfpp_page_pool_bytes(pages: Pages) -> int:
+    return int(lib().cfpp_page_pool_bytes(C.byref(pages)))
+
+
+def cfpp_tree_plan_bytes(pages: Pages, n_heads: int, n_requests: int, max_rows: int, max_nodes: int) -> int:
+    return int(lib().cfpp_tree_plan_bytes(C.byref(pages), C.c_int32(n_heads), C.c_int32(n_requests), C.c_int32(max_rows),
+                                          C.c_int32(max_nodes)))
+
+
+def cfpp_page_tables(pages: Pages, batch: TreeBatch, counts, held, free_pages, free_count, granted, stream=None):
+    _check(lib().cfpp_page_tables(C.byref(pages), C.byref(batch), _ptr(counts), _ptr(held), _ptr(free_pages), _ptr(free_count),
+                                  _ptr(granted), _ptr(stream)), "cfpp_page_tables")
+
+
+def cfpp_tree_plan(pages: Pages, batch: TreeBatch, n_heads: int, stream=None):
+    _check(lib().cfpp_tree_plan(C.byref(pages), C.byref(batch), C.c_int32(n_heads), _ptr(stream)), "cfpp_tree_plan")
+
+
+def cfpp_page_append(pages: Pages, kv_pool, k_rows, v_rows, slots, n_rows: int, row_stride: int | None = None, stream=None):
+    """row_stride: elements between rows, n_kv_heads * head_dim by default."""
+    _check(lib().cfpp_page_append(C.byref(pages), _ptr(kv_pool), _ptr(k_rows), _ptr(v_rows),
+                                  C.c_int64(pages.n_kv_heads * pages.head_dim if row_stride is None else row_stride), _ptr(slots),
+                                  C.c_int32(n_rows), _ptr(stream)), "cfpp_page_append")
+
+
+def cfpp_tree_attention(pages: Pages, kv_pool, batch: TreeBatch, q, n_heads: int, out, q_stride: int | None = None,
+                        out_stride: int | None = None, stream=None):
+    """q_stride, out_stride: elements between rows, n_heads * head_dim by default."""
+    width = n_heads * pages.head_dim
+    _check(lib().cfpp_tree_attention(C.byref(pages), _ptr(kv_pool), C.byref(batch), _ptr(q),
+                                     C.c_int64(width if q_stride is None else q_stride), C.c_int32(n_heads), _ptr(out),
+                                     C.c_int64(width if out_stride is None else out_stride), _ptr(stream)), "cfpp_tree_attention")
+
+
+def cfpp_tree_accept(pages: Pages, kv_pools, batch: TreeBatch, tokens, picks, accepted, path, next_tokens, lens_out, stream=None):
+    _check(lib().cfpp_tree_accept(C.byref(pages), _ptr_array(kv_pools), C.c_int32(len(kv_pools)), C.byref(batch), _ptr(tokens),
+                                  _ptr(picks), _ptr(accepted), _ptr(path), _ptr(next_tokens), _ptr(lens_out), _ptr(stream)),
+           "cfpp_tree_accept")
 
 
 # ---- profiling library only (inside `with profile_build():`) -------------------

@@ -19,6 +19,7 @@
 #include "narrow_params.h"
 #include "prefill_params.h"
 #include "decode_params.h"
+#include "tree_params.h"
 
 using namespace cfpp;
 
@@ -1040,6 +1041,177 @@ extern "C" cfpp_status cfpp_device_error(cfpp_ctx *ctx, cfpp_stream stream)
     if (err == kErrBarrierTimeout) return fail(CFPP_EDEVICE, "grid barrier timed out (workgroups not co-resident?)");
     if (err == kErrBadToken) return fail(CFPP_EDEVICE, "a token in tokens_dev was outside [0, vocab)");
     return fail(CFPP_EDEVICE, "device error code %u", err);
+}
+
+// ---- drafted trees over a paged cache -------------------------------------------------------
+static bool aligned4(const void *p) { return p && (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+static bool overlap(const void *a, size_t na, const void *b, size_t nb)
+{
+    const char *x = static_cast<const char *>(a), *y = static_cast<const char *>(b);
+    return x < y + nb && y < x + na;
+}
+
+extern "C" cfpp_status cfpp_validate_pages(const cfpp_pages *p)
+{
+    if (!p) return fail(CFPP_EINVAL, "pages is NULL");
+    if (p->n_pages <= 0 || p->page_len <= 0 || p->n_kv_heads <= 0 || p->head_dim <= 0) return fail(CFPP_EINVAL, "pages has a non-positive dimension");
+    if ((long long)p->n_pages * p->page_len > 0x7fffffffll) return fail(CFPP_EINVAL, "%d pages of %d positions: at most 2^31 - 1 in all", p->n_pages, p->page_len);
+    if (p->page_len % 16) return fail(CFPP_EUNSUPPORTED, "page_len %d: a multiple of 16 is needed", p->page_len);
+    if (p->head_dim != 64 && p->head_dim != 80 && p->head_dim != 128)
+        return fail(CFPP_EUNSUPPORTED, "head_dim %d: only 64, 80 and 128 have kernels", p->head_dim);
+    if (p->n_kv_heads > 1024) return fail(CFPP_EUNSUPPORTED, "n_kv_heads %d > 1024", p->n_kv_heads);
+    return CFPP_OK;
+}
+
+static PageDims page_dims(const cfpp_pages &p)
+{
+    PageDims g;
+    g.n_pages = p.n_pages; g.page = p.page_len; g.heads = p.n_kv_heads; g.d = p.head_dim;
+    return g;
+}
+
+extern "C" size_t cfpp_page_pool_bytes(const cfpp_pages *p)
+{
+    if (cfpp_validate_pages(p) != CFPP_OK) return 0;
+    return 2 * page_which_elems(page_dims(*p)) * sizeof(__half);
+}
+
+static cfpp_status check_tree_heads(const cfpp_pages *p, int32_t n_heads)
+{
+    if (n_heads <= 0 || n_heads % p->n_kv_heads) return fail(CFPP_EINVAL, "n_heads %d is no multiple of n_kv_heads %d", n_heads, p->n_kv_heads);
+    if (n_heads / p->n_kv_heads > kTreeMaxGroup) return fail(CFPP_EUNSUPPORTED, "%d query heads to a key head: at most %d", n_heads / p->n_kv_heads, kTreeMaxGroup);
+    return CFPP_OK;
+}
+
+static cfpp_status check_tree_sizes(int32_t requests, int32_t max_rows, int32_t max_nodes)
+{
+    if (requests <= 0 || requests > kTreeMaxRequests) return fail(CFPP_EINVAL, "n_requests %d outside [1, %d]", requests, kTreeMaxRequests);
+    if (max_rows <= 0 || max_rows > kTreeMaxRows) return fail(CFPP_EINVAL, "max_rows %d outside [1, %d]", max_rows, kTreeMaxRows);
+    if (max_nodes <= 0 || max_nodes > kTreeMaxNodes) return fail(CFPP_EINVAL, "max_nodes %d outside [1, %d]", max_nodes, kTreeMaxNodes);
+    return CFPP_OK;
+}
+
+extern "C" size_t cfpp_tree_plan_bytes(const cfpp_pages *p, int32_t n_heads, int32_t n_requests, int32_t max_rows, int32_t max_nodes)
+{
+    if (cfpp_validate_pages(p) != CFPP_OK || check_tree_heads(p, n_heads) != CFPP_OK || check_tree_sizes(n_requests, max_rows, max_nodes) != CFPP_OK) return 0;
+    return tree_plan_layout(page_dims(*p), n_heads, n_requests, max_rows, max_nodes).total;
+}
+
+// what every call needs of a batch; its arrays are checked by the calls that use them
+static cfpp_status tree_batch(const cfpp_pages *p, const cfpp_tree_batch *b, TreeBatch *t)
+{
+    cfpp_status st = cfpp_validate_pages(p);
+    if (st != CFPP_OK) return st;
+    if (!b) return fail(CFPP_EINVAL, "batch is NULL");
+    if ((st = check_tree_sizes(b->n_requests, b->max_rows, b->max_nodes)) != CFPP_OK) return st;
+    if (b->table_stride <= 0 || (long long)b->table_stride * p->page_len > 0x7fffffffll)
+        return fail(CFPP_EINVAL, "table_stride %d: positive, and at most 2^31 - 1 positions", b->table_stride);
+    if (!aligned4(b->lens) || !aligned4(b->row_start)) return fail(CFPP_EINVAL, "lens or row_start is NULL or misaligned");
+    t->requests = b->n_requests; t->max_rows = b->max_rows; t->max_nodes = b->max_nodes; t->stride = b->table_stride;
+    t->lens = b->lens; t->row_start = b->row_start; t->table = b->block_table; t->slots = b->slots;
+    t->parents = b->parents; t->masks = b->masks; t->positions = b->positions;
+    return CFPP_OK;
+}
+
+static cfpp_status check_tree_plan(const cfpp_pages *p, const cfpp_tree_batch *b, int32_t n_heads)
+{
+    cfpp_status st = check_tree_heads(p, n_heads);
+    if (st != CFPP_OK) return st;
+    if (!b->plan || (reinterpret_cast<uintptr_t>(b->plan) & 255u)) return fail(CFPP_EINVAL, "plan is NULL or not 256-byte aligned");
+    const size_t need = tree_plan_layout(page_dims(*p), n_heads, b->n_requests, b->max_rows, b->max_nodes).total;
+    if (b->plan_bytes < need) return fail(CFPP_ENOMEM, "plan of %zu bytes, %zu needed", b->plan_bytes, need);
+    if (!aligned4(b->masks)) return fail(CFPP_EINVAL, "masks is NULL or misaligned");
+    return CFPP_OK;
+}
+
+extern "C" cfpp_status cfpp_page_tables(const cfpp_pages *pages, const cfpp_tree_batch *batch, const int32_t *counts, int32_t *held,
+                                        int32_t *free_pages, int32_t *free_count, int32_t *granted, cfpp_stream stream)
+{
+    TablesParams P;
+    cfpp_status st = tree_batch(pages, batch, &P.b);
+    if (st != CFPP_OK) return st;
+    if (!aligned4(batch->block_table) || !aligned4(batch->slots)) return fail(CFPP_EINVAL, "block_table or slots is NULL or misaligned");
+    if (!aligned4(counts) || !aligned4(held) || !aligned4(free_pages) || !aligned4(free_count) || !aligned4(granted))
+        return fail(CFPP_EINVAL, "counts, held, free_pages, free_count or granted is NULL or misaligned");
+    P.pg = page_dims(*pages);
+    P.counts = counts; P.held = held; P.free_pages = free_pages; P.free_count = free_count; P.granted = granted;
+    HIP_OK(launch_page_tables(P, static_cast<hipStream_t>(stream)));
+    return CFPP_OK;
+}
+
+extern "C" cfpp_status cfpp_tree_plan(const cfpp_pages *pages, const cfpp_tree_batch *batch, int32_t n_heads, cfpp_stream stream)
+{
+    TreeBatch b;
+    cfpp_status st = tree_batch(pages, batch, &b);
+    if (st != CFPP_OK) return st;
+    if ((st = check_tree_plan(pages, batch, n_heads)) != CFPP_OK) return st;
+    if (!aligned4(batch->parents) || !aligned4(batch->positions)) return fail(CFPP_EINVAL, "parents or positions is NULL or misaligned");
+    if (batch->slots && !aligned4(batch->slots)) return fail(CFPP_EINVAL, "slots is misaligned");
+    HIP_OK(launch_tree_plan(page_dims(*pages), b, n_heads, static_cast<char *>(batch->plan), static_cast<hipStream_t>(stream)));
+    return CFPP_OK;
+}
+
+extern "C" cfpp_status cfpp_page_append(const cfpp_pages *pages, void *kv_pool, const void *k_rows, const void *v_rows, int64_t row_stride,
+                                        const int32_t *slots, int32_t n_rows, cfpp_stream stream)
+{
+    cfpp_status st = cfpp_validate_pages(pages);
+    if (st != CFPP_OK) return st;
+    if (!aligned16(kv_pool) || !aligned16(k_rows) || !aligned16(v_rows)) return fail(CFPP_EINVAL, "kv_pool, k_rows or v_rows is NULL or not 16-byte aligned");
+    if (!aligned4(slots)) return fail(CFPP_EINVAL, "slots is NULL or misaligned");
+    if (n_rows < 0 || n_rows > kTreeMaxRows) return fail(CFPP_EINVAL, "n_rows %d outside [0, %d]", n_rows, kTreeMaxRows);
+    if (row_stride % 8 || row_stride < (int64_t)pages->n_kv_heads * pages->head_dim || row_stride > (1ll << 32))
+        return fail(CFPP_EINVAL, "row_stride %lld: a multiple of 8, at least n_kv_heads * head_dim and at most 2^32", (long long)row_stride);
+    if (n_rows == 0) return CFPP_OK;
+    HIP_OK(launch_page_append(page_dims(*pages), static_cast<__half *>(kv_pool), static_cast<const __half *>(k_rows),
+                              static_cast<const __half *>(v_rows), row_stride, slots, n_rows, static_cast<hipStream_t>(stream)));
+    return CFPP_OK;
+}
+
+extern "C" cfpp_status cfpp_tree_attention(const cfpp_pages *pages, const void *kv_pool, const cfpp_tree_batch *batch, const void *q,
+                                           int64_t q_stride, int32_t n_heads, void *out, int64_t out_stride, cfpp_stream stream)
+{
+    TreeAttention P;
+    cfpp_status st = tree_batch(pages, batch, &P.b);
+    if (st != CFPP_OK) return st;
+    if ((st = check_tree_plan(pages, batch, n_heads)) != CFPP_OK) return st;
+    if (!aligned4(batch->block_table)) return fail(CFPP_EINVAL, "block_table is NULL or misaligned");
+    if (!aligned16(kv_pool) || !aligned16(q) || !aligned16(out)) return fail(CFPP_EINVAL, "kv_pool, q or out is NULL or not 16-byte aligned");
+    const int64_t width = (int64_t)n_heads * pages->head_dim;
+    if (q_stride % 8 || q_stride < width || q_stride > (1ll << 32) || out_stride % 8 || out_stride < width || out_stride > (1ll << 32))
+        return fail(CFPP_EINVAL, "strides %lld, %lld: multiples of 8, at least n_heads * head_dim and at most 2^32", (long long)q_stride, (long long)out_stride);
+    const size_t rows = (size_t)batch->max_rows - 1;
+    if (overlap(q, (rows * q_stride + width) * 2, out, (rows * out_stride + width) * 2)) return fail(CFPP_EINVAL, "out overlaps q");
+    P.pg = page_dims(*pages);
+    P.n_heads = n_heads; P.group = n_heads / pages->n_kv_heads;
+    P.pool = static_cast<const __half *>(kv_pool);
+    P.q = static_cast<const __half *>(q); P.out = static_cast<__half *>(out);
+    P.q_stride = q_stride; P.out_stride = out_stride;
+    HIP_OK(launch_tree_attention(P, static_cast<char *>(batch->plan), static_cast<hipStream_t>(stream)));
+    return CFPP_OK;
+}
+
+extern "C" cfpp_status cfpp_tree_accept(const cfpp_pages *pages, void *const *kv_pools, int32_t n_layers, const cfpp_tree_batch *batch,
+                                        const int32_t *tokens, const int32_t *picks, int32_t *accepted, int32_t *path, int32_t *next_tokens,
+                                        int32_t *lens_out, cfpp_stream stream)
+{
+    AcceptParams P;
+    std::memset(&P, 0, sizeof P);
+    cfpp_status st = tree_batch(pages, batch, &P.b);
+    if (st != CFPP_OK) return st;
+    if (n_layers < 0 || n_layers > kMaxLayers) return fail(CFPP_EINVAL, "n_layers %d outside [0, %d]", n_layers, kMaxLayers);
+    if (n_layers > 0 && !kv_pools) return fail(CFPP_EINVAL, "kv_pools is NULL");
+    for (int l = 0; l < n_layers; ++l) {
+        if (!aligned16(kv_pools[l])) return fail(CFPP_EINVAL, "layer %d: NULL or misaligned pool", l);
+        P.pool[l] = static_cast<__half *>(kv_pools[l]);
+    }
+    if (!aligned4(batch->slots) || !aligned4(batch->parents)) return fail(CFPP_EINVAL, "slots or parents is NULL or misaligned");
+    if (!aligned4(tokens) || !aligned4(picks) || !aligned4(accepted) || !aligned4(path) || !aligned4(next_tokens) || !aligned4(lens_out))
+        return fail(CFPP_EINVAL, "tokens, picks, accepted, path, next_tokens or lens_out is NULL or misaligned");
+    P.pg = page_dims(*pages);
+    P.tokens = tokens; P.picks = picks;
+    P.accepted = accepted; P.path = path; P.next = next_tokens; P.lens_out = lens_out;
+    HIP_OK(launch_tree_accept(P, n_layers, static_cast<hipStream_t>(stream)));
+    return CFPP_OK;
 }
 
 // ---- block decode for callers that cannot allocate --------------------------------------

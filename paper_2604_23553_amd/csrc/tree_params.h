@@ -1,0 +1,62 @@
+// Arguments of the kernels for drafted trees over a paged cache (page_kernels.hip, tree_attention.hip).
+#pragma once
+#include <hip/hip_runtime.h>
+#include <hip/hip_fp16.h>
+#include "layout.h"
+
+namespace cfpp {
+
+constexpr int kTreeMaxRequests = 4096, kTreeMaxNodes = 256, kTreeMaxGroup = 256, kTreeMaxRows = 1 << 20;
+
+// a pool of pages: fp16 [2][n_pages][heads][d / 16][page][16], and the requests of a step
+struct PageDims { int n_pages, page, heads, d; };
+struct TreeBatch {
+    int requests, max_rows, max_nodes, stride;     // stride: entries of a block table
+    const int *lens;
+    int *row_start, *table, *slots;
+    const int *parents;
+    unsigned *masks;
+    int *positions;
+};
+
+CFPP_HD size_t page_head_elems(const PageDims &p) { return (size_t)p.d * p.page; }
+CFPP_HD size_t page_which_elems(const PageDims &p) { return (size_t)p.n_pages * p.heads * page_head_elems(p); }
+CFPP_HD int tree_words(int max_nodes) { return (max_nodes + 31) / 32; }
+
+struct TablesParams {
+    PageDims pg;
+    TreeBatch b;
+    const int *counts;
+    int *held, *free_pages, *free_count, *granted;
+};
+hipError_t launch_page_tables(const TablesParams &P, hipStream_t s);
+
+hipError_t launch_page_append(const PageDims &pg, __half *pool, const __half *k, const __half *v, long long row_stride, const int *slots,
+                              int n_rows, hipStream_t s);
+
+struct AcceptParams {
+    PageDims pg;
+    TreeBatch b;
+    const int *tokens, *picks;
+    int *accepted, *path, *next, *lens_out;
+    __half *pool[kMaxLayers];
+};
+hipError_t launch_tree_accept(const AcceptParams &P, int n_layers, hipStream_t s);
+
+// ---- the attention and its plan --------------------------------------------------------------
+struct TreePlanLayout { size_t total; };
+TreePlanLayout tree_plan_layout(const PageDims &pg, int n_heads, int requests, int max_rows, int max_nodes);
+
+struct TreeAttention {
+    PageDims pg;
+    TreeBatch b;
+    int n_heads, group;
+    const __half *pool;
+    const __half *q;
+    __half *out;
+    long long q_stride, out_stride;
+};
+hipError_t launch_tree_plan(const PageDims &pg, const TreeBatch &b, int n_heads, char *plan, hipStream_t s);
+hipError_t launch_tree_attention(const TreeAttention &P, char *plan, hipStream_t s);
+
+}  // namespace cfpp
