@@ -1094,7 +1094,7 @@ static cfpp_status check_tree_sizes(int32_t requests, int32_t max_rows, int32_t 
 extern "C" size_t cfpp_tree_plan_bytes(const cfpp_pages *p, int32_t n_heads, int32_t n_requests, int32_t max_rows, int32_t max_nodes)
 {
     if (cfpp_validate_pages(p) != CFPP_OK || check_tree_heads(p, n_heads) != CFPP_OK || check_tree_sizes(n_requests, max_rows, max_nodes) != CFPP_OK) return 0;
-    return tree_plan_layout(page_dims(*p), n_heads, n_requests, max_rows, max_nodes).total;
+    return tree_plan_layout(page_dims(*p), n_heads, n_requests, max_rows, max_nodes, 1).total;
 }
 
 // what every call needs of a batch; its arrays are checked by the calls that use them
@@ -1118,7 +1118,7 @@ static cfpp_status check_tree_plan(const cfpp_pages *p, const cfpp_tree_batch *b
     cfpp_status st = check_tree_heads(p, n_heads);
     if (st != CFPP_OK) return st;
     if (!b->plan || (reinterpret_cast<uintptr_t>(b->plan) & 255u)) return fail(CFPP_EINVAL, "plan is NULL or not 256-byte aligned");
-    const size_t need = tree_plan_layout(page_dims(*p), n_heads, b->n_requests, b->max_rows, b->max_nodes).total;
+    const size_t need = tree_plan_layout(page_dims(*p), n_heads, b->n_requests, b->max_rows, b->max_nodes, b->table_stride).total;
     if (b->plan_bytes < need) return fail(CFPP_ENOMEM, "plan of %zu bytes, %zu needed", b->plan_bytes, need);
     if (!aligned4(b->masks)) return fail(CFPP_EINVAL, "masks is NULL or misaligned");
     return CFPP_OK;

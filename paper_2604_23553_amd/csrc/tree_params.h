@@ -44,8 +44,21 @@ struct AcceptParams {
 hipError_t launch_tree_accept(const AcceptParams &P, int n_layers, hipStream_t s);
 
 // ---- the attention and its plan --------------------------------------------------------------
-struct TreePlanLayout { size_t total; };
-TreePlanLayout tree_plan_layout(const PageDims &pg, int n_heads, int requests, int max_rows, int max_nodes);
+// Query rows (a node's heads that share a key head, nodes one after the other) go to workgroups in tiles of 16, 32 or 64, positions in pieces.
+// A plan: the work list of a key head (TreeItem), an arrival counter for each tile and key head, and the sums of the pieces.
+struct TreeItem {
+    int request, first, nodes, len;    // rows first .. first + nodes - 1 behind len cached positions
+    int tile, piece, pieces, slot;     // slot: the tile's first place among the sums, one for each piece; -1 with a single piece
+    int t0, t1, counter, pad;          // positions; the tile's number
+};
+struct TreePlanHead { int items, key, pad[14]; };
+struct TreePlanLayout {
+    int tile_rows, want, tiles, work;  // rows of a tile; items aimed at; most tiles; most items
+    int key;                           // of the sizes that a plan is made for
+    size_t items, counters, sums, total;   // byte offsets
+};
+CFPP_HD int tree_tile_rows(int max_rows_of_request) { return max_rows_of_request <= 16 ? 16 : max_rows_of_request <= 32 ? 32 : 64; }
+TreePlanLayout tree_plan_layout(const PageDims &pg, int n_heads, int requests, int max_rows, int max_nodes, int stride);
 
 struct TreeAttention {
     PageDims pg;
@@ -55,6 +68,7 @@ struct TreeAttention {
     const __half *q;
     __half *out;
     long long q_stride, out_stride;
+    unsigned page16_inv;               // ceil(2^32 / (page / 16))
 };
 hipError_t launch_tree_plan(const PageDims &pg, const TreeBatch &b, int n_heads, char *plan, hipStream_t s);
 hipError_t launch_tree_attention(const TreeAttention &P, char *plan, hipStream_t s);
