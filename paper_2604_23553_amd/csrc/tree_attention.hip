@@ -2,10 +2,11 @@
 //
 // A node's output is softmax(q K^T / sqrt d) V over its request's cached positions, which every node sees, and the nodes of its
 // own mask.  The query rows of a request that share a key head - its nodes, times the query heads to a key head - are the columns of
-// both products (v_mfma_f32_16x16x32_f16), so a K and V row is read once for up to 64 of them:
+// both products (v_mfma_f32_16x16x32_f16), so a K and V row is read once for up to 128 of them:
 //   S = K Q^T      (16 positions x 16 query rows): a lane holds row lane % 16 and positions 4 (lane / 16) .. + 3
 //   O^T += V^T P^T (16 dimensions x 16 query rows): a lane's 8 K values are the positions of its own scores in two tiles of 16, so
-//                  that P needs no exchange.  V goes through LDS of the wavefront's own, transposed, two positions to a word.
+//                  that P needs no exchange.  V goes through LDS of the wavefront's own, transposed, positions t and t + 16 to a word: a
+//                  lane's 8 values are 16 bytes, and a load from memory covers whole lines.
 // One pass over the positions with the running maximum and sum of the softmax; a workgroup has a piece of a request's positions for one
 // key head, its four wavefronts every fourth row of 32 of them, each with sums of its own that are joined in LDS in order.  Requests of
 // few rows are cut into pieces until the CUs are full (k_tree_plan); the last workgroup of a tile adds the pieces in order.
@@ -20,10 +21,10 @@
 namespace cfpp {
 
 typedef _Float16 ta_f16x8 __attribute__((ext_vector_type(8)));
-typedef _Float16 ta_f16x4 __attribute__((ext_vector_type(4)));
+typedef unsigned ta_u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kTaThreads = 256, kTaWaves = kTaThreads / 64, kTaRow = 32, kTaStep = kTaRow * kTaWaves;
-constexpr int kTaStride = kTaRow + 4;                      // halves between V's dimensions in LDS
+constexpr int kTaStride = kTaRow / 2 + 4;                  // words between V's dimensions in LDS
 constexpr int kTaWgs = 512;                                // workgroups that the pieces aim at
 constexpr float kTaLowest = -3.402823466e38f;
 
@@ -235,27 +236,25 @@ struct TaRow {
             for (int s = 0; s < KS; ++s) k[t][s] = load16_stream(K + w[t].at + (unsigned)min(2 * s + (kg >> 1), D / 16 - 1) * slab + n * 16u + (kg & 1) * 8u);
 #pragma unroll
         for (int u = 0; u < UN; ++u) {
-            const int e = min(lane + 64 * u, D / 8 * (kTaRow / 2) - 1), pc = e / (kTaRow / 2), tp = e % (kTaRow / 2);
-            const __half *from = V + (tp >= 8 ? w[1].at : w[0].at) + (unsigned)(pc >> 1) * slab + (unsigned)(2 * (tp & 7)) * 16u + (pc & 1) * 8u;
+            const int e = min(lane + 64 * u, D / 8 * (kTaRow / 2) - 1), pc = e / (kTaRow / 2), n = e % (kTaRow / 2);
 #pragma unroll
-            for (int i = 0; i < 2; ++i) v[u][i] = load16_stream(from + 16 * i);
+            for (int t = 0; t < 2; ++t) v[u][t] = load16_stream(V + w[t].at + (unsigned)(pc >> 1) * slab + (unsigned)n * 16u + (pc & 1) * 8u);
         }
         __builtin_amdgcn_sched_barrier(0);
     }
     // V, transposed, to LDS: [dimension][kTaStride]; positions from `end` on as zeros
-    __device__ __forceinline__ void store(__half *vt, int row, int end, int lane) const
+    __device__ __forceinline__ void store(unsigned *vt, int row, int end, int lane) const
     {
 #pragma unroll
         for (int u = 0; u < UN; ++u) {
-            const int e = lane + 64 * u, pc = e / (kTaRow / 2), tp = e % (kTaRow / 2), t = row * kTaRow + 2 * tp;
+            const int e = lane + 64 * u, pc = e / (kTaRow / 2), n = e % (kTaRow / 2), t = row * kTaRow + n;
             if (D / 8 * (kTaRow / 2) % 64 != 0 && e >= D / 8 * (kTaRow / 2)) break;
-            const bool ok = tp >= 8 ? good[1] : good[0];
-            const u32x4 a = ok && t < end ? v[u][0] : u32x4{0u, 0u, 0u, 0u}, b = ok && t + 1 < end ? v[u][1] : u32x4{0u, 0u, 0u, 0u};
-            unsigned *to = reinterpret_cast<unsigned *>(vt + 8 * pc * kTaStride) + tp;
+            const u32x4 a = good[0] && t < end ? v[u][0] : u32x4{0u, 0u, 0u, 0u}, b = good[1] && t + 16 < end ? v[u][1] : u32x4{0u, 0u, 0u, 0u};
+            unsigned *to = vt + 8 * pc * kTaStride + n;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                to[2 * j * (kTaStride / 2)] = __builtin_amdgcn_perm(b[j], a[j], 0x05040100u);
-                to[(2 * j + 1) * (kTaStride / 2)] = __builtin_amdgcn_perm(b[j], a[j], 0x07060302u);
+                to[2 * j * kTaStride] = __builtin_amdgcn_perm(b[j], a[j], 0x05040100u);
+                to[(2 * j + 1) * kTaStride] = __builtin_amdgcn_perm(b[j], a[j], 0x07060302u);
             }
         }
     }
@@ -294,8 +293,8 @@ __device__ __forceinline__ unsigned ta_window(const unsigned *words, int n_words
     return __funnelshift_r(word(w), word(w + 1), sh);
 }
 
-// One wavefront, one query row: its sums over the wavefront's rows in fp32, position by position, unseen ones left out
-template <int D>
+// One wavefront, one query row: its sums over rows row0, row0 + STEP .. of the piece in fp32, position by position, unseen ones left out
+template <int D, int STEP>
 __device__ __forceinline__ void ta_alone(const TreeAttention &P, const TreeItem &it, const TaPages &pages, const __half *K, const __half *V, const unsigned *mask,
                                          const __half *q, int row0, int lane, float *o_out, float *m_out, float *l_out)
 {
@@ -311,7 +310,7 @@ __device__ __forceinline__ void ta_alone(const TreeAttention &P, const TreeItem 
         qs[e] = lane + 64 * e < D ? __half2float(q[dim]) : 0.f;
         o[e] = 0.f;
     }
-    for (int row = row0; row * kTaRow < it.t1; row += kTaWaves) {
+    for (int row = row0; row * kTaRow < it.t1; row += STEP) {
         for (int t = row * kTaRow; t < min(row * kTaRow + kTaRow, it.t1); ++t) {
             const int node = t - it.len;
             if (node >= 0 && !((mask[node >> 5] >> (node & 31)) & 1)) continue;        // (uniform)
@@ -334,73 +333,212 @@ __device__ __forceinline__ void ta_alone(const TreeAttention &P, const TreeItem 
     if (lane == 0) { *m_out = m; *l_out = l; }
 }
 
+// four dimensions of a query row's output
 template <int D>
-constexpr int ta_lds()                                     // V; then the wavefronts' sums of 16 query rows
+__device__ __forceinline__ void ta_deliver(const TreeAttention &P, const TreeItem &it, int head, int qr, int dim, f32x4 s, float l)
 {
-    const int v = kTaWaves * D * kTaStride * 2, w = kTaWaves * 16 * (D + 2) * 4;
+    const int G = P.group, node = qr / G, qh = head * G + (qr - node * G);
+    f32x4 v = s / l;
+    if (l == 0.f) {                                        // every score was minus infinity, or nothing is seen
+        const int words = tree_words(P.b.max_nodes);
+        bool any = it.len > 0;
+        for (int w = 0; w < words; ++w) {
+            const int left = it.nodes - 32 * w;
+            any = any || (left > 0 && (P.b.masks[(size_t)(it.first + node) * words + w] & (left < 32 ? (1u << left) - 1u : ~0u)));
+        }
+        const float z = any ? NAN : 0.f;
+        v = f32x4{z, z, z, z};
+    }
+    ta_u32x2 o;
+    o.x = (unsigned)__half_as_ushort(__float2half_rn(v[0])) | (unsigned)__half_as_ushort(__float2half_rn(v[1])) << 16;
+    o.y = (unsigned)__half_as_ushort(__float2half_rn(v[2])) | (unsigned)__half_as_ushort(__float2half_rn(v[3])) << 16;
+    *as_global(reinterpret_cast<ta_u32x2 *>(P.out + (size_t)(it.first + node) * P.out_stride + (size_t)qh * D + dim)) = o;
+}
+
+// Where a tile's pieces leave their sums: [piece][key head], each [row][D] and then (maximum, weight) of each row
+template <int D>
+struct TaSlot {
+    float *p;
+    int tile_rows;
+    __device__ __forceinline__ void put(int i, int dim, f32x4 s) const
+    {
+        xwg_store2(p + i * D + dim, s[0], s[1]);
+        xwg_store2(p + i * D + dim + 2, s[2], s[3]);
+    }
+    __device__ __forceinline__ void put_ml(int i, float m, float l) const { xwg_store2(p + tile_rows * D + 2 * i, m, l); }
+};
+template <int D>
+__device__ __forceinline__ TaSlot<D> ta_slot(const TreePlanLayout &L, char *plan, const TreeItem &it, int H, int head, int piece)
+{
+    return TaSlot<D>{reinterpret_cast<float *>(plan + L.sums) + ((size_t)max(it.slot + piece, 0) * H + head) * ((size_t)L.tile_rows * (D + 2)), L.tile_rows};
+}
+
+// The tile's last workgroup adds the pieces in order.
+template <int D>
+__device__ __forceinline__ void ta_join(const TreeAttention &P, const TreePlanLayout &L, char *plan, const TreeItem &it, int H, int head, int rows, int *last_one)
+{
+    constexpr int D4 = D / 4;
+    const int tid = threadIdx.x;
+    unsigned *counter = reinterpret_cast<unsigned *>(plan + L.counters) + (size_t)it.counter * H + head;
+    xwg_wait_stores();
+    __syncthreads();
+    if (tid == 0) *last_one = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (unsigned)it.pieces - 1;
+    __syncthreads();
+    if (!*last_one) return;
+    const float *from = ta_slot<D>(L, plan, it, H, head, 0).p;
+    const size_t step = (size_t)H * L.tile_rows * (D + 2);                 // from piece to piece
+    for (int e = tid; e < rows * D4; e += kTaThreads) {
+        const int i = e / D4, dim = 4 * (e - i * D4);
+        float M = kTaLowest, l = 0.f;
+        f32x4 s = {0.f, 0.f, 0.f, 0.f};
+        constexpr int AT = 8;                              // in flight together (past the last: the last again)
+        for (int z = 0; z < it.pieces; z += AT) {
+            float2 ml[AT];
+            f32x4 a[AT];
+#pragma unroll
+            for (int u = 0; u < AT; ++u) {
+                const float *f = from + (size_t)min(z + u, it.pieces - 1) * step;
+                ml[u] = xwg_load2(f + L.tile_rows * D + 2 * i);
+                const float2 lo = xwg_load2(f + i * D + dim), hi = xwg_load2(f + i * D + dim + 2);
+                a[u] = f32x4{lo.x, lo.y, hi.x, hi.y};
+            }
+#pragma unroll
+            for (int u = 0; u < AT; ++u) {
+                if (z + u >= it.pieces) continue;          // (uniform)
+                const float mn = fmaxf(M, ml[u].x), c0 = __builtin_amdgcn_exp2f(M - mn), c1 = __builtin_amdgcn_exp2f(ml[u].x - mn);
+                l = l * c0 + ml[u].y * c1;
+                s = s * c0 + a[u] * c1;
+                M = mn;
+            }
+        }
+        ta_deliver<D>(P, it, head, it.tile * L.tile_rows + i, dim, s, l);
+    }
+    if (tid == 0) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+// What the workgroups of both kernels begin with
+template <int D, int TQ>
+struct TaStart {
+    TreeItem it;
+    int head, rows, n_rows;            // key head; query rows of the tile, of the request
+    const __half *K, *V;
+    unsigned slab;
+    TaPages pages;
+    __device__ __forceinline__ bool of(const TreeAttention &P, const TreePlanLayout &L, const char *plan)
+    {
+        const int H = P.pg.heads, item = (int)blockIdx.x / H;
+        head = (int)blockIdx.x - item * H;
+        const TreePlanHead &plan_head = *reinterpret_cast<const TreePlanHead *>(plan);
+        it = reinterpret_cast<const TreeItem *>(plan + L.items)[item];
+        if (plan_head.key != L.key || item >= plan_head.items) return false;           // (a plan that was made for other sizes, or never)
+        n_rows = it.nodes * P.group;
+        rows = min(TQ, n_rows - it.tile * TQ);
+        K = P.pool; V = P.pool + page_which_elems(P.pg);
+        slab = (unsigned)P.pg.page * 16u;
+        pages.table = P.b.table + (size_t)it.request * P.b.stride;
+        pages.page16 = P.pg.page >> 4; pages.n_pages = P.pg.n_pages; pages.last = (it.t1 - 1) >> 4; pages.inv = P.page16_inv;
+        pages.per_page = (size_t)H * page_head_elems(P.pg);
+        pages.head = (size_t)head * page_head_elems(P.pg);
+        return true;
+    }
+    // masks of the tile's query rows; those past the last are the last again (a barrier behind it)
+    __device__ __forceinline__ void masks(const TreeAttention &P, unsigned (*smask)[kTreeMaxNodes / 32]) const
+    {
+        const int words = tree_words(P.b.max_nodes);
+        for (int e = threadIdx.x; e < TQ * words; e += kTaThreads) {
+            const int i = e / words, node = min(it.tile * TQ + i, n_rows - 1) / P.group;
+            smask[i][e - i * words] = P.b.masks[(size_t)(it.first + node) * words + (e - i * words)];
+        }
+    }
+    // query row i of the tile: node (tile TQ + i) / G, query head (head G + the rest)
+    __device__ __forceinline__ const __half *query(const TreeAttention &P, int i) const
+    {
+        const int G = P.group, qr = min(it.tile * TQ + i, n_rows - 1), node = qr / G;
+        return P.q + (size_t)(it.first + node) * P.q_stride + (size_t)(head * G + (qr - node * G)) * D;
+    }
+    // Q^T: dimensions 32 s + 8 kg .. + 7 of a query row
+    __device__ __forceinline__ u32x4 fragment(const TreeAttention &P, int i, int s, int kg) const
+    {
+        const bool real = D % 32 == 0 || 32 * s + 8 * kg < D;
+        u32x4 x = load16(query(P, i) + (real ? 32 * s + 8 * kg : 0));
+        if (!real) x = u32x4{0u, 0u, 0u, 0u};
+        return x;
+    }
+};
+
+// A query tile's 16 rows and 32 positions: scores (of this lane: row lane % 16, positions 4 (lane / 16) .. + 3 of both granules) to weights, and the
+// sums so far to the new maximum.  window: which positions the row sees, where `masked`.
+template <int NT>
+__device__ __forceinline__ void ta_weights(f32x4 (&S)[2], float scale, bool masked, const bool (&good)[2], unsigned window, int kg, float &m_run, float &l_run,
+                                           f32x4 (&O)[NT], ta_f16x8 &ph, ta_f16x8 &pl)
+{
+    float most = -INFINITY;
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            float s = S[t][e] * scale;
+            if (masked) {
+                s = good[t] ? s : NAN;
+                s = (window >> (16 * t + 4 * kg + e)) & 1 ? s : -INFINITY;
+            }
+            S[t][e] = s;
+            most = fmaxf(most, s);
+        }
+    most = ta_max4(most);
+    if (__any(most > m_run)) {
+        const float mn = fmaxf(m_run, most), corr = __builtin_amdgcn_exp2f(m_run - mn);
+        m_run = mn;
+        l_run *= corr;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) O[t] *= corr;
+    }
+    const float base = m_run - kTaUp;
+    float sum = 0.f;
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float p = split_value(__builtin_amdgcn_exp2f(S[t][e] - base));
+            const _Float16 h = (_Float16)p;
+            sum += p;
+            ph[2 * e + t] = h;
+            pl[2 * e + t] = (_Float16)(p - (float)h);
+        }
+    l_run += sum;
+}
+
+// ---- up to 32 query rows: the wavefronts share the positions --------------------------------------------
+template <int D, int QT>
+constexpr int ta_lds()                                     // V, or the wavefronts' sums
+{
+    const int v = kTaWaves * D * kTaStride * 4, w = kTaWaves * 16 * QT * (D + 2) * 4;
     return v > w ? v : w;
 }
 
 template <int D, int QT>
 __global__ void __launch_bounds__(kTaThreads, 2) k_tree_attention(TreeAttention P, TreePlanLayout L, char *plan)
 {
-    constexpr int KS = TaRow<D>::KS, NT = D / 16, TQ = 16 * QT, W = kTaWaves;
-    __shared__ __align__(16) char mem[ta_lds<D>()];
-    constexpr bool LDS_Q = QT * KS > 8;
-    __shared__ __align__(16) u32x4 sq[LDS_Q ? QT * KS : 1][LDS_Q ? 64 : 1];
+    constexpr int KS = TaRow<D>::KS, NT = D / 16, TQ = 16 * QT, W = kTaWaves, D4 = D / 4;
+    __shared__ __align__(16) char mem[ta_lds<D, QT>()];
     __shared__ unsigned smask[TQ][kTreeMaxNodes / 32];
     __shared__ int last_one;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 15, kg = lane >> 4;
-    const int H = P.pg.heads, item = (int)blockIdx.x / H, head = (int)blockIdx.x - item * H;
-    const TreePlanHead &plan_head = *reinterpret_cast<const TreePlanHead *>(plan);
-    if (plan_head.key != L.key || item >= plan_head.items) return;     // (a plan that was made for other sizes, or never)
-    const TreeItem it = reinterpret_cast<const TreeItem *>(plan + L.items)[item];
-    const int G = P.group, words = tree_words(P.b.max_nodes), n_rows = it.nodes * G;
-    const __half *K = P.pool, *V = P.pool + page_which_elems(P.pg);
-    const unsigned slab = (unsigned)P.pg.page * 16u;
-    TaPages pages;
-    pages.table = P.b.table + (size_t)it.request * P.b.stride;
-    pages.page16 = P.pg.page >> 4; pages.n_pages = P.pg.n_pages; pages.last = (it.t1 - 1) >> 4; pages.inv = P.page16_inv;
-    pages.per_page = (size_t)H * page_head_elems(P.pg);
-    pages.head = (size_t)head * page_head_elems(P.pg);
+    TaStart<D, TQ> w;
+    if (!w.of(P, L, plan)) return;
+    const TreeItem &it = w.it;
+    const int n_tiles = (w.rows + 15) >> 4, words = tree_words(P.b.max_nodes);         // query tiles that have a row
     TaRow<D> r;
     const int row0 = it.t0 / kTaRow + wave;
-    r.request(K, V, pages, slab, row0, lane);
-    // query rows: node (tile TQ + i) / G, query head (head G + the rest); those past the last are the last again
+    r.request(w.K, w.V, w.pages, w.slab, row0, lane);
     const bool tail = it.t1 > it.len;
-    if (tail) {
-        for (int e = tid; e < TQ * words; e += kTaThreads) {
-            const int i = e / words, node = min(it.tile * TQ + i, n_rows - 1) / G;
-            smask[i][e - i * words] = P.b.masks[(size_t)(it.first + node) * words + (e - i * words)];
-        }
-    }
-    auto query = [&](int i) {
-        const int qr = min(it.tile * TQ + i, n_rows - 1), node = qr / G;
-        return P.q + (size_t)(it.first + node) * P.q_stride + (size_t)(head * G + (qr - node * G)) * D;
-    };
-    // Q^T: dimensions 32 s + 8 kg .. + 7 of query row col; in registers, or, where these are short, in LDS
-    auto fragment = [&](int j, int s) {
-        const bool real = D % 32 == 0 || 32 * s + 8 * kg < D;
-        u32x4 x = load16(query(16 * j + col) + (real ? 32 * s + 8 * kg : 0));
-        if (!real) x = u32x4{0u, 0u, 0u, 0u};
-        return x;
-    };
-    u32x4 Qr[LDS_Q ? 1 : QT][LDS_Q ? 1 : KS];
-    if constexpr (LDS_Q) {
-        for (int j = wave; j < QT; j += W)
+    if (tail) w.masks(P, smask);
+    u32x4 Q[QT][KS];
 #pragma unroll
-            for (int s = 0; s < KS; ++s) sq[j * KS + s][lane] = fragment(j, s);
-    } else {
+    for (int j = 0; j < QT; ++j)
 #pragma unroll
-        for (int j = 0; j < QT; ++j)
-#pragma unroll
-            for (int s = 0; s < KS; ++s) Qr[j][s] = fragment(j, s);
-    }
-    if (tail || LDS_Q) __syncthreads();                    // (uniform)
-    auto Q = [&](int j, int s) -> ta_f16x8 {
-        if constexpr (LDS_Q) return __builtin_bit_cast(ta_f16x8, sq[j * KS + s][lane]);
-        else return __builtin_bit_cast(ta_f16x8, Qr[j][s]);
-    };
+        for (int s = 0; s < KS; ++s) Q[j][s] = w.fragment(P, 16 * j + col, s, kg);
+    if (tail) __syncthreads();                             // (uniform)
     const float scale = 1.44269504088896340736f / sqrtf((float)D);
     f32x4 O[QT][NT];
     float m_run[QT], l_run[QT];                            // l_run: of this lane's positions
@@ -411,7 +549,7 @@ __global__ void __launch_bounds__(kTaThreads, 2) k_tree_attention(TreeAttention 
 #pragma unroll
         for (int t = 0; t < NT; ++t) O[j][t] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    __half *vt = reinterpret_cast<__half *>(mem) + wave * D * kTaStride;
+    unsigned *vt = reinterpret_cast<unsigned *>(mem) + wave * D * kTaStride;
     for (int row = row0; row * kTaRow < it.t1; row += W) {
         r.store(vt, row, it.t1, lane);
         asm volatile("" ::: "memory");                     // (LDS takes a wavefront's accesses in order)
@@ -425,170 +563,280 @@ __global__ void __launch_bounds__(kTaThreads, 2) k_tree_attention(TreeAttention 
                 u32x4 k = r.k[t][s];
                 if (D % 32 != 0 && s == KS - 1 && 32 * s + 8 * kg >= D) k = u32x4{0u, 0u, 0u, 0u};
 #pragma unroll
-                for (int j = 0; j < QT; ++j) S[j][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(ta_f16x8, k), Q(j, s), S[j][t], 0, 0, 0);
+                for (int j = 0; j < QT; ++j)
+                    if (j < n_tiles) S[j][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(ta_f16x8, k), __builtin_bit_cast(ta_f16x8, Q[j][s]), S[j][t], 0, 0, 0);
             }
         }
         const bool good[2] = {r.good[0], r.good[1]};
-        r.request(K, V, pages, slab, row + W, lane);
+        r.request(w.K, w.V, w.pages, w.slab, row + W, lane);
         const bool masked = row * kTaRow + kTaRow > it.len || !good[0] || !good[1];    // (uniform)
-        ta_f16x8 ph[QT], pl[QT];
+        ta_f16x8 ph[QT], pl[QT];                           // element 2 e + t: position 16 t + 4 kg + e
 #pragma unroll
         for (int j = 0; j < QT; ++j) {
+            if (j >= n_tiles) continue;
             unsigned window = ~0u;
             if (masked) window = ta_window(smask[16 * j + col], words, row * kTaRow, it.len, it.nodes);
-            float most = -INFINITY;
-#pragma unroll
-            for (int t = 0; t < 2; ++t)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    float s = S[j][t][e] * scale;
-                    if (masked) {
-                        s = good[t] ? s : NAN;
-                        s = (window >> (16 * t + 4 * kg + e)) & 1 ? s : -INFINITY;
-                    }
-                    S[j][t][e] = s;
-                    most = fmaxf(most, s);
-                }
-            most = ta_max4(most);
-            if (__any(most > m_run[j])) {
-                const float mn = fmaxf(m_run[j], most), corr = __builtin_amdgcn_exp2f(m_run[j] - mn);
-                m_run[j] = mn;
-                l_run[j] *= corr;
-#pragma unroll
-                for (int t = 0; t < NT; ++t) O[j][t] *= corr;
-            }
-            const float base = m_run[j] - kTaUp;
-            float sum = 0.f;
-#pragma unroll
-            for (int t = 0; t < 2; ++t)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float p = split_value(__builtin_amdgcn_exp2f(S[j][t][e] - base));
-                    const _Float16 h = (_Float16)p;
-                    sum += p;
-                    ph[j][4 * t + e] = h;
-                    pl[j][4 * t + e] = (_Float16)(p - (float)h);
-                }
-            l_run[j] += sum;
+            ta_weights(S[j], scale, masked, good, window, kg, m_run[j], l_run[j], O[j], ph[j], pl[j]);
         }
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-            const __half *at = vt + (16 * t + col) * kTaStride + 4 * kg;
-            const ta_f16x4 v0 = *reinterpret_cast<const ta_f16x4 *>(at), v1 = *reinterpret_cast<const ta_f16x4 *>(at + 16);
-            const ta_f16x8 v = __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7);
+            const ta_f16x8 v = __builtin_bit_cast(ta_f16x8, *reinterpret_cast<const u32x4 *>(vt + (16 * t + col) * kTaStride + 4 * kg));
 #pragma unroll
-            for (int j = 0; j < QT; ++j) {
-                O[j][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, ph[j], O[j][t], 0, 0, 0);
-                O[j][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, pl[j], O[j][t], 0, 0, 0);
-            }
+            for (int j = 0; j < QT; ++j)
+                if (j < n_tiles) {
+                    O[j][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, ph[j], O[j][t], 0, 0, 0);
+                    O[j][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, pl[j], O[j][t], 0, 0, 0);
+                }
         }
         asm volatile("" ::: "memory");
     }
-    // The wavefronts' sums, 16 query rows at a time: maxima and weights [wave][row], sums [wave][row][D] in the place of V
-    float *wp = reinterpret_cast<float *>(mem), *wm = wp + W * 16 * D, *wl = wm + W * 16;
-    float *sums = reinterpret_cast<float *>(plan + L.sums);
-    const size_t slot_size = (size_t)TQ * (D + 2);
-    float *slot = sums + ((size_t)(it.slot + it.piece) * H + head) * slot_size;        // (single pieces: not used)
-    auto deliver = [&](int i, int dim, float s, float l) {
-        const int qr = it.tile * TQ + i;
-        if (qr >= n_rows) return;
-        const int node = qr / G, qh = head * G + (qr - node * G);
-        float v = s / l;
-        if (l == 0.f) {                                    // every score was minus infinity, or nothing is seen
-            bool any = it.len > 0;
-            for (int w = 0; w < words; ++w) {
-                const int left = it.nodes - 32 * w;
-                any = any || (left > 0 && (P.b.masks[(size_t)(it.first + node) * words + w] & (left < 32 ? (1u << left) - 1u : ~0u)));
-            }
-            v = any ? NAN : 0.f;
-        }
-        P.out[(size_t)(it.first + node) * P.out_stride + (size_t)qh * D + dim] = __float2half_rn(v);
-    };
+    // The wavefronts' sums: [wave][row][D], maxima and weights [wave][row], in the place of V
+    float *wp = reinterpret_cast<float *>(mem), *wm = wp + W * TQ * D, *wl = wm + W * TQ;
+    __syncthreads();                                       // V has been read
 #pragma unroll
     for (int j = 0; j < QT; ++j) {
+        const int at = wave * TQ + 16 * j;
+        if (j >= n_tiles) continue;
         const float l = ta_sum4(l_run[j]);
+        bool finite = fabsf(l) < INFINITY;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) finite = finite && fabsf(O[j][t][e]) < INFINITY;
+            *reinterpret_cast<f32x4 *>(wp + (at + col) * D + 16 * t + 4 * kg) = O[j][t];
+        }
+        if (kg == 0) { wm[at + col] = m_run[j]; wl[at + col] = l; }
+        const unsigned long long again = __ballot(!finite);            // (bit i: query row i % 16)
+        if (again) {                                       // (uniform)
+            asm volatile("" ::: "memory");
+            for (int i = 0; i < 16; ++i)
+                if (again & (0x0001000100010001ull << i))
+                    ta_alone<D, W>(P, it, w.pages, w.K, w.V, smask[16 * j + i], w.query(P, 16 * j + i), row0, lane, wp + (at + i) * D, wm + at + i, wl + at + i);
+        }
+    }
+    __syncthreads();
+    const TaSlot<D> slot = ta_slot<D>(L, plan, it, P.pg.heads, w.head, it.piece);
+    for (int e = tid; e < w.rows * D4; e += kTaThreads) {
+        const int i = e / D4, dim = 4 * (e - i * D4);
+        float M = wm[i], l = 0.f;
+        f32x4 s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int v = 1; v < W; ++v) M = fmaxf(M, wm[v * TQ + i]);
+#pragma unroll
+        for (int v = 0; v < W; ++v) {
+            const float ew = __builtin_amdgcn_exp2f(wm[v * TQ + i] - M);
+            l += wl[v * TQ + i] * ew;
+            s += *reinterpret_cast<const f32x4 *>(wp + (v * TQ + i) * D + dim) * ew;
+        }
+        if (it.pieces == 1) {
+            ta_deliver<D>(P, it, w.head, it.tile * TQ + i, dim, s, l);
+        } else {
+            slot.put(i, dim, s);
+            if (dim == 0) slot.put_ml(i, M, l);
+        }
+    }
+    if (it.pieces > 1) ta_join<D>(P, L, plan, it, P.pg.heads, w.head, w.rows, &last_one);
+}
+
+// ---- more query rows: the wavefronts share the rows -------------------------------------------------------
+// A tile of 64 positions goes through LDS for all four wavefronts, K as it is and V transposed as above, in two buffers: while one is
+// multiplied the next tile is on its way in registers.  A wavefront has 16 QT query rows and all positions of the piece, so
+// nothing is joined but the pieces.
+constexpr int kTwPos = 64;
+template <int D>
+struct TwLds {
+    static constexpr int ks = D * 2 + 16, vs = (kTwPos / 2 + 4) * 4;       // bytes from position to position of K, from dimension to dimension of V
+    static constexpr int k = kTwPos * ks, v = D * vs, bytes = 2 * (k + v);
+};
+
+template <int D, int QT>
+__global__ void __launch_bounds__(kTaThreads, 2) k_tree_attention_wide(TreeAttention P, TreePlanLayout L, char *plan)
+{
+    using Lds = TwLds<D>;
+    constexpr int KS = TaRow<D>::KS, NT = D / 16, RW = 16 * QT, TQ = kTaWaves * RW;
+    // pieces of 16 bytes a thread: K as (slab, position, half), V as (8 dimensions, position of 16 granules two by two)
+    constexpr int KN = kTwPos * (D / 8), VN = (kTwPos / 2) * (D / 8), KU = (KN + kTaThreads - 1) / kTaThreads, VU = (VN + kTaThreads - 1) / kTaThreads;
+    extern __shared__ __align__(16) char tw_mem[];
+    __shared__ unsigned smask[TQ][kTreeMaxNodes / 32];
+    __shared__ int last_one;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 15, kg = lane >> 4;
+    TaStart<D, TQ> w;
+    if (!w.of(P, L, plan)) return;
+    const TreeItem &it = w.it;
+    const int words = tree_words(P.b.max_nodes);
+    const int n_tiles = min(QT, max(0, (w.rows - wave * RW + 15) >> 4));               // this wavefront's query tiles that have a row
+    u32x4 rk[KU], rv[VU][2];
+    unsigned good = 0;                                     // of the tile on its way: bit g: granule g lies in a page of the pool
+    auto request = [&](int t) {
+        TaPlace pl[4];
+        good = 0;
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            pl[g] = w.pages.place((t >> 4) + g);
+            good |= (unsigned)pl[g].good << g;
+        }
+        auto at = [&](int g) { return g == 0 ? pl[0].at : g == 1 ? pl[1].at : g == 2 ? pl[2].at : pl[3].at; };
+#pragma unroll
+        for (int u = 0; u < KU; ++u) {
+            const int e = min(tid + kTaThreads * u, KN - 1), half = e & 1, n = (e >> 1) & 15, g = (e >> 5) & 3, s = e >> 7;
+            rk[u] = load16(w.K + at(g) + (unsigned)s * w.slab + (unsigned)n * 16u + half * 8u);
+        }
+#pragma unroll
+        for (int u = 0; u < VU; ++u) {
+            const int e = min(tid + kTaThreads * u, VN - 1), n = e & 15, half = (e >> 4) & 1, g2 = (e >> 5) & 1, s = e >> 6;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) rv[u][i] = load16(w.V + at(2 * g2 + i) + (unsigned)s * w.slab + (unsigned)n * 16u + half * 8u);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    auto store = [&](char *buf, int t) {
+#pragma unroll
+        for (int u = 0; u < KU; ++u) {
+            const int e = tid + kTaThreads * u, half = e & 1, n = (e >> 1) & 15, g = (e >> 5) & 3, s = e >> 7;
+            if (KN % kTaThreads != 0 && e >= KN) break;
+            *reinterpret_cast<u32x4 *>(buf + (16 * g + n) * Lds::ks + s * 32 + half * 16) = rk[u];
+        }
+#pragma unroll
+        for (int u = 0; u < VU; ++u) {
+            const int e = tid + kTaThreads * u, n = e & 15, half = (e >> 4) & 1, g2 = (e >> 5) & 1, s = e >> 6, p = t + 32 * g2 + n;
+            if (VN % kTaThreads != 0 && e >= VN) break;
+            const u32x4 zero = {0u, 0u, 0u, 0u};           // positions from the piece's end on
+            const u32x4 a = (good >> (2 * g2)) & 1 && p < it.t1 ? rv[u][0] : zero, b = (good >> (2 * g2 + 1)) & 1 && p + 16 < it.t1 ? rv[u][1] : zero;
+            char *to = buf + Lds::k + (16 * s + 8 * half) * Lds::vs + (16 * g2 + n) * 4;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                *reinterpret_cast<unsigned *>(to + 2 * j * Lds::vs) = __builtin_amdgcn_perm(b[j], a[j], 0x05040100u);
+                *reinterpret_cast<unsigned *>(to + (2 * j + 1) * Lds::vs) = __builtin_amdgcn_perm(b[j], a[j], 0x07060302u);
+            }
+        }
+    };
+    request(it.t0);
+    if (it.t1 > it.len) w.masks(P, smask);
+    u32x4 Q[QT][KS];
+#pragma unroll
+    for (int j = 0; j < QT; ++j)
+#pragma unroll
+        for (int s = 0; s < KS; ++s) Q[j][s] = w.fragment(P, wave * RW + 16 * j + col, s, kg);
+    const float scale = 1.44269504088896340736f / sqrtf((float)D);
+    f32x4 O[QT][NT];
+    float m_run[QT], l_run[QT];
+#pragma unroll
+    for (int j = 0; j < QT; ++j) {
+        m_run[j] = kTaLowest;
+        l_run[j] = 0.f;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) O[j][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    store(tw_mem, it.t0);
+    unsigned now = good;
+    __syncthreads();
+    int side = 0;
+    for (int t0 = it.t0; t0 < it.t1; t0 += kTwPos, side ^= 1) {
+        const char *kb = tw_mem + side * (Lds::k + Lds::v), *vb = kb + Lds::k;
+        const bool more = t0 + kTwPos < it.t1;             // (uniform)
+        if (more) request(t0 + kTwPos);
+#pragma unroll 1
+        for (int half = 0; half < 2; ++half) {             // (one at a time: registers)
+            const int row = t0 + 32 * half;
+            if (row >= it.t1) break;                       // (uniform)
+            const bool two[2] = {((now >> (2 * half)) & 1) != 0, ((now >> (2 * half + 1)) & 1) != 0};
+            const bool masked = row + 32 > it.len || !two[0] || !two[1];
+            f32x4 S[QT][2];
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+#pragma unroll
+                for (int j = 0; j < QT; ++j) S[j][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int s = 0; s < KS; ++s) {
+                    const bool real = D % 32 == 0 || 32 * s + 8 * kg < D;
+                    u32x4 k = *reinterpret_cast<const u32x4 *>(kb + (32 * half + 16 * t + col) * Lds::ks + (real ? 64 * s + 16 * kg : 0));
+                    if (!real) k = u32x4{0u, 0u, 0u, 0u};
+#pragma unroll
+                    for (int j = 0; j < QT; ++j)
+                        if (j < n_tiles) S[j][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(ta_f16x8, k), __builtin_bit_cast(ta_f16x8, Q[j][s]), S[j][t], 0, 0, 0);
+                }
+            }
+            ta_f16x8 ph[QT], pl[QT];
+#pragma unroll
+            for (int j = 0; j < QT; ++j) {
+                if (j >= n_tiles) continue;
+                unsigned window = ~0u;
+                if (masked) window = ta_window(smask[wave * RW + 16 * j + col], words, row, it.len, it.nodes);
+                ta_weights(S[j], scale, masked, two, window, kg, m_run[j], l_run[j], O[j], ph[j], pl[j]);
+            }
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                const ta_f16x8 v = __builtin_bit_cast(ta_f16x8, *reinterpret_cast<const u32x4 *>(vb + (16 * t + col) * Lds::vs + 64 * half + 16 * kg));
+#pragma unroll
+                for (int j = 0; j < QT; ++j)
+                    if (j < n_tiles) {
+                        O[j][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, ph[j], O[j][t], 0, 0, 0);
+                        O[j][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, pl[j], O[j][t], 0, 0, 0);
+                    }
+            }
+        }
+        if (more) {
+            store(tw_mem + (side ^ 1) * (Lds::k + Lds::v), t0 + kTwPos);   // (read last ahead of the barrier before this tile)
+            now = good;
+        }
+        __syncthreads();
+    }
+    const TaSlot<D> slot = ta_slot<D>(L, plan, it, P.pg.heads, w.head, it.piece);
+#pragma unroll
+    for (int j = 0; j < QT; ++j) {
+        if (j >= n_tiles) continue;
+        const int i = wave * RW + 16 * j + col;
+        float l = ta_sum4(l_run[j]);
         bool finite = fabsf(l) < INFINITY;
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
             for (int e = 0; e < 4; ++e) finite = finite && fabsf(O[j][t][e]) < INFINITY;
-        const unsigned long long again = __ballot(!finite);            // (bit i: query row i % 16)
-        __syncthreads();                                   // V, or the rows before these, have been read
-#pragma unroll
-        for (int t = 0; t < NT; ++t) *reinterpret_cast<f32x4 *>(wp + (wave * 16 + col) * D + 16 * t + 4 * kg) = O[j][t];
-        if (kg == 0) { wm[wave * 16 + col] = m_run[j]; wl[wave * 16 + col] = l; }
-        if (again) {                                       // (uniform)
+        const unsigned long long again = __ballot(!finite);
+        if (again) {                                       // (uniform) rows worked out once more, through LDS that no one needs now
+            float *o = reinterpret_cast<float *>(tw_mem) + wave * 16 * (D + 2);
+            for (int q = 0; q < 16; ++q)
+                if (again & (0x0001000100010001ull << q))
+                    ta_alone<D, 1>(P, it, w.pages, w.K, w.V, smask[wave * RW + 16 * j + q], w.query(P, wave * RW + 16 * j + q), it.t0 / kTaRow, lane, o + q * (D + 2),
+                                   o + q * (D + 2) + D, o + q * (D + 2) + D + 1);
             asm volatile("" ::: "memory");
-            for (int i = 0; i < 16; ++i)
-                if (again & (0x0001000100010001ull << i))
-                    ta_alone<D>(P, it, pages, K, V, smask[16 * j + i], query(16 * j + i), row0, lane, wp + (wave * 16 + i) * D, wm + wave * 16 + i, wl + wave * 16 + i);
-        }
-        __syncthreads();
-        for (int e = tid; e < 16 * D; e += kTaThreads) {
-            const int i = e / D, dim = e - i * D;
-            float M = wm[i], l = 0.f, s = 0.f;
+            if (again & (0x0001000100010001ull << col)) {
+                const float *mine = o + col * (D + 2);
 #pragma unroll
-            for (int w = 1; w < W; ++w) M = fmaxf(M, wm[w * 16 + i]);
+                for (int t = 0; t < NT; ++t)
 #pragma unroll
-            for (int w = 0; w < W; ++w) {
-                const float ew = __builtin_amdgcn_exp2f(wm[w * 16 + i] - M);
-                l += wl[w * 16 + i] * ew;
-                s += wp[(w * 16 + i) * D + dim] * ew;
-            }
-            if (it.pieces == 1) {
-                deliver(16 * j + i, dim, s, l);
-            } else {
-                xwg_store(slot + (16 * j + i) * D + dim, s);
-                if (dim == 0) { xwg_store(slot + TQ * D + 16 * j + i, M); xwg_store(slot + TQ * D + TQ + 16 * j + i, l); }
+                    for (int e = 0; e < 4; ++e) O[j][t][e] = mine[16 * t + 4 * kg + e];
+                m_run[j] = mine[D];
+                l = mine[D + 1];
             }
         }
+        if (i >= w.rows) continue;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            if (it.pieces == 1) ta_deliver<D>(P, it, w.head, it.tile * TQ + i, 16 * t + 4 * kg, O[j][t], l);
+            else slot.put(i, 16 * t + 4 * kg, O[j][t]);
+        }
+        if (it.pieces > 1 && kg == 0) slot.put_ml(i, m_run[j], l);
     }
-    if (it.pieces == 1) return;
-    // the tile's last workgroup adds the pieces in order
-    unsigned *counter = reinterpret_cast<unsigned *>(plan + L.counters) + (size_t)it.counter * H + head;
-    xwg_wait_stores();
-    __syncthreads();
-    if (tid == 0) last_one = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (unsigned)it.pieces - 1;
-    __syncthreads();
-    if (!last_one) return;
-    const float *from = sums + ((size_t)it.slot * H + head) * slot_size;
-    const size_t step = (size_t)H * slot_size;             // from piece to piece
-    const int rows = min(TQ, n_rows - it.tile * TQ);
-    for (int e = tid; e < rows * D; e += kTaThreads) {
-        const int i = e / D, dim = e - i * D;
-        float M = kTaLowest, l = 0.f, s = 0.f;
-        constexpr int AT = 8;                              // in flight together (past the last: the last again)
-        for (int z = 0; z < it.pieces; z += AT) {
-            float mj[AT], lj[AT], oj[AT];
-#pragma unroll
-            for (int u = 0; u < AT; ++u) {
-                const float *f = from + (size_t)min(z + u, it.pieces - 1) * step;
-                mj[u] = xwg_load(f + TQ * D + i);
-                lj[u] = xwg_load(f + TQ * D + TQ + i);
-                oj[u] = xwg_load(f + i * D + dim);
-            }
-#pragma unroll
-            for (int u = 0; u < AT; ++u) {
-                if (z + u >= it.pieces) continue;          // (uniform)
-                const float mn = fmaxf(M, mj[u]), c0 = __builtin_amdgcn_exp2f(M - mn), c1 = __builtin_amdgcn_exp2f(mj[u] - mn);
-                l = l * c0 + lj[u] * c1;
-                s = s * c0 + oj[u] * c1;
-                M = mn;
-            }
-        }
-        deliver(i, dim, s, l);
-    }
-    if (tid == 0) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (it.pieces > 1) ta_join<D>(P, L, plan, it, P.pg.heads, w.head, w.rows, &last_one);
 }
 
 template <int D>
 static hipError_t launch_of(const TreeAttention &P, const TreePlanLayout &L, char *plan, hipStream_t s)
 {
     const dim3 grid((unsigned)L.work * P.pg.heads), block(kTaThreads);
+    constexpr int lds = TwLds<D>::bytes;
+    const bool two = L.tile_rows > 64;
+    if (L.tile_rows > 32 && lds > 64 * 1024 - 8192) {      // (more than the default limit)
+        const hipError_t e = hipFuncSetAttribute(two ? (const void *)k_tree_attention_wide<D, 2> : (const void *)k_tree_attention_wide<D, 1>,
+                                                 hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+        if (e != hipSuccess) return e;
+    }
     switch (L.tile_rows) {
     case 16: hipLaunchKernelGGL((k_tree_attention<D, 1>), grid, block, 0, s, P, L, plan); break;
     case 32: hipLaunchKernelGGL((k_tree_attention<D, 2>), grid, block, 0, s, P, L, plan); break;
-    default: hipLaunchKernelGGL((k_tree_attention<D, 4>), grid, block, 0, s, P, L, plan); break;
+    case 64: hipLaunchKernelGGL((k_tree_attention_wide<D, 1>), grid, block, lds, s, P, L, plan); break;
+    default: hipLaunchKernelGGL((k_tree_attention_wide<D, 2>), grid, block, lds, s, P, L, plan); break;
     }
     return hipGetLastError();
 }

@@ -44,7 +44,7 @@ struct AcceptParams {
 hipError_t launch_tree_accept(const AcceptParams &P, int n_layers, hipStream_t s);
 
 // ---- the attention and its plan --------------------------------------------------------------
-// Query rows (a node's heads that share a key head, nodes one after the other) go to workgroups in tiles of 16, 32 or 64, positions in pieces.
+// Query rows (a node's heads that share a key head, nodes one after the other) go to workgroups in tiles of 16, 32, 64 or 128, positions in pieces.
 // A plan: the work list of a key head (TreeItem), an arrival counter for each tile and key head, and the sums of the pieces.
 struct TreeItem {
     int request, first, nodes, len;    // rows first .. first + nodes - 1 behind len cached positions
@@ -57,7 +57,7 @@ struct TreePlanLayout {
     int key;                           // of the sizes that a plan is made for
     size_t items, counters, sums, total;   // byte offsets
 };
-CFPP_HD int tree_tile_rows(int max_rows_of_request) { return max_rows_of_request <= 16 ? 16 : max_rows_of_request <= 32 ? 32 : 64; }
+CFPP_HD int tree_tile_rows(int max_rows_of_request) { return max_rows_of_request <= 16 ? 16 : max_rows_of_request <= 32 ? 32 : max_rows_of_request <= 64 ? 64 : 128; }
 TreePlanLayout tree_plan_layout(const PageDims &pg, int n_heads, int requests, int max_rows, int max_nodes, int stride);
 
 struct TreeAttention {
