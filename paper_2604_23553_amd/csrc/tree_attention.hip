@@ -467,25 +467,27 @@ struct TaStart {
 };
 
 // A query tile's 16 rows and 32 positions: scores (of this lane: row lane % 16, positions 4 (lane / 16) .. + 3 of both granules) to weights, and the
-// sums so far to the new maximum.  window: which positions the row sees, where `masked`.
+// sums so far to the new maximum.  window: which positions the row sees, where `masked`.  A weight's head is cut off, not rounded, and its
+// remainder, which is exact, is cut off in turn: together 2^-21 of it.
 template <int NT>
 __device__ __forceinline__ void ta_weights(f32x4 (&S)[2], float scale, bool masked, const bool (&good)[2], unsigned window, int kg, float &m_run, float &l_run,
                                            f32x4 (&O)[NT], ta_f16x8 &ph, ta_f16x8 &pl)
 {
+    if (masked) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float s = good[t] ? S[t][e] : NAN;
+                S[t][e] = (window >> (16 * t + 4 * kg + e)) & 1 ? s : -INFINITY;
+            }
+    }
     float most = -INFINITY;
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            float s = S[t][e] * scale;
-            if (masked) {
-                s = good[t] ? s : NAN;
-                s = (window >> (16 * t + 4 * kg + e)) & 1 ? s : -INFINITY;
-            }
-            S[t][e] = s;
-            most = fmaxf(most, s);
-        }
-    most = ta_max4(most);
+        for (int e = 0; e < 4; ++e) most = fmaxf(most, S[t][e]);
+    most = ta_max4(most) * scale;
     if (__any(most > m_run)) {
         const float mn = fmaxf(m_run, most), corr = __builtin_amdgcn_exp2f(m_run - mn);
         m_run = mn;
@@ -493,22 +495,25 @@ __device__ __forceinline__ void ta_weights(f32x4 (&S)[2], float scale, bool mask
 #pragma unroll
         for (int t = 0; t < NT; ++t) O[t] *= corr;
     }
-    const float base = m_run - kTaUp;
-    float sum = 0.f;
+    const float base = kTaUp - m_run;
+    u32x4 hi, lo;
+    float sum[2] = {0.f, 0.f};
 #pragma unroll
-    for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const float p = split_value(__builtin_amdgcn_exp2f(S[t][e] - base));
-            const _Float16 h = (_Float16)p;
-            sum += p;
-            ph[2 * e + t] = h;
-            pl[2 * e + t] = (_Float16)(p - (float)h);
-        }
-    l_run += sum;
+    for (int e = 0; e < 4; ++e) {
+        const float p0 = split_value(__builtin_amdgcn_exp2f(fmaf(S[0][e], scale, base))), p1 = split_value(__builtin_amdgcn_exp2f(fmaf(S[1][e], scale, base)));
+        const auto h = __builtin_amdgcn_cvt_pkrtz(p0, p1);
+        const auto l = __builtin_amdgcn_cvt_pkrtz(fmaf((float)h[0], -1.f, p0), fmaf((float)h[1], -1.f, p1));
+        sum[0] += p0;
+        sum[1] += p1;
+        hi[e] = __builtin_bit_cast(unsigned, h);
+        lo[e] = __builtin_bit_cast(unsigned, l);
+    }
+    l_run += sum[0] + sum[1];
+    ph = __builtin_bit_cast(ta_f16x8, hi);
+    pl = __builtin_bit_cast(ta_f16x8, lo);
 }
 
-// ---- up to 32 query rows: the wavefronts share the positions --------------------------------------------
+// ---- up to 32 query rows of a tile: the wavefronts share the positions --------------------------------------------
 template <int D, int QT>
 constexpr int ta_lds()                                     // V, or the wavefronts' sums
 {
@@ -516,18 +521,14 @@ constexpr int ta_lds()                                     // V, or the wavefron
     return v > w ? v : w;
 }
 
-template <int D, int QT>
-__global__ void __launch_bounds__(kTaThreads, 2) k_tree_attention(TreeAttention P, TreePlanLayout L, char *plan)
+template <int D, int TQ, int QT>
+__device__ __forceinline__ void ta_narrow(const TreeAttention &P, const TreePlanLayout &L, char *plan, const TaStart<D, TQ> &w, char *mem,
+                                          unsigned (*smask)[kTreeMaxNodes / 32], int *last_one)
 {
-    constexpr int KS = TaRow<D>::KS, NT = D / 16, TQ = 16 * QT, W = kTaWaves, D4 = D / 4;
-    __shared__ __align__(16) char mem[ta_lds<D, QT>()];
-    __shared__ unsigned smask[TQ][kTreeMaxNodes / 32];
-    __shared__ int last_one;
+    constexpr int KS = TaRow<D>::KS, NT = D / 16, TR = 16 * QT, W = kTaWaves, D4 = D / 4;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 15, kg = lane >> 4;
-    TaStart<D, TQ> w;
-    if (!w.of(P, L, plan)) return;
     const TreeItem &it = w.it;
-    const int n_tiles = (w.rows + 15) >> 4, words = tree_words(P.b.max_nodes);         // query tiles that have a row
+    const int words = tree_words(P.b.max_nodes);
     TaRow<D> r;
     const int row0 = it.t0 / kTaRow + wave;
     r.request(w.K, w.V, w.pages, w.slab, row0, lane);
@@ -563,8 +564,7 @@ __global__ void __launch_bounds__(kTaThreads, 2) k_tree_attention(TreeAttention 
                 u32x4 k = r.k[t][s];
                 if (D % 32 != 0 && s == KS - 1 && 32 * s + 8 * kg >= D) k = u32x4{0u, 0u, 0u, 0u};
 #pragma unroll
-                for (int j = 0; j < QT; ++j)
-                    if (j < n_tiles) S[j][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(ta_f16x8, k), __builtin_bit_cast(ta_f16x8, Q[j][s]), S[j][t], 0, 0, 0);
+                for (int j = 0; j < QT; ++j) S[j][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(ta_f16x8, k), __builtin_bit_cast(ta_f16x8, Q[j][s]), S[j][t], 0, 0, 0);
             }
         }
         const bool good[2] = {r.good[0], r.good[1]};
@@ -573,7 +573,6 @@ __global__ void __launch_bounds__(kTaThreads, 2) k_tree_attention(TreeAttention 
         ta_f16x8 ph[QT], pl[QT];                           // element 2 e + t: position 16 t + 4 kg + e
 #pragma unroll
         for (int j = 0; j < QT; ++j) {
-            if (j >= n_tiles) continue;
             unsigned window = ~0u;
             if (masked) window = ta_window(smask[16 * j + col], words, row * kTaRow, it.len, it.nodes);
             ta_weights(S[j], scale, masked, good, window, kg, m_run[j], l_run[j], O[j], ph[j], pl[j]);
@@ -582,21 +581,19 @@ __global__ void __launch_bounds__(kTaThreads, 2) k_tree_attention(TreeAttention 
         for (int t = 0; t < NT; ++t) {
             const ta_f16x8 v = __builtin_bit_cast(ta_f16x8, *reinterpret_cast<const u32x4 *>(vt + (16 * t + col) * kTaStride + 4 * kg));
 #pragma unroll
-            for (int j = 0; j < QT; ++j)
-                if (j < n_tiles) {
-                    O[j][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, ph[j], O[j][t], 0, 0, 0);
-                    O[j][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, pl[j], O[j][t], 0, 0, 0);
-                }
+            for (int j = 0; j < QT; ++j) {
+                O[j][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, ph[j], O[j][t], 0, 0, 0);
+                O[j][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, pl[j], O[j][t], 0, 0, 0);
+            }
         }
         asm volatile("" ::: "memory");
     }
     // The wavefronts' sums: [wave][row][D], maxima and weights [wave][row], in the place of V
-    float *wp = reinterpret_cast<float *>(mem), *wm = wp + W * TQ * D, *wl = wm + W * TQ;
+    float *wp = reinterpret_cast<float *>(mem), *wm = wp + W * TR * D, *wl = wm + W * TR;
     __syncthreads();                                       // V has been read
 #pragma unroll
     for (int j = 0; j < QT; ++j) {
-        const int at = wave * TQ + 16 * j;
-        if (j >= n_tiles) continue;
+        const int at = wave * TR + 16 * j;
         const float l = ta_sum4(l_run[j]);
         bool finite = fabsf(l) < INFINITY;
 #pragma unroll
@@ -621,12 +618,12 @@ __global__ void __launch_bounds__(kTaThreads, 2) k_tree_attention(TreeAttention 
         float M = wm[i], l = 0.f;
         f32x4 s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int v = 1; v < W; ++v) M = fmaxf(M, wm[v * TQ + i]);
+        for (int v = 1; v < W; ++v) M = fmaxf(M, wm[v * TR + i]);
 #pragma unroll
         for (int v = 0; v < W; ++v) {
-            const float ew = __builtin_amdgcn_exp2f(wm[v * TQ + i] - M);
-            l += wl[v * TQ + i] * ew;
-            s += *reinterpret_cast<const f32x4 *>(wp + (v * TQ + i) * D + dim) * ew;
+            const float ew = __builtin_amdgcn_exp2f(wm[v * TR + i] - M);
+            l += wl[v * TR + i] * ew;
+            s += *reinterpret_cast<const f32x4 *>(wp + (v * TR + i) * D + dim) * ew;
         }
         if (it.pieces == 1) {
             ta_deliver<D>(P, it, w.head, it.tile * TQ + i, dim, s, l);
@@ -635,7 +632,6 @@ __global__ void __launch_bounds__(kTaThreads, 2) k_tree_attention(TreeAttention 
             if (dim == 0) slot.put_ml(i, M, l);
         }
     }
-    if (it.pieces > 1) ta_join<D>(P, L, plan, it, P.pg.heads, w.head, w.rows, &last_one);
 }
 
 // ---- more query rows: the wavefronts share the rows -------------------------------------------------------
@@ -649,22 +645,17 @@ struct TwLds {
     static constexpr int k = kTwPos * ks, v = D * vs, bytes = 2 * (k + v);
 };
 
-template <int D, int QT>
-__global__ void __launch_bounds__(kTaThreads, 2) k_tree_attention_wide(TreeAttention P, TreePlanLayout L, char *plan)
+template <int D, int TQ, int QT>
+__device__ __forceinline__ void ta_wide(const TreeAttention &P, const TreePlanLayout &L, char *plan, const TaStart<D, TQ> &w, char *mem,
+                                        unsigned (*smask)[kTreeMaxNodes / 32], int *last_one)
 {
     using Lds = TwLds<D>;
-    constexpr int KS = TaRow<D>::KS, NT = D / 16, RW = 16 * QT, TQ = kTaWaves * RW;
+    constexpr int KS = TaRow<D>::KS, NT = D / 16, RW = 16 * QT;
     // pieces of 16 bytes a thread: K as (slab, position, half), V as (8 dimensions, position of 16 granules two by two)
     constexpr int KN = kTwPos * (D / 8), VN = (kTwPos / 2) * (D / 8), KU = (KN + kTaThreads - 1) / kTaThreads, VU = (VN + kTaThreads - 1) / kTaThreads;
-    extern __shared__ __align__(16) char tw_mem[];
-    __shared__ unsigned smask[TQ][kTreeMaxNodes / 32];
-    __shared__ int last_one;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 15, kg = lane >> 4;
-    TaStart<D, TQ> w;
-    if (!w.of(P, L, plan)) return;
     const TreeItem &it = w.it;
     const int words = tree_words(P.b.max_nodes);
-    const int n_tiles = min(QT, max(0, (w.rows - wave * RW + 15) >> 4));               // this wavefront's query tiles that have a row
     u32x4 rk[KU], rv[VU][2];
     unsigned good = 0;                                     // of the tile on its way: bit g: granule g lies in a page of the pool
     auto request = [&](int t) {
@@ -727,12 +718,12 @@ __global__ void __launch_bounds__(kTaThreads, 2) k_tree_attention_wide(TreeAtten
 #pragma unroll
         for (int t = 0; t < NT; ++t) O[j][t] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    store(tw_mem, it.t0);
+    store(mem, it.t0);
     unsigned now = good;
     __syncthreads();
     int side = 0;
     for (int t0 = it.t0; t0 < it.t1; t0 += kTwPos, side ^= 1) {
-        const char *kb = tw_mem + side * (Lds::k + Lds::v), *vb = kb + Lds::k;
+        const char *kb = mem + side * (Lds::k + Lds::v), *vb = kb + Lds::k;
         const bool more = t0 + kTwPos < it.t1;             // (uniform)
         if (more) request(t0 + kTwPos);
 #pragma unroll 1
@@ -752,14 +743,12 @@ __global__ void __launch_bounds__(kTaThreads, 2) k_tree_attention_wide(TreeAtten
                     u32x4 k = *reinterpret_cast<const u32x4 *>(kb + (32 * half + 16 * t + col) * Lds::ks + (real ? 64 * s + 16 * kg : 0));
                     if (!real) k = u32x4{0u, 0u, 0u, 0u};
 #pragma unroll
-                    for (int j = 0; j < QT; ++j)
-                        if (j < n_tiles) S[j][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(ta_f16x8, k), __builtin_bit_cast(ta_f16x8, Q[j][s]), S[j][t], 0, 0, 0);
+                    for (int j = 0; j < QT; ++j) S[j][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(ta_f16x8, k), __builtin_bit_cast(ta_f16x8, Q[j][s]), S[j][t], 0, 0, 0);
                 }
             }
             ta_f16x8 ph[QT], pl[QT];
 #pragma unroll
             for (int j = 0; j < QT; ++j) {
-                if (j >= n_tiles) continue;
                 unsigned window = ~0u;
                 if (masked) window = ta_window(smask[wave * RW + 16 * j + col], words, row, it.len, it.nodes);
                 ta_weights(S[j], scale, masked, two, window, kg, m_run[j], l_run[j], O[j], ph[j], pl[j]);
@@ -768,15 +757,14 @@ __global__ void __launch_bounds__(kTaThreads, 2) k_tree_attention_wide(TreeAtten
             for (int t = 0; t < NT; ++t) {
                 const ta_f16x8 v = __builtin_bit_cast(ta_f16x8, *reinterpret_cast<const u32x4 *>(vb + (16 * t + col) * Lds::vs + 64 * half + 16 * kg));
 #pragma unroll
-                for (int j = 0; j < QT; ++j)
-                    if (j < n_tiles) {
-                        O[j][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, ph[j], O[j][t], 0, 0, 0);
-                        O[j][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, pl[j], O[j][t], 0, 0, 0);
-                    }
+                for (int j = 0; j < QT; ++j) {
+                    O[j][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, ph[j], O[j][t], 0, 0, 0);
+                    O[j][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, pl[j], O[j][t], 0, 0, 0);
+                }
             }
         }
         if (more) {
-            store(tw_mem + (side ^ 1) * (Lds::k + Lds::v), t0 + kTwPos);   // (read last ahead of the barrier before this tile)
+            store(mem + (side ^ 1) * (Lds::k + Lds::v), t0 + kTwPos);      // (read last ahead of the barrier before this tile)
             now = good;
         }
         __syncthreads();
@@ -784,7 +772,6 @@ __global__ void __launch_bounds__(kTaThreads, 2) k_tree_attention_wide(TreeAtten
     const TaSlot<D> slot = ta_slot<D>(L, plan, it, P.pg.heads, w.head, it.piece);
 #pragma unroll
     for (int j = 0; j < QT; ++j) {
-        if (j >= n_tiles) continue;
         const int i = wave * RW + 16 * j + col;
         float l = ta_sum4(l_run[j]);
         bool finite = fabsf(l) < INFINITY;
@@ -794,7 +781,7 @@ __global__ void __launch_bounds__(kTaThreads, 2) k_tree_attention_wide(TreeAtten
             for (int e = 0; e < 4; ++e) finite = finite && fabsf(O[j][t][e]) < INFINITY;
         const unsigned long long again = __ballot(!finite);
         if (again) {                                       // (uniform) rows worked out once more, through LDS that no one needs now
-            float *o = reinterpret_cast<float *>(tw_mem) + wave * 16 * (D + 2);
+            float *o = reinterpret_cast<float *>(mem) + wave * 16 * (D + 2);
             for (int q = 0; q < 16; ++q)
                 if (again & (0x0001000100010001ull << q))
                     ta_alone<D, 1>(P, it, w.pages, w.K, w.V, smask[wave * RW + 16 * j + q], w.query(P, wave * RW + 16 * j + q), it.t0 / kTaRow, lane, o + q * (D + 2),
@@ -818,27 +805,54 @@ __global__ void __launch_bounds__(kTaThreads, 2) k_tree_attention_wide(TreeAtten
         }
         if (it.pieces > 1 && kg == 0) slot.put_ml(i, m_run[j], l);
     }
-    if (it.pieces > 1) ta_join<D>(P, L, plan, it, P.pg.heads, w.head, w.rows, &last_one);
 }
 
+// A tile runs by the query rows that it has: requests of one step may differ in size.
+template <int D, int TQ>
+constexpr int ta_lds_of()
+{
+    return TQ <= 32 ? ta_lds<D, TQ / 16>() : TwLds<D>::bytes > ta_lds<D, 2>() ? TwLds<D>::bytes : ta_lds<D, 2>();
+}
+template <int D, int TQ>
+__global__ void __launch_bounds__(kTaThreads, 2) k_tree_attention(TreeAttention P, TreePlanLayout L, char *plan)
+{
+    extern __shared__ __align__(16) char ta_mem[];
+    __shared__ unsigned smask[TQ][kTreeMaxNodes / 32];
+    __shared__ int last_one;
+    TaStart<D, TQ> w;
+    if (!w.of(P, L, plan)) return;
+    if (TQ == 16 || w.rows <= 16) {
+        ta_narrow<D, TQ, 1>(P, L, plan, w, ta_mem, smask, &last_one);
+    } else if (TQ == 32 || w.rows <= 32) {
+        if constexpr (TQ >= 32) ta_narrow<D, TQ, 2>(P, L, plan, w, ta_mem, smask, &last_one);
+    } else if (TQ == 64 || w.rows <= 64) {
+        if constexpr (TQ >= 64) ta_wide<D, TQ, 1>(P, L, plan, w, ta_mem, smask, &last_one);
+    } else {
+        if constexpr (TQ >= 128) ta_wide<D, TQ, 2>(P, L, plan, w, ta_mem, smask, &last_one);
+    }
+    if (w.it.pieces > 1) ta_join<D>(P, L, plan, w.it, P.pg.heads, w.head, w.rows, &last_one);
+}
+
+template <int D, int TQ>
+static hipError_t launch_tile(const TreeAttention &P, const TreePlanLayout &L, char *plan, hipStream_t s)
+{
+    constexpr int lds = ta_lds_of<D, TQ>();
+    if constexpr (lds > 64 * 1024 - 8192) {                // (more than the default limit, with the masks)
+        const hipError_t e = hipFuncSetAttribute((const void *)k_tree_attention<D, TQ>, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+        if (e != hipSuccess) return e;
+    }
+    hipLaunchKernelGGL((k_tree_attention<D, TQ>), dim3((unsigned)L.work * P.pg.heads), dim3(kTaThreads), lds, s, P, L, plan);
+    return hipGetLastError();
+}
 template <int D>
 static hipError_t launch_of(const TreeAttention &P, const TreePlanLayout &L, char *plan, hipStream_t s)
 {
-    const dim3 grid((unsigned)L.work * P.pg.heads), block(kTaThreads);
-    constexpr int lds = TwLds<D>::bytes;
-    const bool two = L.tile_rows > 64;
-    if (L.tile_rows > 32 && lds > 64 * 1024 - 8192) {      // (more than the default limit)
-        const hipError_t e = hipFuncSetAttribute(two ? (const void *)k_tree_attention_wide<D, 2> : (const void *)k_tree_attention_wide<D, 1>,
-                                                 hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-        if (e != hipSuccess) return e;
-    }
     switch (L.tile_rows) {
-    case 16: hipLaunchKernelGGL((k_tree_attention<D, 1>), grid, block, 0, s, P, L, plan); break;
-    case 32: hipLaunchKernelGGL((k_tree_attention<D, 2>), grid, block, 0, s, P, L, plan); break;
-    case 64: hipLaunchKernelGGL((k_tree_attention_wide<D, 1>), grid, block, lds, s, P, L, plan); break;
-    default: hipLaunchKernelGGL((k_tree_attention_wide<D, 2>), grid, block, lds, s, P, L, plan); break;
+    case 16: return launch_tile<D, 16>(P, L, plan, s);
+    case 32: return launch_tile<D, 32>(P, L, plan, s);
+    case 64: return launch_tile<D, 64>(P, L, plan, s);
+    default: return launch_tile<D, 128>(P, L, plan, s);
     }
-    return hipGetLastError();
 }
 
 hipError_t launch_tree_attention(const TreeAttention &A, char *plan, hipStream_t s)
