@@ -71,6 +71,8 @@ def _load(kind: str) -> C.CDLL:
         L.cfpp_page_pool_bytes.restype = L.cfpp_tree_plan_bytes.restype = C.c_size_t
         L.cfpp_prefill_scratch_bytes.restype = C.c_size_t
         L.cfpp_prefill_scratch_bytes.argtypes = [C.POINTER(Config), C.c_int32]
+        for n, types in _TREE_CALLS.items():
+            getattr(L, n).argtypes = types
         L.cfpp_destroy.restype = None
         L.cfpp_destroy.argtypes = [C.c_void_p]
         _loaded[kind] = L
@@ -103,6 +105,14 @@ def _ptr(t) -> C.c_void_p:
     if hasattr(t, "data_ptr"):
         t = t.data_ptr()
     return C.c_void_p(int(t))
+
+
+def _addr(t):
+    """An address for a parameter that is declared as a pointer: less than half of what _ptr takes."""
+    if t is None:
+        return None
+    of = getattr(t, "data_ptr", None)
+    return int(t) if of is None else of()
 
 
 def _check(st: int, where: str):
@@ -186,7 +196,7 @@ def cfpp_block_decode(ctx: int, packed_layer, kv_layer, x, pos_dev, batch: int, 
 
 
 def _ptr_array(items):
-    return (C.c_void_p * len(items))(*[_ptr(t).value or 0 for t in items])
+    return (C.c_void_p * len(items))(*[_addr(t) for t in items])
 
 
 def cfpp_stack_decode(ctx: int, packed_layers, kv_layers, x, pos_dev, batch: int, out, stream=None):
@@ -297,35 +307,53 @@ def cfpp_tree_plan_bytes(pages: Pages, n_heads: int, n_requests: int, max_rows: 
                                           C.c_int32(max_nodes)))
 
 
+# (calls of some microseconds: their parameters are declared, so that plain numbers go through)
+_PAGES, _BATCH, _P, _I, _L = C.POINTER(Pages), C.POINTER(TreeBatch), C.c_void_p, C.c_int32, C.c_int64
+_TREE_CALLS = {
+    "cfpp_page_tables": (_PAGES, _BATCH, _P, _P, _P, _P, _P, _P),
+    "cfpp_tree_plan": (_PAGES, _BATCH, _I, _P),
+    "cfpp_page_append": (_PAGES, _P, _P, _P, _L, _P, _I, _P),
+    "cfpp_tree_attention": (_PAGES, _P, _BATCH, _P, _L, _I, _P, _L, _P),
+    "cfpp_tree_accept": (_PAGES, C.POINTER(_P), _I, _BATCH, _P, _P, _P, _P, _P, _P, _P),
+}
+
+
 def cfpp_page_tables(pages: Pages, batch: TreeBatch, counts, held, free_pages, free_count, granted, stream=None):
-    _check(lib().cfpp_page_tables(C.byref(pages), C.byref(batch), _ptr(counts), _ptr(held), _ptr(free_pages), _ptr(free_count),
-                                  _ptr(granted), _ptr(stream)), "cfpp_page_tables")
+    st = lib().cfpp_page_tables(pages, batch, _addr(counts), _addr(held), _addr(free_pages), _addr(free_count), _addr(granted), _addr(stream))
+    if st:
+        _check(st, "cfpp_page_tables")
 
 
 def cfpp_tree_plan(pages: Pages, batch: TreeBatch, n_heads: int, stream=None):
-    _check(lib().cfpp_tree_plan(C.byref(pages), C.byref(batch), C.c_int32(n_heads), _ptr(stream)), "cfpp_tree_plan")
+    st = lib().cfpp_tree_plan(pages, batch, n_heads, _addr(stream))
+    if st:
+        _check(st, "cfpp_tree_plan")
 
 
 def cfpp_page_append(pages: Pages, kv_pool, k_rows, v_rows, slots, n_rows: int, row_stride: int | None = None, stream=None):
     """row_stride: elements between rows, n_kv_heads * head_dim by default."""
-    _check(lib().cfpp_page_append(C.byref(pages), _ptr(kv_pool), _ptr(k_rows), _ptr(v_rows),
-                                  C.c_int64(pages.n_kv_heads * pages.head_dim if row_stride is None else row_stride), _ptr(slots),
-                                  C.c_int32(n_rows), _ptr(stream)), "cfpp_page_append")
+    if row_stride is None:
+        row_stride = pages.n_kv_heads * pages.head_dim
+    st = lib().cfpp_page_append(pages, _addr(kv_pool), _addr(k_rows), _addr(v_rows), row_stride, _addr(slots), n_rows, _addr(stream))
+    if st:
+        _check(st, "cfpp_page_append")
 
 
 def cfpp_tree_attention(pages: Pages, kv_pool, batch: TreeBatch, q, n_heads: int, out, q_stride: int | None = None,
                         out_stride: int | None = None, stream=None):
     """q_stride, out_stride: elements between rows, n_heads * head_dim by default."""
     width = n_heads * pages.head_dim
-    _check(lib().cfpp_tree_attention(C.byref(pages), _ptr(kv_pool), C.byref(batch), _ptr(q),
-                                     C.c_int64(width if q_stride is None else q_stride), C.c_int32(n_heads), _ptr(out),
-                                     C.c_int64(width if out_stride is None else out_stride), _ptr(stream)), "cfpp_tree_attention")
+    st = lib().cfpp_tree_attention(pages, _addr(kv_pool), batch, _addr(q), width if q_stride is None else q_stride, n_heads, _addr(out),
+                                   width if out_stride is None else out_stride, _addr(stream))
+    if st:
+        _check(st, "cfpp_tree_attention")
 
 
 def cfpp_tree_accept(pages: Pages, kv_pools, batch: TreeBatch, tokens, picks, accepted, path, next_tokens, lens_out, stream=None):
-    _check(lib().cfpp_tree_accept(C.byref(pages), _ptr_array(kv_pools), C.c_int32(len(kv_pools)), C.byref(batch), _ptr(tokens),
-                                  _ptr(picks), _ptr(accepted), _ptr(path), _ptr(next_tokens), _ptr(lens_out), _ptr(stream)),
-           "cfpp_tree_accept")
+    st = lib().cfpp_tree_accept(pages, _ptr_array(kv_pools), len(kv_pools), batch, _addr(tokens), _addr(picks), _addr(accepted), _addr(path),
+                                _addr(next_tokens), _addr(lens_out), _addr(stream))
+    if st:
+        _check(st, "cfpp_tree_accept")
 
 
 # ---- profiling library only (inside `with profile_build():`) -------------------
