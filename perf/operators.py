@@ -256,6 +256,8 @@ def prepare(case, seed):
         s.plan = torch.empty(nbytes, dtype=torch.uint8, **dev)
         s.batch = cf.TreeBatch.of(max_nodes=case["nodes"], lens=s.lens, row_start=s.row_start, block_table=s.table, slots=s.slots,
                                   parents=s.parents, masks=s.masks, positions=s.positions, plan=s.plan)
+        if case["op"] == "accept":
+            s.pools = list(s.pool)                         # a program has its layers' pools at hand
         if case["op"] == "attention":                      # once a step; its layers then share it
             cf.cfpp_tree_plan(s.pages, s.batch, q, torch.cuda.current_stream().cuda_stream)
     return s
@@ -417,7 +419,7 @@ def run(s):
         elif op == "attention":
             cf.cfpp_tree_attention(s.pages, s.pool[0], s.batch, s.q, HEADS[s.case["heads"]][0], s.out, stream=stream)
         else:
-            cf.cfpp_tree_accept(s.pages, list(s.pool), s.batch, s.tokens, s.picks, s.accepted, s.path, s.next, s.lens_out, stream)
+            cf.cfpp_tree_accept(s.pages, s.pools, s.batch, s.tokens, s.picks, s.accepted, s.path, s.next, s.lens_out, stream)
     elif op == "tables":
         _plain_tables(s)
     elif op == "plan":
