@@ -496,6 +496,28 @@ cfpp_status cfpp_tree_accept(const cfpp_pages *pages, void *const *kv_pools, int
                              const int32_t *picks, int32_t *accepted, int32_t *path,
                              int32_t *next_tokens, int32_t *lens_out, cfpp_stream stream);
 
+/* One pass of a model's cfg.n_layers blocks for the rows of all requests' trees (a
+ * step's verification): the products of cfpp_stack_prefill_gemm, each layer's weights
+ * read once for all rows; every layer's new K and V rows go to their slots, rotated by
+ * their row's position, and every node attends to its request's cached positions and its
+ * ancestors.  A request of one row is a decode step, a chain a piece of a prompt.
+ *   kv_pools : HOST array of n_layers DEVICE pools; pages->n_kv_heads and head_dim are
+ *              the configuration's
+ *   batch    : after cfpp_page_tables and cfpp_tree_plan (n_heads: the
+ *              configuration's); at most 4096 max_rows, all of which the products run over
+ *   x, out   : DEVICE fp16 [max_rows][hidden]; rows without a slot are not
+ *              written; out must not overlap x
+ *   scratch  : DEVICE, 256-byte aligned, at least cfpp_tree_scratch_bytes(cfg, max_rows)
+ *              bytes; contents undefined afterwards
+ * A position outside [0, cfg.max_seq) raises the context's device error flag, and its row
+ * is of no use.  Any launch mode.  CFPP_EUNSUPPORTED for shapes that cfpp_stack_prefill_gemm refuses.
+ * Rows of cfpp_lm_next's logits and cfpp_tree_accept follow.  Asynchronous on `stream`;
+ * may be captured. */
+size_t cfpp_tree_scratch_bytes(const cfpp_config *cfg, int32_t max_rows);
+cfpp_status cfpp_stack_tree(cfpp_ctx *ctx, const void *const *packed_layers, void *const *kv_pools,
+                            const cfpp_pages *pages, const cfpp_tree_batch *batch, const void *x,
+                            void *out, void *scratch, size_t scratch_bytes, cfpp_stream stream);
+
 /* The whole-stack kernel marks the words its workgroups exchange with a 32-bit
  * epoch that every launch advances by n_layers + 1; the library counts the
  * epochs on the host and, before they could wrap (after about 2^32 / (n_layers + 1)

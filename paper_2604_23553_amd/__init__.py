@@ -12,7 +12,7 @@ from .binding import (  # noqa: F401
     cfpp_block_decode, cfpp_stack_decode, cfpp_stack_prefill, cfpp_prefill_scratch_bytes, cfpp_stack_prefill_gemm, cfpp_stack_capture, cfpp_stack_replay,
     cfpp_block_decode_static, cfpp_device_error, cfpp_debug_read, cfpp_debug_prefill_plan, cfpp_debug_prefill_narrow, cfpp_debug_prefill_beside, cfpp_debug_attention_plan, cfpp_debug_prefill_tiles, cfpp_debug_prefill_long, cfpp_debug_prefill_scratch, cfpp_debug_gelu, cfpp_stream_read, cfpp_stream_copy,
     Pages, TreeBatch, cfpp_validate_pages, cfpp_page_pool_bytes, cfpp_tree_plan_bytes, cfpp_page_tables, cfpp_tree_plan, cfpp_page_append,
-    cfpp_tree_attention, cfpp_tree_accept,
+    cfpp_tree_attention, cfpp_tree_accept, cfpp_tree_scratch_bytes, cfpp_stack_tree,
     Lm, cfpp_lm_embed, cfpp_lm_next, cfpp_generate_capture,
     OPT_MODE, OPT_GRID, OPT_THREADS, OPT_PROFILE_SKIP, OPT_EPOCH_LIMIT, MODE_AUTO,
 )

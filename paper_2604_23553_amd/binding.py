@@ -68,7 +68,7 @@ def _load(kind: str) -> C.CDLL:
         for n in ("cfpp_packed_layer_bytes", "cfpp_kv_layer_bytes", "cfpp_workspace_bytes"):
             getattr(L, n).restype = C.c_size_t
             getattr(L, n).argtypes = [C.POINTER(Config)]
-        L.cfpp_page_pool_bytes.restype = L.cfpp_tree_plan_bytes.restype = C.c_size_t
+        L.cfpp_page_pool_bytes.restype = L.cfpp_tree_plan_bytes.restype = L.cfpp_tree_scratch_bytes.restype = C.c_size_t
         L.cfpp_prefill_scratch_bytes.restype = C.c_size_t
         L.cfpp_prefill_scratch_bytes.argtypes = [C.POINTER(Config), C.c_int32]
         for n, types in _TREE_CALLS.items():
@@ -354,6 +354,15 @@ def cfpp_tree_accept(pages: Pages, kv_pools, batch: TreeBatch, tokens, picks, ac
                                 _addr(next_tokens), _addr(lens_out), _addr(stream))
     if st:
         _check(st, "cfpp_tree_accept")
+
+
+def cfpp_tree_scratch_bytes(cfg: Config, max_rows: int) -> int:
+    return int(lib().cfpp_tree_scratch_bytes(C.byref(cfg), C.c_int32(max_rows)))
+
+
+def cfpp_stack_tree(ctx: int, packed_layers, kv_pools, pages: Pages, batch: TreeBatch, x, out, scratch, scratch_bytes: int, stream=None):
+    _check(lib().cfpp_stack_tree(C.c_void_p(ctx), _ptr_array(packed_layers), _ptr_array(kv_pools), C.byref(pages), C.byref(batch),
+                                 _ptr(x), _ptr(out), _ptr(scratch), C.c_size_t(scratch_bytes), _ptr(stream)), "cfpp_stack_tree")
 
 
 # ---- profiling library only (inside `with profile_build():`) -------------------

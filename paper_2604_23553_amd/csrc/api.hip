@@ -1214,6 +1214,92 @@ extern "C" cfpp_status cfpp_tree_accept(const cfpp_pages *pages, void *const *kv
     return CFPP_OK;
 }
 
+// Scratch of a stack's step over the rows of trees, byte offsets: that of a prompt's pass, then the layer's new K and V rows in
+// slabs, a rotary line for each row, and the output of all rows.
+struct TreeScratch { size_t kv, rope, out, total; int rows; };
+static TreeScratch tree_scratch(const Dims &dm, int max_rows)
+{
+    TreeScratch S;
+    S.rows = (max_rows + kPfTile - 1) / kPfTile * kPfTile;
+    size_t o = align_up(pf_layout(dm, S.rows).total, 256);
+    auto take = [&](size_t bytes) { const size_t at = o; o = align_up(o + bytes, 256); return at; };
+    S.kv = take((size_t)2 * S.rows * dm.h * sizeof(__half));
+    S.rope = take((size_t)S.rows * (dm.r / 2) * sizeof(float2));
+    S.out = take((size_t)S.rows * dm.h * sizeof(__half));
+    S.total = o;
+    return S;
+}
+
+extern "C" size_t cfpp_tree_scratch_bytes(const cfpp_config *c, int32_t max_rows)
+{
+    if (cfpp_validate_config(c) != CFPP_OK || max_rows <= 0 || max_rows > kPfMaxRows) return 0;
+    return tree_scratch(dims_of(*c), max_rows).total;
+}
+
+extern "C" cfpp_status cfpp_stack_tree(cfpp_ctx *ctx, const void *const *packed_layers, void *const *kv_pools, const cfpp_pages *pages,
+                                       const cfpp_tree_batch *batch, const void *x, void *out, void *scratch, size_t scratch_bytes,
+                                       cfpp_stream stream)
+{
+    if (!ctx) return fail(CFPP_EINVAL, "ctx is NULL");
+    const Dims &dm = ctx->dm;
+    TreePass T;
+    cfpp_status st = tree_batch(pages, batch, &T.b);
+    if (st != CFPP_OK) return st;
+    if (pages->n_kv_heads != dm.H || pages->head_dim != dm.d)
+        return fail(CFPP_EINVAL, "pages of %d heads of %d, the configuration has %d of %d", pages->n_kv_heads, pages->head_dim, dm.H, dm.d);
+    if ((st = check_tree_plan(pages, batch, dm.H)) != CFPP_OK) return st;
+    if (!aligned4(batch->block_table) || !aligned4(batch->slots) || !aligned4(batch->positions))
+        return fail(CFPP_EINVAL, "block_table, slots or positions is NULL or misaligned");
+    if (!packed_layers || !kv_pools) return fail(CFPP_EINVAL, "layer pointer arrays are NULL");
+    const int L = ctx->cfg.n_layers, n = batch->max_rows;
+    if (n > kPfMaxRows) return fail(CFPP_EUNSUPPORTED, "max_rows %d: at most %d", n, kPfMaxRows);
+    for (int l = 0; l < L; ++l)
+        if (!aligned16(packed_layers[l]) || !aligned16(kv_pools[l])) return fail(CFPP_EINVAL, "layer %d: NULL or misaligned pointer", l);
+    if (!aligned16(x) || !aligned16(out)) return fail(CFPP_EINVAL, "x or out is NULL or not 16-byte aligned");
+    const size_t io = (size_t)n * dm.h * sizeof(__half);
+    if (overlap(x, io, out, io)) return fail(CFPP_EINVAL, "out overlaps x");
+    if (!pf_supported(dm))
+        return fail(CFPP_EUNSUPPORTED, "the prompt-sized kernels need hidden and ffn multiples of %d, hidden <= 4096 and "
+                    "the parallel residual form", kPfTile);
+    const TreeScratch S = tree_scratch(dm, n);
+    if (!scratch || (reinterpret_cast<uintptr_t>(scratch) & 255u)) return fail(CFPP_EINVAL, "scratch is NULL or not 256-byte aligned");
+    if (scratch_bytes < S.total) return fail(CFPP_ENOMEM, "scratch of %zu bytes, %zu needed for %d rows", scratch_bytes, S.total, n);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    char *sc = static_cast<char *>(scratch);
+    T.pg = page_dims(*pages);
+    T.plan = static_cast<char *>(batch->plan);
+    PfParams P;
+    std::memset(&P, 0, sizeof P);
+    P.dm = dm;
+    P.dm.max_seq = S.rows; P.dm.max_batch = 1;             // (of the scratch that takes K and V rows)
+    P.lay = ctx->lay;
+    P.n_rows = n; P.rows = S.rows; P.n_layers = L;
+    P.x_in = static_cast<const __half *>(x);
+    P.out = reinterpret_cast<__half *>(sc + S.out);
+    const PfLayout pl = pf_layout(P.dm, S.rows);
+    pf_place(P, pl, sc);
+    P.kv = reinterpret_cast<__half *>(sc + S.kv);
+    float2 *rope_rows = reinterpret_cast<float2 *>(sc + S.rope);
+    P.rope = rope_rows;
+    P.tree = &T;
+    HIP_OK(launch_tree_rope(T.b, reinterpret_cast<const float2 *>(ctx->ws + ctx->wl.rope), dm.r / 2, dm.max_seq, rope_rows,
+                            reinterpret_cast<unsigned *>(ctx->ws + ctx->wl.sync) + kSyncErr, s));
+    pf_plan_pass(P);
+    if (!pf_plan_narrow(P, ctx->n_cu)) { pf_plan_middle(P); pf_plan_long(P); }
+    float *xa = reinterpret_cast<float *>(sc + pl.xres), *xb = reinterpret_cast<float *>(sc + pl.xnext);
+    for (int l = 0; l < L; ++l) {
+        P.layer = l;
+        P.w = static_cast<const __half *>(packed_layers[l]);
+        P.w_next = static_cast<const __half *>(packed_layers[l + 1 < L ? l + 1 : l]);
+        T.pool = static_cast<__half *>(kv_pools[l]);
+        P.xres = (l & 1) ? xb : xa;                        // the block's output is the next block's input
+        P.xnext = (l & 1) ? xa : xb;
+        HIP_OK(launch_pf_layer(P, s));
+    }
+    HIP_OK(launch_tree_out(batch->slots, n, P.out, static_cast<__half *>(out), dm.h, s));
+    return CFPP_OK;
+}
+
 // ---- block decode for callers that cannot allocate --------------------------------------
 // The same step as cfpp_block_decode with the phase kernels, on a workspace that
 // is a fixed array in device memory instead of a caller's buffer: nothing is

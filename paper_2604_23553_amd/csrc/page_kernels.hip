@@ -171,11 +171,16 @@ hipError_t launch_page_tables(const TablesParams &P, hipStream_t s)
 }
 
 // ---- append ------------------------------------------------------------------------------------
-// 16 bytes a thread.  Neighbouring threads have neighbouring pieces of a row: whole lines are read, and records of 32 bytes written.
-__global__ void __launch_bounds__(256) k_page_append(PageDims pg, __half *pool, const __half *k, const __half *v, long long row_stride,
-                                                     const int *slots, int n_rows)
+// 16 bytes a thread.  Rows [row][head][d]: neighbouring threads have neighbouring pieces of a row, whole lines are read and records of 32 bytes
+// written.  `from`: where the pieces of K and V rows lie.
+struct AppendFrom {
+    const __half *k, *v;
+    long long row, head;       // halves from row to row, from head to head
+    int slab;                  // from 16 dimensions to the next
+};
+__global__ void __launch_bounds__(256) k_page_append(PageDims pg, __half *pool, AppendFrom from, const int *slots, int n_rows)
 {
-    const int per = pg.heads * pg.d / 8;
+    const int d8 = pg.d / 8, per = pg.heads * d8;
     const long long n = 2LL * n_rows * per;
     const size_t which = page_which_elems(pg);
     for (long long i = blockIdx.x * 256LL + threadIdx.x; i < n; i += gridDim.x * 256LL) {
@@ -183,18 +188,58 @@ __global__ void __launch_bounds__(256) k_page_append(PageDims pg, __half *pool, 
         const int piece = (int)(i - rw * per), row = (int)(rw >> 1), w = (int)(rw & 1);
         const int slot = slots[row];
         if (slot < 0 || slot >= pg.n_pages * pg.page) continue;
-        const int page = slot / pg.page, at = slot - page * pg.page, head = piece / (pg.d / 8), pc = piece - head * (pg.d / 8);
-        const u32x4 x = load16((w ? v : k) + (size_t)row * row_stride + piece * 8);
+        const int page = slot / pg.page, at = slot - page * pg.page, head = piece / d8, pc = piece - head * d8;
+        const u32x4 x = load16((w ? from.v : from.k) + row * from.row + head * from.head + (long long)(pc >> 1) * from.slab + (pc & 1) * 8);
         __half *to = pool + w * which + ((size_t)page * pg.heads + head) * page_head_elems(pg) + ((size_t)(pc >> 1) * pg.page + at) * 16 + (pc & 1) * 8;
         *as_global(reinterpret_cast<u32x4 *>(to)) = x;
     }
 }
 
+static hipError_t append(const PageDims &pg, __half *pool, const AppendFrom &from, const int *slots, int n_rows, hipStream_t s)
+{
+    const long long n = 2LL * n_rows * (pg.heads * pg.d / 8), wgs = (n + 255) / 256;
+    hipLaunchKernelGGL(k_page_append, dim3((unsigned)(wgs < 8192 ? wgs : 8192)), dim3(256), 0, s, pg, pool, from, slots, n_rows);
+    return hipGetLastError();
+}
 hipError_t launch_page_append(const PageDims &pg, __half *pool, const __half *k, const __half *v, long long row_stride, const int *slots,
                               int n_rows, hipStream_t s)
 {
-    const long long n = 2LL * n_rows * (pg.heads * pg.d / 8), wgs = (n + 255) / 256;
-    hipLaunchKernelGGL(k_page_append, dim3((unsigned)(wgs < 8192 ? wgs : 8192)), dim3(256), 0, s, pg, pool, k, v, row_stride, slots, n_rows);
+    return append(pg, pool, AppendFrom{k, v, row_stride, pg.d, 16}, slots, n_rows, s);
+}
+hipError_t launch_page_append_slabs(const PageDims &pg, __half *pool, const __half *kv, int rows, const int *slots, int n_rows, hipStream_t s)
+{
+    return append(pg, pool, AppendFrom{kv, kv + (size_t)pg.heads * pg.d * rows, 16, (long long)pg.d * rows, 16 * rows}, slots, n_rows, s);
+}
+
+// ---- either side of a stack's step ---------------------------------------------------------------
+__global__ void __launch_bounds__(256) k_tree_rope(TreeBatch b, const float2 *rope, int half, int max_seq, float2 *rope_rows, unsigned *err)
+{
+    const int i = blockIdx.x * 256 + threadIdx.x, row = i / half, j = i - row * half;
+    if (row >= b.max_rows) return;
+    int pos = b.slots[row] >= 0 ? b.positions[row] : 0;
+    if (pos < 0 || pos >= max_seq) {
+        *err = kErrBadPos;
+        pos = 0;
+    }
+    rope_rows[i] = rope[(size_t)pos * half + j];
+}
+hipError_t launch_tree_rope(const TreeBatch &b, const float2 *rope, int half, int max_seq, float2 *rope_rows, unsigned *err, hipStream_t s)
+{
+    if (half == 0) return hipSuccess;
+    hipLaunchKernelGGL(k_tree_rope, dim3((unsigned)(((long long)b.max_rows * half + 255) / 256)), dim3(256), 0, s, b, rope, half, max_seq, rope_rows, err);
+    return hipGetLastError();
+}
+
+__global__ void __launch_bounds__(256) k_tree_out(const int *slots, const __half *from, __half *to, int h)
+{
+    const int row = blockIdx.x;
+    if (slots[row] < 0) return;
+    for (int i = threadIdx.x * 8; i < h; i += 256 * 8)
+        *as_global(reinterpret_cast<u32x4 *>(to + (size_t)row * h + i)) = load16(from + (size_t)row * h + i);
+}
+hipError_t launch_tree_out(const int *slots, int n_rows, const __half *from, __half *to, int h, hipStream_t s)
+{
+    hipLaunchKernelGGL(k_tree_out, dim3(n_rows), dim3(256), 0, s, slots, from, to, h);
     return hipGetLastError();
 }
 

@@ -275,7 +275,8 @@ hipError_t launch_pf_layer(const PfParams &P, hipStream_t s)
     if (P.layer == 0 || !P.row_fused) pf_rows<false>(P, s);
     hipError_t e = P.nrw.on ? launch_pf_narrow_in(P, s) : launch_pf_gemm_in(P, s);
     if (e != hipSuccess) return e;
-    switch (dm.d) {
+    switch (P.tree ? 0 : dm.d) {
+    case 0: e = launch_tree_rows(P, s); break;
     case 64: e = pf_attention<64>(P, s); break;
     case 80: e = pf_attention<80>(P, s); break;
     case 128: e = pf_attention<128>(P, s); break;

@@ -3,6 +3,7 @@
 #include <hip/hip_runtime.h>
 #include <hip/hip_fp16.h>
 #include "layout.h"
+#include "tree_params.h"
 
 namespace cfpp {
 
@@ -100,6 +101,9 @@ struct PfParams {
     PfNarrow nrw;
     bool row_fused;         // the kernel that adds the second product's parts prepares the next layer's input too
     const float2 *rope;
+    // (host) not null: the rows are nodes of drafted trees; K and V rows of the first product go to their slots and every node attends over its
+    // request's pages (tree_params.h).  kv is then scratch of the pass's rows (dm.max_seq of them, dm.max_batch 1), rope has a line for each
+    const TreePass *tree;
 };
 
 // where a pass's buffers lie in the scratch at `sc`

@@ -17,6 +17,7 @@
 #include "tree_params.h"
 #include "device_utils.h"
 #include "half_split.h"
+#include "prefill_device.h"
 
 namespace cfpp {
 
@@ -294,9 +295,9 @@ __device__ __forceinline__ unsigned ta_window(const unsigned *words, int n_words
 }
 
 // One wavefront, one query row: its sums over rows row0, row0 + STEP .. of the piece in fp32, position by position, unseen ones left out
-template <int D, int STEP>
+template <int D, int STEP, class T>
 __device__ __forceinline__ void ta_alone(const TreeAttention &P, const TreeItem &it, const TaPages &pages, const __half *K, const __half *V, const unsigned *mask,
-                                         const __half *q, int row0, int lane, float *o_out, float *m_out, float *l_out)
+                                         const T *q, int row0, int lane, float *o_out, float *m_out, float *l_out)
 {
     constexpr int NE = (D + 63) / 64;
     const float scale = 1.44269504088896340736f / sqrtf((float)D);
@@ -307,7 +308,7 @@ __device__ __forceinline__ void ta_alone(const TreeAttention &P, const TreeItem 
     for (int e = 0; e < NE; ++e) {
         const int dim = min(lane + 64 * e, D - 1);
         at[e] = (unsigned)(dim >> 4) * slab + (dim & 15);
-        qs[e] = lane + 64 * e < D ? __half2float(q[dim]) : 0.f;
+        qs[e] = lane + 64 * e < D ? (float)q[dim] : 0.f;
         o[e] = 0.f;
     }
     for (int row = row0; row * kTaRow < it.t1; row += STEP) {
@@ -333,8 +334,8 @@ __device__ __forceinline__ void ta_alone(const TreeAttention &P, const TreeItem 
     if (lane == 0) { *m_out = m; *l_out = l; }
 }
 
-// four dimensions of a query row's output
-template <int D>
+// four dimensions of a query row's output; STACK: of a node among a stack's rows, as its output projection takes them, heads and remainders
+template <int D, bool STACK>
 __device__ __forceinline__ void ta_deliver(const TreeAttention &P, const TreeItem &it, int head, int qr, int dim, f32x4 s, float l)
 {
     const int G = P.group, node = qr / G, qh = head * G + (qr - node * G);
@@ -348,6 +349,16 @@ __device__ __forceinline__ void ta_deliver(const TreeAttention &P, const TreeIte
         }
         const float z = any ? NAN : 0.f;
         v = f32x4{z, z, z, z};
+    }
+    if constexpr (STACK) {
+        const int row = it.first + node, k = qh * D + dim, width = P.n_heads * D;
+        __half *to = P.planes + (P.narrow ? ng_at(row, k, width, kNgSet) : pf_at(row, k, width));
+        __align__(8) __half hi[4], lo[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) split_half(v[e], hi[e], lo[e]);
+        *as_global(reinterpret_cast<ta_u32x2 *>(to)) = *reinterpret_cast<const ta_u32x2 *>(hi);
+        *as_global(reinterpret_cast<ta_u32x2 *>(to + (P.narrow ? 8 * kNgSet : kPfLo))) = *reinterpret_cast<const ta_u32x2 *>(lo);
+        return;
     }
     ta_u32x2 o;
     o.x = (unsigned)__half_as_ushort(__float2half_rn(v[0])) | (unsigned)__half_as_ushort(__float2half_rn(v[1])) << 16;
@@ -374,7 +385,7 @@ __device__ __forceinline__ TaSlot<D> ta_slot(const TreePlanLayout &L, char *plan
 }
 
 // The tile's last workgroup adds the pieces in order.
-template <int D>
+template <int D, bool STACK>
 __device__ __forceinline__ void ta_join(const TreeAttention &P, const TreePlanLayout &L, char *plan, const TreeItem &it, int H, int head, int rows, int *last_one)
 {
     constexpr int D4 = D / 4;
@@ -411,14 +422,15 @@ __device__ __forceinline__ void ta_join(const TreeAttention &P, const TreePlanLa
                 M = mn;
             }
         }
-        ta_deliver<D>(P, it, head, it.tile * L.tile_rows + i, dim, s, l);
+        ta_deliver<D, STACK>(P, it, head, it.tile * L.tile_rows + i, dim, s, l);
     }
     if (tid == 0) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
 // What the workgroups of both kernels begin with
-template <int D, int TQ>
+template <int D, int TQ, bool STACK>
 struct TaStart {
+    using Query = std::conditional_t<STACK, float, __half>;
     TreeItem it;
     int head, rows, n_rows;            // key head; query rows of the tile, of the request
     const __half *K, *V;
@@ -451,18 +463,48 @@ struct TaStart {
         }
     }
     // query row i of the tile: node (tile TQ + i) / G, query head (head G + the rest)
-    __device__ __forceinline__ const __half *query(const TreeAttention &P, int i) const
+    __device__ __forceinline__ const Query *query(const TreeAttention &P, int i) const
     {
         const int G = P.group, qr = min(it.tile * TQ + i, n_rows - 1), node = qr / G;
-        return P.q + (size_t)(it.first + node) * P.q_stride + (size_t)(head * G + (qr - node * G)) * D;
+        const Query *q;
+        if constexpr (STACK) q = P.q32;
+        else q = P.q;
+        return q + (size_t)(it.first + node) * P.q_stride + (size_t)(head * G + (qr - node * G)) * D;
     }
-    // Q^T: dimensions 32 s + 8 kg .. + 7 of a query row
-    __device__ __forceinline__ u32x4 fragment(const TreeAttention &P, int i, int s, int kg) const
+};
+
+// Q^T of a query row: dimensions 32 s + 8 kg .. + 7; a stack's queries, in 32 bits, are head and remainder (half_split.h)
+template <int D, bool STACK>
+struct TaQuery {
+    static constexpr int KS = (D + 31) / 32;
+    ta_f16x8 hi[KS], lo[STACK ? KS : 1];
+    template <class T>
+    __device__ __forceinline__ void load(const T *q, int kg)
     {
-        const bool real = D % 32 == 0 || 32 * s + 8 * kg < D;
-        u32x4 x = load16(query(P, i) + (real ? 32 * s + 8 * kg : 0));
-        if (!real) x = u32x4{0u, 0u, 0u, 0u};
-        return x;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+            const bool real = D % 32 == 0 || 32 * s + 8 * kg < D;
+            const T *at = q + (real ? 32 * s + 8 * kg : 0);
+            if constexpr (STACK) {
+                const f32x4 a = *as_global(reinterpret_cast<const f32x4 *>(at)), b = *as_global(reinterpret_cast<const f32x4 *>(at + 4));
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float v = split_value(real ? (e < 4 ? a[e & 3] : b[e & 3]) : 0.f);
+                    hi[s][e] = (_Float16)v;
+                    lo[s][e] = (_Float16)(v - (float)hi[s][e]);
+                }
+            } else {
+                u32x4 x = load16(at);
+                if (!real) x = u32x4{0u, 0u, 0u, 0u};
+                hi[s] = __builtin_bit_cast(ta_f16x8, x);
+            }
+        }
+    }
+    __device__ __forceinline__ f32x4 score(u32x4 k, int s, f32x4 S) const
+    {
+        S = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(ta_f16x8, k), hi[s], S, 0, 0, 0);
+        if constexpr (STACK) S = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(ta_f16x8, k), lo[s], S, 0, 0, 0);
+        return S;
     }
 };
 
@@ -521,9 +563,9 @@ constexpr int ta_lds()                                     // V, or the wavefron
     return v > w ? v : w;
 }
 
-template <int D, int TQ, int QT>
-__device__ __forceinline__ void ta_narrow(const TreeAttention &P, const TreePlanLayout &L, char *plan, const TaStart<D, TQ> &w, char *mem,
-                                          unsigned (*smask)[kTreeMaxNodes / 32], int *last_one)
+template <int D, int TQ, int QT, bool STACK>
+__device__ __forceinline__ void ta_narrow(const TreeAttention &P, const TreePlanLayout &L, char *plan, const TaStart<D, TQ, STACK> &w, char *mem,
+                                          unsigned (*smask)[kTreeMaxNodes / 32])
 {
     constexpr int KS = TaRow<D>::KS, NT = D / 16, TR = 16 * QT, W = kTaWaves, D4 = D / 4;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 15, kg = lane >> 4;
@@ -534,11 +576,9 @@ __device__ __forceinline__ void ta_narrow(const TreeAttention &P, const TreePlan
     r.request(w.K, w.V, w.pages, w.slab, row0, lane);
     const bool tail = it.t1 > it.len;
     if (tail) w.masks(P, smask);
-    u32x4 Q[QT][KS];
+    TaQuery<D, STACK> Q[QT];
 #pragma unroll
-    for (int j = 0; j < QT; ++j)
-#pragma unroll
-        for (int s = 0; s < KS; ++s) Q[j][s] = w.fragment(P, 16 * j + col, s, kg);
+    for (int j = 0; j < QT; ++j) Q[j].load(w.query(P, 16 * j + col), kg);
     if (tail) __syncthreads();                             // (uniform)
     const float scale = 1.44269504088896340736f / sqrtf((float)D);
     f32x4 O[QT][NT];
@@ -564,7 +604,7 @@ __device__ __forceinline__ void ta_narrow(const TreeAttention &P, const TreePlan
                 u32x4 k = r.k[t][s];
                 if (D % 32 != 0 && s == KS - 1 && 32 * s + 8 * kg >= D) k = u32x4{0u, 0u, 0u, 0u};
 #pragma unroll
-                for (int j = 0; j < QT; ++j) S[j][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(ta_f16x8, k), __builtin_bit_cast(ta_f16x8, Q[j][s]), S[j][t], 0, 0, 0);
+                for (int j = 0; j < QT; ++j) S[j][t] = Q[j].score(k, s, S[j][t]);
             }
         }
         const bool good[2] = {r.good[0], r.good[1]};
@@ -626,7 +666,7 @@ __device__ __forceinline__ void ta_narrow(const TreeAttention &P, const TreePlan
             s += *reinterpret_cast<const f32x4 *>(wp + (v * TR + i) * D + dim) * ew;
         }
         if (it.pieces == 1) {
-            ta_deliver<D>(P, it, w.head, it.tile * TQ + i, dim, s, l);
+            ta_deliver<D, STACK>(P, it, w.head, it.tile * TQ + i, dim, s, l);
         } else {
             slot.put(i, dim, s);
             if (dim == 0) slot.put_ml(i, M, l);
@@ -645,9 +685,9 @@ struct TwLds {
     static constexpr int k = kTwPos * ks, v = D * vs, bytes = 2 * (k + v);
 };
 
-template <int D, int TQ, int QT>
-__device__ __forceinline__ void ta_wide(const TreeAttention &P, const TreePlanLayout &L, char *plan, const TaStart<D, TQ> &w, char *mem,
-                                        unsigned (*smask)[kTreeMaxNodes / 32], int *last_one)
+template <int D, int TQ, int QT, bool STACK>
+__device__ __forceinline__ void ta_wide(const TreeAttention &P, const TreePlanLayout &L, char *plan, const TaStart<D, TQ, STACK> &w, char *mem,
+                                        unsigned (*smask)[kTreeMaxNodes / 32])
 {
     using Lds = TwLds<D>;
     constexpr int KS = TaRow<D>::KS, NT = D / 16, RW = 16 * QT;
@@ -703,11 +743,9 @@ __device__ __forceinline__ void ta_wide(const TreeAttention &P, const TreePlanLa
     };
     request(it.t0);
     if (it.t1 > it.len) w.masks(P, smask);
-    u32x4 Q[QT][KS];
+    TaQuery<D, STACK> Q[QT];
 #pragma unroll
-    for (int j = 0; j < QT; ++j)
-#pragma unroll
-        for (int s = 0; s < KS; ++s) Q[j][s] = w.fragment(P, wave * RW + 16 * j + col, s, kg);
+    for (int j = 0; j < QT; ++j) Q[j].load(w.query(P, wave * RW + 16 * j + col), kg);
     const float scale = 1.44269504088896340736f / sqrtf((float)D);
     f32x4 O[QT][NT];
     float m_run[QT], l_run[QT];
@@ -743,7 +781,7 @@ __device__ __forceinline__ void ta_wide(const TreeAttention &P, const TreePlanLa
                     u32x4 k = *reinterpret_cast<const u32x4 *>(kb + (32 * half + 16 * t + col) * Lds::ks + (real ? 64 * s + 16 * kg : 0));
                     if (!real) k = u32x4{0u, 0u, 0u, 0u};
 #pragma unroll
-                    for (int j = 0; j < QT; ++j) S[j][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(ta_f16x8, k), __builtin_bit_cast(ta_f16x8, Q[j][s]), S[j][t], 0, 0, 0);
+                    for (int j = 0; j < QT; ++j) S[j][t] = Q[j].score(k, s, S[j][t]);
                 }
             }
             ta_f16x8 ph[QT], pl[QT];
@@ -800,7 +838,7 @@ __device__ __forceinline__ void ta_wide(const TreeAttention &P, const TreePlanLa
         if (i >= w.rows) continue;
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-            if (it.pieces == 1) ta_deliver<D>(P, it, w.head, it.tile * TQ + i, 16 * t + 4 * kg, O[j][t], l);
+            if (it.pieces == 1) ta_deliver<D, STACK>(P, it, w.head, it.tile * TQ + i, 16 * t + 4 * kg, O[j][t], l);
             else slot.put(i, 16 * t + 4 * kg, O[j][t]);
         }
         if (it.pieces > 1 && kg == 0) slot.put_ml(i, m_run[j], l);
@@ -813,59 +851,81 @@ constexpr int ta_lds_of()
 {
     return TQ <= 32 ? ta_lds<D, TQ / 16>() : TwLds<D>::bytes > ta_lds<D, 2>() ? TwLds<D>::bytes : ta_lds<D, 2>();
 }
-template <int D, int TQ>
+// STACK: the rows of a stack's step, queries in 32 bits and outputs as its products take them
+template <int D, int TQ, bool STACK>
 __global__ void __launch_bounds__(kTaThreads, 2) k_tree_attention(TreeAttention P, TreePlanLayout L, char *plan)
 {
     extern __shared__ __align__(16) char ta_mem[];
     __shared__ unsigned smask[TQ][kTreeMaxNodes / 32];
     __shared__ int last_one;
-    TaStart<D, TQ> w;
+    TaStart<D, TQ, STACK> w;
     if (!w.of(P, L, plan)) return;
     if (TQ == 16 || w.rows <= 16) {
-        ta_narrow<D, TQ, 1>(P, L, plan, w, ta_mem, smask, &last_one);
+        ta_narrow<D, TQ, 1, STACK>(P, L, plan, w, ta_mem, smask);
     } else if (TQ == 32 || w.rows <= 32) {
-        if constexpr (TQ >= 32) ta_narrow<D, TQ, 2>(P, L, plan, w, ta_mem, smask, &last_one);
+        if constexpr (TQ >= 32) ta_narrow<D, TQ, 2, STACK>(P, L, plan, w, ta_mem, smask);
     } else if (TQ == 64 || w.rows <= 64) {
-        if constexpr (TQ >= 64) ta_wide<D, TQ, 1>(P, L, plan, w, ta_mem, smask, &last_one);
+        if constexpr (TQ >= 64) ta_wide<D, TQ, 1, STACK>(P, L, plan, w, ta_mem, smask);
     } else {
-        if constexpr (TQ >= 128) ta_wide<D, TQ, 2>(P, L, plan, w, ta_mem, smask, &last_one);
+        if constexpr (TQ >= 128) ta_wide<D, TQ, 2, STACK>(P, L, plan, w, ta_mem, smask);
     }
-    if (w.it.pieces > 1) ta_join<D>(P, L, plan, w.it, P.pg.heads, w.head, w.rows, &last_one);
+    if (w.it.pieces > 1) ta_join<D, STACK>(P, L, plan, w.it, P.pg.heads, w.head, w.rows, &last_one);
 }
 
-template <int D, int TQ>
+template <int D, int TQ, bool STACK>
 static hipError_t launch_tile(const TreeAttention &P, const TreePlanLayout &L, char *plan, hipStream_t s)
 {
     constexpr int lds = ta_lds_of<D, TQ>();
     if constexpr (lds > 64 * 1024 - 8192) {                // (more than the default limit, with the masks)
-        const hipError_t e = hipFuncSetAttribute((const void *)k_tree_attention<D, TQ>, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+        const hipError_t e = hipFuncSetAttribute((const void *)k_tree_attention<D, TQ, STACK>, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
         if (e != hipSuccess) return e;
     }
-    hipLaunchKernelGGL((k_tree_attention<D, TQ>), dim3((unsigned)L.work * P.pg.heads), dim3(kTaThreads), lds, s, P, L, plan);
+    hipLaunchKernelGGL((k_tree_attention<D, TQ, STACK>), dim3((unsigned)L.work * P.pg.heads), dim3(kTaThreads), lds, s, P, L, plan);
     return hipGetLastError();
 }
-template <int D>
+template <int D, bool STACK>
 static hipError_t launch_of(const TreeAttention &P, const TreePlanLayout &L, char *plan, hipStream_t s)
 {
     switch (L.tile_rows) {
-    case 16: return launch_tile<D, 16>(P, L, plan, s);
-    case 32: return launch_tile<D, 32>(P, L, plan, s);
-    case 64: return launch_tile<D, 64>(P, L, plan, s);
-    default: return launch_tile<D, 128>(P, L, plan, s);
+    case 16: return launch_tile<D, 16, STACK>(P, L, plan, s);
+    case 32: return launch_tile<D, 32, STACK>(P, L, plan, s);
+    case 64: return launch_tile<D, 64, STACK>(P, L, plan, s);
+    default: return launch_tile<D, 128, STACK>(P, L, plan, s);
     }
 }
 
-hipError_t launch_tree_attention(const TreeAttention &A, char *plan, hipStream_t s)
+template <bool STACK>
+static hipError_t launch_attention(const TreeAttention &A, char *plan, hipStream_t s)
 {
     TreeAttention P = A;
     const TreePlanLayout L = tree_plan_layout(P.pg, P.n_heads, P.b.requests, P.b.max_rows, P.b.max_nodes, P.b.stride);
     const unsigned page16 = (unsigned)P.pg.page >> 4;
     P.page16_inv = (unsigned)(((1ull << 32) + page16 - 1) / page16);
     switch (P.pg.d) {
-    case 64: return launch_of<64>(P, L, plan, s);
-    case 80: return launch_of<80>(P, L, plan, s);
-    default: return launch_of<128>(P, L, plan, s);
+    case 64: return launch_of<64, STACK>(P, L, plan, s);
+    case 80: return launch_of<80, STACK>(P, L, plan, s);
+    default: return launch_of<128, STACK>(P, L, plan, s);
     }
+}
+
+hipError_t launch_tree_attention(const TreeAttention &P, char *plan, hipStream_t s) { return launch_attention<false>(P, plan, s); }
+
+// ---- a stack's rows ------------------------------------------------------------------------------------
+// Its first product leaves K and V rows in slabs of its own scratch, [2][head][d / 16][row][16], and queries in 32 bits; the K and V rows go
+// to their slots, then every node attends.
+hipError_t launch_tree_rows(const PfParams &F, hipStream_t s)
+{
+    const TreePass &T = *F.tree;
+    hipError_t e = launch_page_append_slabs(T.pg, T.pool, F.kv, F.dm.max_seq, T.b.slots, F.n_rows, s);
+    if (e != hipSuccess) return e;
+    TreeAttention P;
+    P.pg = T.pg; P.b = T.b;
+    P.n_heads = F.dm.H; P.group = 1;
+    P.pool = T.pool;
+    P.q = nullptr; P.out = nullptr;
+    P.q32 = F.q; P.planes = F.o; P.narrow = F.nrw.on;
+    P.q_stride = F.dm.h; P.out_stride = 0;
+    return launch_attention<true>(P, T.plan, s);
 }
 
 }  // namespace cfpp

@@ -68,9 +68,28 @@ struct TreeAttention {
     const __half *q;
     __half *out;
     long long q_stride, out_stride;
-    unsigned page16_inv;               // ceil(2^32 / (page / 16))
+    unsigned page16_inv;               // ceil(2^32 / (page / 16)), set by the launcher
+    // of a stack's rows instead of q and out: queries in 32 bits, outputs as heads and remainders in the order of its products
+    const float *q32;
+    __half *planes;
+    bool narrow;
 };
 hipError_t launch_tree_plan(const PageDims &pg, const TreeBatch &b, int n_heads, char *plan, hipStream_t s);
 hipError_t launch_tree_attention(const TreeAttention &P, char *plan, hipStream_t s);
+
+// ---- the rows of a stack's step (PfParams::tree) ---------------------------------------------
+struct TreePass {
+    PageDims pg;
+    TreeBatch b;
+    __half *pool;                      // the layer's
+    char *plan;
+};
+hipError_t launch_page_append_slabs(const PageDims &pg, __half *pool, const __half *kv, int rows, const int *slots, int n_rows, hipStream_t s);
+// rotary table by row: rope_rows[row] = rope[positions[row]]; rows without a slot take position 0, positions outside the table raise the error flag
+hipError_t launch_tree_rope(const TreeBatch &b, const float2 *rope, int half, int max_seq, float2 *rope_rows, unsigned *err, hipStream_t s);
+// rows that have a slot
+hipError_t launch_tree_out(const int *slots, int n_rows, const __half *from, __half *to, int h, hipStream_t s);
+struct PfParams;
+hipError_t launch_tree_rows(const PfParams &P, hipStream_t s);
 
 }  // namespace cfpp

@@ -103,6 +103,13 @@ def test_refusals_of_each_call():
     assert cf.lib().cfpp_tree_plan(C.byref(p), None, 8, None) == -1
 
 
+def test_the_stack_without_a_context():
+    cfg = cf.Config(512, 8, 64, 16, 2048, 1, 64, 1, 10000.0, 1e-5, 0)
+    assert refused(cf.cfpp_stack_tree, 0, [65536], [65536], cf.Pages(4, 16, 8, 64), a_batch(), 65536, 1 << 20, 1 << 21, 1 << 30) == -1
+    assert cf.cfpp_tree_scratch_bytes(cfg, 0) == 0 and cf.cfpp_tree_scratch_bytes(cfg, 4097) == 0
+    assert cf.cfpp_tree_scratch_bytes(cfg, 1) == cf.cfpp_tree_scratch_bytes(cfg, 128) > cf.cfpp_prefill_scratch_bytes(cfg, 128)
+
+
 def test_nothing_to_append_is_no_error():
     cf.cfpp_page_append(cf.Pages(*PAGES), 65536, 65536, 65536, 65536, 0)
 
