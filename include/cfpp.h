@@ -386,8 +386,8 @@ cfpp_status cfpp_generate_capture(cfpp_ctx *ctx, const void *const *packed_layer
  * position of the pool. */
 typedef struct cfpp_pages {
     int32_t n_pages;      /* pages of a layer's pool; n_pages * page_len < 2^31    */
-    int32_t page_len;     /* positions to a page, a multiple of 16                 */
-    int32_t n_kv_heads;   /* heads that have K and V                               */
+    int32_t page_len;     /* positions to a page, a multiple of 16 up to 2^20      */
+    int32_t n_kv_heads;   /* heads that have K and V, at most 1024                 */
     int32_t head_dim;     /* 64, 80 or 128                                         */
 } cfpp_pages;
 

@@ -1056,6 +1056,7 @@ extern "C" cfpp_status cfpp_validate_pages(const cfpp_pages *p)
     if (!p) return fail(CFPP_EINVAL, "pages is NULL");
     if (p->n_pages <= 0 || p->page_len <= 0 || p->n_kv_heads <= 0 || p->head_dim <= 0) return fail(CFPP_EINVAL, "pages has a non-positive dimension");
     if ((long long)p->n_pages * p->page_len > 0x7fffffffll) return fail(CFPP_EINVAL, "%d pages of %d positions: at most 2^31 - 1 in all", p->n_pages, p->page_len);
+    if (p->page_len > (1 << 20)) return fail(CFPP_EUNSUPPORTED, "page_len %d > 2^20", p->page_len);
     if (p->page_len % 16) return fail(CFPP_EUNSUPPORTED, "page_len %d: a multiple of 16 is needed", p->page_len);
     if (p->head_dim != 64 && p->head_dim != 80 && p->head_dim != 128)
         return fail(CFPP_EUNSUPPORTED, "head_dim %d: only 64, 80 and 128 have kernels", p->head_dim);

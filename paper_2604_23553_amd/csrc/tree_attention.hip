@@ -4,9 +4,9 @@
 // own mask.  The query rows of a request that share a key head - its nodes, times the query heads to a key head - are the columns of
 // both products (v_mfma_f32_16x16x32_f16), so a K and V row is read once for up to 128 of them:
 //   S = K Q^T      (16 positions x 16 query rows): a lane holds row lane % 16 and positions 4 (lane / 16) .. + 3
-//   O^T += V^T P^T (16 dimensions x 16 query rows): a lane's 8 K values are the positions of its own scores in two tiles of 16, so
-//                  that P needs no exchange.  V goes through LDS of the wavefront's own, transposed, positions t and t + 16 to a word: a
-//                  lane's 8 values are 16 bytes, and a load from memory covers whole lines.
+//   O^T += V^T P^T (16 dimensions x 16 query rows): a lane's 8 K values are the positions of its own scores in two granules of 16, so
+//                  that P needs no exchange.  V goes through LDS as it lies in the pool; ds_read_b64_tr_b16 gives a lane four positions of its
+//                  dimension, 512 contiguous bytes to a wavefront.
 // One pass over the positions with the running maximum and sum of the softmax; a workgroup has a piece of a request's positions for one
 // key head, its four wavefronts every fourth row of 32 of them, each with sums of its own that are joined in LDS in order.  Requests of
 // few rows are cut into pieces until the CUs are full (k_tree_plan); the last workgroup of a tile adds the pieces in order.
@@ -18,6 +18,7 @@
 #include "device_utils.h"
 #include "half_split.h"
 #include "prefill_device.h"
+#include "lds_dma.h"
 
 namespace cfpp {
 
@@ -25,7 +26,7 @@ typedef _Float16 ta_f16x8 __attribute__((ext_vector_type(8)));
 typedef unsigned ta_u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kTaThreads = 256, kTaWaves = kTaThreads / 64, kTaRow = 32, kTaStep = kTaRow * kTaWaves;
-constexpr int kTaStride = kTaRow / 2 + 4;                  // words between V's dimensions in LDS
+constexpr int kTaWhole = 256;                              // positions that are not cut
 constexpr int kTaWgs = 512;                                // workgroups that the pieces aim at
 constexpr float kTaLowest = -3.402823466e38f;
 
@@ -124,7 +125,7 @@ __device__ __forceinline__ void tree_work(const PageDims &pg, const TreeBatch &b
     // (C is at least kTaStep wherever there is a position)
     int sum[3] = {0, 0, 0};
     for (int r = lo; r < hi; ++r) {
-        const int t = tiles[r], pieces = t > 0 ? (int)((items[r] + C - 1) / C) : 0;
+        const int t = tiles[r], pieces = t <= 0 ? 0 : items[r] <= kTaWhole ? 1 : (int)((items[r] + C - 1) / C);
         sum[0] += t * pieces;
         sum[1] += pieces > 1 ? t * pieces : 0;
         sum[2] += t;
@@ -169,7 +170,7 @@ __device__ __forceinline__ void tree_work(const PageDims &pg, const TreeBatch &b
         it.tile = at - it.piece * n_tiles;
         it.slot = it.pieces > 1 ? (r > 0 ? multi[r - 1] : 0) + it.tile * it.pieces : -1;
         it.t0 = (int)(it.piece * C);
-        it.t1 = (int)min((long long)it.len + it.nodes, (it.piece + 1) * C);
+        it.t1 = it.piece == it.pieces - 1 ? it.len + it.nodes : (int)((it.piece + 1) * C);
         it.counter = t0 + it.tile;
         it.pad = 0;
         list[i] = it;
@@ -195,40 +196,65 @@ hipError_t launch_tree_plan(const PageDims &pg, const TreeBatch &b, int n_heads,
 // ---- the attention -----------------------------------------------------------------------------------
 // A granule of 16 positions lies in one page.
 struct TaPlace { size_t at; bool good; };                  // elements into the K or V half of the pool
+struct TaPick { int page[2], in[2]; };                     // of a row's granules: table entries, granules inside of their pages
 
 struct TaPages {
     const int *table;
     int page16, n_pages, last;                             // last: the piece's last granule
     unsigned inv;
     size_t per_page, head;
-    __device__ __forceinline__ TaPlace place(int granule) const
+    // Rows are looked up well ahead of their request, by scalar loads: a vector load's wait would wait for the rows that are on their way too.
+    __device__ __forceinline__ void look(int granule, int &page, int &in) const
     {
         const int g = min(granule, last);
         // g / page16: inv is ceil(2^32 / page16), so the product is at most one too large
         int p = (int)__umulhi((unsigned)g, inv);
         if (page16 == 1) p = g;
         else if (p * page16 > g) --p;
-        const int page = __builtin_amdgcn_readfirstlane(table[p]);
+        p = __builtin_amdgcn_readfirstlane(p);
+        page = reinterpret_cast<const __attribute__((address_space(4))) int *>(reinterpret_cast<uintptr_t>(table))[p];
+        in = g - p * page16;
+    }
+    __device__ __forceinline__ TaPick pick(int row) const
+    {
+        TaPick k;
+        look(2 * row, k.page[0], k.in[0]);
+        look(2 * row + 1, k.page[1], k.in[1]);
+        return k;
+    }
+    __device__ __forceinline__ TaPlace place(int page, int in) const
+    {
         TaPlace w;
         w.good = (unsigned)page < (unsigned)n_pages;
-        w.at = (size_t)(w.good ? page : 0) * per_page + head + (size_t)(g - p * page16) * 256;
+        w.at = (size_t)(w.good ? page : 0) * per_page + head + (size_t)in * 256;
         return w;
     }
+    __device__ __forceinline__ TaPlace place(const TaPick &k, int t) const { return place(k.page[t], k.in[t]); }
 };
+
+constexpr int ta_granule(int D) { return D * 32; }         // bytes of 16 positions of K or V: [d / 16][16][16] fp16
+
+// V of 16 dimensions and a granule, transposed: this lane's dimension lane % 16, positions 4 (lane / 16) .. + 3
+__device__ __forceinline__ ta_u32x2 ta_transposed(const char *at, int lane)
+{
+    typedef short s16x4 __attribute__((ext_vector_type(4)));
+    typedef __attribute__((address_space(3))) s16x4 *lds;
+    return __builtin_bit_cast(ta_u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds)(at + lane * 8)));
+}
 
 // what a wavefront holds of a row of 32 positions
 template <int D>
 struct TaRow {
-    static constexpr int KS = (D + 31) / 32, UN = (D / 8 * (kTaRow / 2) + 63) / 64;
-    u32x4 k[2][KS], v[UN][2];
+    static constexpr int KS = (D + 31) / 32, PG = 2 * D, UN = 2 * PG / 64;             // PG: pieces of 16 bytes to a granule
+    u32x4 k[2][KS], v[UN];
     bool good[2];
-    __device__ __forceinline__ void request(const __half *K, const __half *V, const TaPages &pages, unsigned slab, int row, int lane)
+    __device__ __forceinline__ void request(const __half *K, const __half *V, const TaPages &pages, unsigned slab, const TaPick &pick, int lane)
     {
         const int n = lane & 15, kg = lane >> 4;
         TaPlace w[2];
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-            w[t] = pages.place(2 * row + t);
+            w[t] = pages.place(pick, t);
             good[t] = w[t].good;
         }
 #pragma unroll
@@ -237,26 +263,19 @@ struct TaRow {
             for (int s = 0; s < KS; ++s) k[t][s] = load16_stream(K + w[t].at + (unsigned)min(2 * s + (kg >> 1), D / 16 - 1) * slab + n * 16u + (kg & 1) * 8u);
 #pragma unroll
         for (int u = 0; u < UN; ++u) {
-            const int e = min(lane + 64 * u, D / 8 * (kTaRow / 2) - 1), pc = e / (kTaRow / 2), n = e % (kTaRow / 2);
-#pragma unroll
-            for (int t = 0; t < 2; ++t) v[u][t] = load16_stream(V + w[t].at + (unsigned)(pc >> 1) * slab + (unsigned)n * 16u + (pc & 1) * 8u);
+            const int e = lane + 64 * u, t = PG % 64 == 0 ? (64 * u) / PG : e >= PG, i = e - t * PG;
+            v[u] = load16_stream(V + (t ? w[1].at : w[0].at) + (unsigned)(i >> 5) * slab + (i & 31) * 8u);
         }
         __builtin_amdgcn_sched_barrier(0);
     }
-    // V, transposed, to LDS: [dimension][kTaStride]; positions from `end` on as zeros
-    __device__ __forceinline__ void store(unsigned *vt, int row, int end, int lane) const
+    // V to LDS as it is: [granule][d / 16][16][16]; positions from `end` on as zeros
+    __device__ __forceinline__ void store(char *vt, int row, int end, int lane) const
     {
 #pragma unroll
         for (int u = 0; u < UN; ++u) {
-            const int e = lane + 64 * u, pc = e / (kTaRow / 2), n = e % (kTaRow / 2), t = row * kTaRow + n;
-            if (D / 8 * (kTaRow / 2) % 64 != 0 && e >= D / 8 * (kTaRow / 2)) break;
-            const u32x4 a = good[0] && t < end ? v[u][0] : u32x4{0u, 0u, 0u, 0u}, b = good[1] && t + 16 < end ? v[u][1] : u32x4{0u, 0u, 0u, 0u};
-            unsigned *to = vt + 8 * pc * kTaStride + n;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                to[2 * j * kTaStride] = __builtin_amdgcn_perm(b[j], a[j], 0x05040100u);
-                to[(2 * j + 1) * kTaStride] = __builtin_amdgcn_perm(b[j], a[j], 0x07060302u);
-            }
+            const int e = lane + 64 * u, t = PG % 64 == 0 ? (64 * u) / PG : e >= PG, i = e - t * PG;
+            const bool ok = (t ? good[1] : good[0]) && row * kTaRow + 16 * t + ((i >> 1) & 15) < end;
+            *reinterpret_cast<u32x4 *>(vt + e * 16) = ok ? v[u] : u32x4{0u, 0u, 0u, 0u};
         }
     }
 };
@@ -315,7 +334,9 @@ __device__ __forceinline__ void ta_alone(const TreeAttention &P, const TreeItem 
         for (int t = row * kTaRow; t < min(row * kTaRow + kTaRow, it.t1); ++t) {
             const int node = t - it.len;
             if (node >= 0 && !((mask[node >> 5] >> (node & 31)) & 1)) continue;        // (uniform)
-            const TaPlace w = pages.place(t >> 4);
+            int page, in16;
+            pages.look(t >> 4, page, in16);
+            const TaPlace w = pages.place(page, in16);
             const unsigned in = (unsigned)(t & 15) * 16u;
             float s = 0.f;
 #pragma unroll
@@ -541,8 +562,9 @@ __device__ __forceinline__ void ta_weights(f32x4 (&S)[2], float scale, bool mask
     u32x4 hi, lo;
     float sum[2] = {0.f, 0.f};
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        const float p0 = split_value(__builtin_amdgcn_exp2f(fmaf(S[0][e], scale, base))), p1 = split_value(__builtin_amdgcn_exp2f(fmaf(S[1][e], scale, base)));
+    for (int e = 0; e < 4; ++e) {                          // words: positions 4 kg + 0, 1; + 2, 3; the same of the second granule
+        const int t = e >> 1, i = 2 * (e & 1);
+        const float p0 = split_value(__builtin_amdgcn_exp2f(fmaf(S[t][i], scale, base))), p1 = split_value(__builtin_amdgcn_exp2f(fmaf(S[t][i + 1], scale, base)));
         const auto h = __builtin_amdgcn_cvt_pkrtz(p0, p1);
         const auto l = __builtin_amdgcn_cvt_pkrtz(fmaf((float)h[0], -1.f, p0), fmaf((float)h[1], -1.f, p1));
         sum[0] += p0;
@@ -559,7 +581,7 @@ __device__ __forceinline__ void ta_weights(f32x4 (&S)[2], float scale, bool mask
 template <int D, int QT>
 constexpr int ta_lds()                                     // V, or the wavefronts' sums
 {
-    const int v = kTaWaves * D * kTaStride * 4, w = kTaWaves * 16 * QT * (D + 2) * 4;
+    const int v = kTaWaves * 2 * ta_granule(D), w = kTaWaves * 16 * QT * (D + 2) * 4;
     return v > w ? v : w;
 }
 
@@ -571,9 +593,13 @@ __device__ __forceinline__ void ta_narrow(const TreeAttention &P, const TreePlan
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 15, kg = lane >> 4;
     const TreeItem &it = w.it;
     const int words = tree_words(P.b.max_nodes);
-    TaRow<D> r;
+    // rows on their way: as many as registers hold beside the sums
+    constexpr int AHEAD = QT == 1 || D <= 80 ? 2 : 1;
+    TaRow<D> r[AHEAD];
     const int row0 = it.t0 / kTaRow + wave;
-    r.request(w.K, w.V, w.pages, w.slab, row0, lane);
+#pragma unroll
+    for (int a = 0; a < AHEAD; ++a) r[a].request(w.K, w.V, w.pages, w.slab, w.pages.pick(row0 + a * W), lane);
+    TaPick next = w.pages.pick(row0 + AHEAD * W);
     const bool tail = it.t1 > it.len;
     if (tail) w.masks(P, smask);
     TaQuery<D, STACK> Q[QT];
@@ -590,8 +616,8 @@ __device__ __forceinline__ void ta_narrow(const TreeAttention &P, const TreePlan
 #pragma unroll
         for (int t = 0; t < NT; ++t) O[j][t] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    unsigned *vt = reinterpret_cast<unsigned *>(mem) + wave * D * kTaStride;
-    for (int row = row0; row * kTaRow < it.t1; row += W) {
+    char *vt = mem + wave * 2 * ta_granule(D);
+    auto step = [&](TaRow<D> &r, int row) {
         r.store(vt, row, it.t1, lane);
         asm volatile("" ::: "memory");                     // (LDS takes a wavefront's accesses in order)
         f32x4 S[QT][2];
@@ -608,9 +634,10 @@ __device__ __forceinline__ void ta_narrow(const TreeAttention &P, const TreePlan
             }
         }
         const bool good[2] = {r.good[0], r.good[1]};
-        r.request(w.K, w.V, w.pages, w.slab, row + W, lane);
+        r.request(w.K, w.V, w.pages, w.slab, next, lane);
+        next = w.pages.pick(row + (AHEAD + 1) * W);
         const bool masked = row * kTaRow + kTaRow > it.len || !good[0] || !good[1];    // (uniform)
-        ta_f16x8 ph[QT], pl[QT];                           // element 2 e + t: position 16 t + 4 kg + e
+        ta_f16x8 ph[QT], pl[QT];                           // element 4 t + e: position 16 t + 4 kg + e
 #pragma unroll
         for (int j = 0; j < QT; ++j) {
             unsigned window = ~0u;
@@ -619,7 +646,8 @@ __device__ __forceinline__ void ta_narrow(const TreeAttention &P, const TreePlan
         }
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-            const ta_f16x8 v = __builtin_bit_cast(ta_f16x8, *reinterpret_cast<const u32x4 *>(vt + (16 * t + col) * kTaStride + 4 * kg));
+            const ta_u32x2 v0 = ta_transposed(vt + t * 512, lane), v1 = ta_transposed(vt + ta_granule(D) + t * 512, lane);
+            const ta_f16x8 v = __builtin_bit_cast(ta_f16x8, u32x4{v0[0], v0[1], v1[0], v1[1]});
 #pragma unroll
             for (int j = 0; j < QT; ++j) {
                 O[j][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, ph[j], O[j][t], 0, 0, 0);
@@ -627,7 +655,11 @@ __device__ __forceinline__ void ta_narrow(const TreeAttention &P, const TreePlan
             }
         }
         asm volatile("" ::: "memory");
-    }
+    };
+    for (int row = row0; row * kTaRow < it.t1; row += AHEAD * W)
+#pragma unroll
+        for (int a = 0; a < AHEAD; ++a)
+            if ((row + a * W) * kTaRow < it.t1) step(r[a], row + a * W);               // (uniform)
     // The wavefronts' sums: [wave][row][D], maxima and weights [wave][row], in the place of V
     float *wp = reinterpret_cast<float *>(mem), *wm = wp + W * TR * D, *wl = wm + W * TR;
     __syncthreads();                                       // V has been read
@@ -675,15 +707,20 @@ __device__ __forceinline__ void ta_narrow(const TreeAttention &P, const TreePlan
 }
 
 // ---- more query rows: the wavefronts share the rows -------------------------------------------------------
-// A tile of 64 positions goes through LDS for all four wavefronts, K as it is and V transposed as above, in two buffers: while one is
-// multiplied the next tile is on its way in registers.  A wavefront has 16 QT query rows and all positions of the piece, so
-// nothing is joined but the pieces.
-constexpr int kTwPos = 64;
+// A row of 32 positions goes through LDS for all four wavefronts, K and V as they lie in the pool, straight from memory: a ring of kTwRing
+// rows, one granule of K or V of each to a wavefront, waited for by count, and one barrier a row.  A wavefront has 16 QT query rows and all positions
+// of the piece, so nothing is joined but the pieces.  Positions past the piece's end read its last one again: their weights are zero.
+constexpr int kTwRing = 4;
 template <int D>
 struct TwLds {
-    static constexpr int ks = D * 2 + 16, vs = (kTwPos / 2 + 4) * 4;       // bytes from position to position of K, from dimension to dimension of V
-    static constexpr int k = kTwPos * ks, v = D * vs, bytes = 2 * (k + v);
+    // (an odd slab's second half is left free, so that a load's 64 lanes always fill two)
+    static constexpr int slabs = D / 16, loads = (slabs + 1) / 2, granule = loads * 1024, row = 4 * granule, bytes = kTwRing * row;
 };
+template <int N>
+__device__ __forceinline__ void tw_arrive()                // all but the N newest loads of this wavefront have landed, and every wavefront is here
+{
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" :: "n"(N) : "memory");
+}
 
 template <int D, int TQ, int QT, bool STACK>
 __device__ __forceinline__ void ta_wide(const TreeAttention &P, const TreePlanLayout &L, char *plan, const TaStart<D, TQ, STACK> &w, char *mem,
@@ -691,57 +728,30 @@ __device__ __forceinline__ void ta_wide(const TreeAttention &P, const TreePlanLa
 {
     using Lds = TwLds<D>;
     constexpr int KS = TaRow<D>::KS, NT = D / 16, RW = 16 * QT;
-    // pieces of 16 bytes a thread: K as (slab, position, half), V as (8 dimensions, position of 16 granules two by two)
-    constexpr int KN = kTwPos * (D / 8), VN = (kTwPos / 2) * (D / 8), KU = (KN + kTaThreads - 1) / kTaThreads, VU = (VN + kTaThreads - 1) / kTaThreads;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 15, kg = lane >> 4;
     const TreeItem &it = w.it;
     const int words = tree_words(P.b.max_nodes);
-    u32x4 rk[KU], rv[VU][2];
-    unsigned good = 0;                                     // of the tile on its way: bit g: granule g lies in a page of the pool
-    auto request = [&](int t) {
-        TaPlace pl[4];
-        good = 0;
+    // this wavefront's granule of a row: K (0, 1) or V (2, 3)
+    const __half *half = wave < 2 ? w.K : w.V;
+    const int mine = wave & 1, last_n = (it.t1 - 1) & 15;
+    const unsigned base = lds_address(mem);
+    unsigned goods = 0;                                    // bits 2 i, 2 i + 1: the granules of the ring's row i lie in pages of the pool
+    auto request = [&](int row, int at, const TaPick &pick) {
+        const TaPlace p0 = w.pages.place(pick, 0), p1 = w.pages.place(pick, 1), p = mine ? p1 : p0;
+        goods = (goods & ~(3u << (2 * at))) | ((unsigned)p0.good | (unsigned)p1.good << 1) << (2 * at);
+        const int n = min((lane & 31) >> 1, 2 * row + mine < w.pages.last ? 15 : last_n);
+        const i32x4 rsrc = dma_rsrc(half + p.at, 0x7fffffffu);
+        const unsigned to = base + at * Lds::row + wave * Lds::granule;
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            pl[g] = w.pages.place((t >> 4) + g);
-            good |= (unsigned)pl[g].good << g;
-        }
-        auto at = [&](int g) { return g == 0 ? pl[0].at : g == 1 ? pl[1].at : g == 2 ? pl[2].at : pl[3].at; };
-#pragma unroll
-        for (int u = 0; u < KU; ++u) {
-            const int e = min(tid + kTaThreads * u, KN - 1), half = e & 1, n = (e >> 1) & 15, g = (e >> 5) & 3, s = e >> 7;
-            rk[u] = load16(w.K + at(g) + (unsigned)s * w.slab + (unsigned)n * 16u + half * 8u);
-        }
-#pragma unroll
-        for (int u = 0; u < VU; ++u) {
-            const int e = min(tid + kTaThreads * u, VN - 1), n = e & 15, half = (e >> 4) & 1, g2 = (e >> 5) & 1, s = e >> 6;
-#pragma unroll
-            for (int i = 0; i < 2; ++i) rv[u][i] = load16(w.V + at(2 * g2 + i) + (unsigned)s * w.slab + (unsigned)n * 16u + half * 8u);
-        }
-        __builtin_amdgcn_sched_barrier(0);
-    };
-    auto store = [&](char *buf, int t) {
-#pragma unroll
-        for (int u = 0; u < KU; ++u) {
-            const int e = tid + kTaThreads * u, half = e & 1, n = (e >> 1) & 15, g = (e >> 5) & 3, s = e >> 7;
-            if (KN % kTaThreads != 0 && e >= KN) break;
-            *reinterpret_cast<u32x4 *>(buf + (16 * g + n) * Lds::ks + s * 32 + half * 16) = rk[u];
-        }
-#pragma unroll
-        for (int u = 0; u < VU; ++u) {
-            const int e = tid + kTaThreads * u, n = e & 15, half = (e >> 4) & 1, g2 = (e >> 5) & 1, s = e >> 6, p = t + 32 * g2 + n;
-            if (VN % kTaThreads != 0 && e >= VN) break;
-            const u32x4 zero = {0u, 0u, 0u, 0u};           // positions from the piece's end on
-            const u32x4 a = (good >> (2 * g2)) & 1 && p < it.t1 ? rv[u][0] : zero, b = (good >> (2 * g2 + 1)) & 1 && p + 16 < it.t1 ? rv[u][1] : zero;
-            char *to = buf + Lds::k + (16 * s + 8 * half) * Lds::vs + (16 * g2 + n) * 4;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                *reinterpret_cast<unsigned *>(to + 2 * j * Lds::vs) = __builtin_amdgcn_perm(b[j], a[j], 0x05040100u);
-                *reinterpret_cast<unsigned *>(to + (2 * j + 1) * Lds::vs) = __builtin_amdgcn_perm(b[j], a[j], 0x07060302u);
-            }
+        for (int u = 0; u < Lds::loads; ++u) {
+            const unsigned off = ((lane >> 5) * w.slab + n * 16u + (lane & 1) * 8u) * 2u;
+            if (Lds::slabs % 2 == 0 || u < Lds::loads - 1 || lane < 32) lds_dma16(rsrc, to + u * 1024, off, 2 * u * w.slab * 2u);
         }
     };
-    request(it.t0);
+    const int first = it.t0 / kTaRow;
+#pragma unroll
+    for (int a = 0; a < kTwRing - 1; ++a) request(first + a, a, w.pages.pick(first + a));
+    TaPick next = w.pages.pick(first + kTwRing - 1);
     if (it.t1 > it.len) w.masks(P, smask);
     TaQuery<D, STACK> Q[QT];
 #pragma unroll
@@ -756,57 +766,48 @@ __device__ __forceinline__ void ta_wide(const TreeAttention &P, const TreePlanLa
 #pragma unroll
         for (int t = 0; t < NT; ++t) O[j][t] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    store(mem, it.t0);
-    unsigned now = good;
-    __syncthreads();
-    int side = 0;
-    for (int t0 = it.t0; t0 < it.t1; t0 += kTwPos, side ^= 1) {
-        const char *kb = mem + side * (Lds::k + Lds::v), *vb = kb + Lds::k;
-        const bool more = t0 + kTwPos < it.t1;             // (uniform)
-        if (more) request(t0 + kTwPos);
-#pragma unroll 1
-        for (int half = 0; half < 2; ++half) {             // (one at a time: registers)
-            const int row = t0 + 32 * half;
-            if (row >= it.t1) break;                       // (uniform)
-            const bool two[2] = {((now >> (2 * half)) & 1) != 0, ((now >> (2 * half + 1)) & 1) != 0};
-            const bool masked = row + 32 > it.len || !two[0] || !two[1];
-            f32x4 S[QT][2];
+    int at = 0;
+    for (int row = first; row * kTaRow < it.t1; ++row, at = (at + 1) % kTwRing) {
+        tw_arrive<(kTwRing - 2) * Lds::loads>();
+        const unsigned good = (goods >> (2 * at)) & 3;
+        request(row + kTwRing - 1, (at + kTwRing - 1) % kTwRing, next);    // (the place of the row before this one, which everyone has read)
+        next = w.pages.pick(row + kTwRing);
+        const char *kb = mem + at * Lds::row, *vb = kb + 2 * Lds::granule;
+        const bool two[2] = {(good & 1) != 0, (good & 2) != 0};
+        const bool masked = row * kTaRow + kTaRow > it.len || good != 3;
+        f32x4 S[QT][2];
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
+        for (int t = 0; t < 2; ++t) {
 #pragma unroll
-                for (int j = 0; j < QT; ++j) S[j][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+            for (int j = 0; j < QT; ++j) S[j][t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int s = 0; s < KS; ++s) {
-                    const bool real = D % 32 == 0 || 32 * s + 8 * kg < D;
-                    u32x4 k = *reinterpret_cast<const u32x4 *>(kb + (32 * half + 16 * t + col) * Lds::ks + (real ? 64 * s + 16 * kg : 0));
-                    if (!real) k = u32x4{0u, 0u, 0u, 0u};
+            for (int s = 0; s < KS; ++s) {
+                const bool real = D % 32 == 0 || 32 * s + 8 * kg < D;
+                u32x4 k = *reinterpret_cast<const u32x4 *>(kb + t * Lds::granule + (real ? 2 * s + (kg >> 1) : 0) * 512 + col * 32 + (kg & 1) * 16);
+                if (!real) k = u32x4{0u, 0u, 0u, 0u};
 #pragma unroll
-                    for (int j = 0; j < QT; ++j) S[j][t] = Q[j].score(k, s, S[j][t]);
-                }
+                for (int j = 0; j < QT; ++j) S[j][t] = Q[j].score(k, s, S[j][t]);
             }
-            ta_f16x8 ph[QT], pl[QT];
+        }
+        ta_f16x8 ph[QT], pl[QT];
+#pragma unroll
+        for (int j = 0; j < QT; ++j) {
+            unsigned window = ~0u;
+            if (masked) window = ta_window(smask[wave * RW + 16 * j + col], words, row * kTaRow, it.len, it.nodes);
+            ta_weights(S[j], scale, masked, two, window, kg, m_run[j], l_run[j], O[j], ph[j], pl[j]);
+        }
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            const ta_u32x2 v0 = ta_transposed(vb + t * 512, lane), v1 = ta_transposed(vb + Lds::granule + t * 512, lane);
+            const ta_f16x8 v = __builtin_bit_cast(ta_f16x8, u32x4{v0[0], v0[1], v1[0], v1[1]});
 #pragma unroll
             for (int j = 0; j < QT; ++j) {
-                unsigned window = ~0u;
-                if (masked) window = ta_window(smask[wave * RW + 16 * j + col], words, row, it.len, it.nodes);
-                ta_weights(S[j], scale, masked, two, window, kg, m_run[j], l_run[j], O[j], ph[j], pl[j]);
-            }
-#pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                const ta_f16x8 v = __builtin_bit_cast(ta_f16x8, *reinterpret_cast<const u32x4 *>(vb + (16 * t + col) * Lds::vs + 64 * half + 16 * kg));
-#pragma unroll
-                for (int j = 0; j < QT; ++j) {
-                    O[j][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, ph[j], O[j][t], 0, 0, 0);
-                    O[j][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, pl[j], O[j][t], 0, 0, 0);
-                }
+                O[j][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, ph[j], O[j][t], 0, 0, 0);
+                O[j][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, pl[j], O[j][t], 0, 0, 0);
             }
         }
-        if (more) {
-            store(mem + (side ^ 1) * (Lds::k + Lds::v), t0 + kTwPos);      // (read last ahead of the barrier before this tile)
-            now = good;
-        }
-        __syncthreads();
     }
+    tw_arrive<0>();                                        // nothing is on its way to LDS any more
     const TaSlot<D> slot = ta_slot<D>(L, plan, it, P.pg.heads, w.head, it.piece);
 #pragma unroll
     for (int j = 0; j < QT; ++j) {

@@ -30,6 +30,7 @@ def refused(call, *args, **more):
 @pytest.mark.parametrize("pages,status", [
     (PAGES, 0), ((1, 16, 1, 64), 0), ((1 << 20, 16, 32, 128), 0), ((0, 64, 4, 80), -1), ((4, 0, 4, 80), -1), ((4, 64, 0, 80), -1),
     ((4, 64, 4, 0), -1), ((1 << 27, 16, 1, 64), -1), ((4, 40, 4, 80), -2), ((4, 8, 4, 80), -2), ((4, 64, 4, 96), -2), ((4, 64, 1025, 64), -2),
+    ((2, (1 << 20) + 16, 1, 64), -2), ((2, 1 << 20, 1, 64), 0),
 ])
 def test_pages(pages, status):
     p = cf.Pages(*pages)
