@@ -39,7 +39,8 @@ TreePlanLayout tree_plan_layout(const PageDims &pg, int n_heads, int requests, i
     const long long each = (group * max_nodes + L.tile_rows - 1) / L.tile_rows * requests, all = group * max_rows / L.tile_rows + requests;
     L.tiles = (int)(each < all ? each : all);
     L.want = (kTaWgs + pg.heads - 1) / pg.heads;
-    L.work = L.want + L.tiles;                             // (pieces of a tile: its share of `want`, rounded up)
+    L.work = L.want + L.tiles;                             // (pieces of a tile: its share of `want`, to the nearest whole number, and one at least)
+    L.piece_step = L.tile_rows <= 32 ? kTaStep : kTaRow;
     size_t o = align_up(sizeof(TreePlanHead), 256);
     L.items = o; o = align_up(o + (size_t)L.work * sizeof(TreeItem), 256);
     L.counters = o; o = align_up(o + (size_t)L.tiles * pg.heads * 4, 256);
@@ -99,8 +100,8 @@ __device__ __forceinline__ void tree_masks(const PageDims &pg, const TreeBatch &
     b.positions[first + i] = b.lens[r] + depth;
 }
 
-// The work list, by one workgroup: with tiles_r tiles of query rows, a request's positions are cut into pieces of C, a multiple of what the wavefronts take
-// at a time, so that all pieces come to `want` and one more for each tile at most.
+// The work list, by one workgroup: with tiles_r tiles of query rows, a request's positions are cut into equal pieces of about C, multiples of what the
+// wavefronts take at a time, so that all pieces come to about `want`.
 __device__ __forceinline__ void tree_work(const PageDims &pg, const TreeBatch &b, int group, const TreePlanLayout &L, char *plan)
 {
     __shared__ int items[kTreeMaxRequests], multi[kTreeMaxRequests], tiles[kTreeMaxRequests];     // running sums
@@ -121,11 +122,13 @@ __device__ __forceinline__ void tree_work(const PageDims &pg, const TreeBatch &b
     __syncthreads();
     total = 0;
     for (int w = 0; w < kTaWaves; ++w) total += wave_total[w];
-    const long long least = (total + L.want - 1) / L.want, C = (least + kTaStep - 1) / kTaStep * kTaStep;
-    // (C is at least kTaStep wherever there is a position)
+    const long long C = max((total + L.want - 1) / L.want, (long long)kTaStep);
+    // the nearest number of pieces: they come to 4 / 3 of `want` at most beside those of the tiles that stay whole
+    auto piece_size = [&](int x, int pieces) { return ((x + pieces - 1) / pieces + L.piece_step - 1) / L.piece_step * L.piece_step; };
+    auto pieces_of = [&](int x) { return x <= kTaWhole ? 1 : max(1, (int)((2 * (long long)x + C) / (2 * C))); };
     int sum[3] = {0, 0, 0};
     for (int r = lo; r < hi; ++r) {
-        const int t = tiles[r], pieces = t <= 0 ? 0 : items[r] <= kTaWhole ? 1 : (int)((items[r] + C - 1) / C);
+        const int t = tiles[r], x = items[r], n = pieces_of(x), size = piece_size(x, n), pieces = t <= 0 ? 0 : (x + size - 1) / size;
         sum[0] += t * pieces;
         sum[1] += pieces > 1 ? t * pieces : 0;
         sum[2] += t;
@@ -169,8 +172,9 @@ __device__ __forceinline__ void tree_work(const PageDims &pg, const TreeBatch &b
         it.piece = at / n_tiles;                           // (the tiles of a piece follow one another: they read the same rows)
         it.tile = at - it.piece * n_tiles;
         it.slot = it.pieces > 1 ? (r > 0 ? multi[r - 1] : 0) + it.tile * it.pieces : -1;
-        it.t0 = (int)(it.piece * C);
-        it.t1 = it.piece == it.pieces - 1 ? it.len + it.nodes : (int)((it.piece + 1) * C);
+        const int x = it.len + it.nodes, size = piece_size(x, pieces_of(x));
+        it.t0 = it.piece * size;
+        it.t1 = min(x, it.t0 + size);
         it.counter = t0 + it.tile;
         it.pad = 0;
         list[i] = it;
@@ -387,23 +391,27 @@ __device__ __forceinline__ void ta_deliver(const TreeAttention &P, const TreeIte
     *as_global(reinterpret_cast<ta_u32x2 *>(P.out + (size_t)(it.first + node) * P.out_stride + (size_t)qh * D + dim)) = o;
 }
 
+// 16 bytes that another workgroup of the launch reads or has written, as xwg_store and xwg_load (device scope), at an offset of a buffer
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t ta_sums(char *p) { return __builtin_amdgcn_make_buffer_rsrc(p, 0, 0x7fffffff, 0x00020000); }
+constexpr int kTaDevice = 16;                              // sc1
+__device__ __forceinline__ f32x4 ta_load(__amdgpu_buffer_rsrc_t b, unsigned off) { return __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(b, (int)off, 0, kTaDevice)); }
+__device__ __forceinline__ void ta_store(__amdgpu_buffer_rsrc_t b, unsigned off, f32x4 v) { __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), b, (int)off, 0, kTaDevice); }
+
 // Where a tile's pieces leave their sums: [piece][key head], each [row][D] and then (maximum, weight) of each row
 template <int D>
 struct TaSlot {
+    __amdgpu_buffer_rsrc_t sums;
     float *p;
+    unsigned at;                       // bytes
     int tile_rows;
-    __device__ __forceinline__ void put(int i, int dim, f32x4 s) const
+    __device__ __forceinline__ TaSlot(const TreePlanLayout &L, char *plan, const TreeItem &it, int H, int head, int piece)
+        : sums(ta_sums(plan + L.sums)), p(reinterpret_cast<float *>(plan + L.sums)),
+          at((unsigned)(((size_t)max(it.slot + piece, 0) * H + head) * (L.tile_rows * (D + 2)) * 4)), tile_rows(L.tile_rows)
     {
-        xwg_store2(p + i * D + dim, s[0], s[1]);
-        xwg_store2(p + i * D + dim + 2, s[2], s[3]);
     }
-    __device__ __forceinline__ void put_ml(int i, float m, float l) const { xwg_store2(p + tile_rows * D + 2 * i, m, l); }
+    __device__ __forceinline__ void put(int i, int dim, f32x4 s) const { ta_store(sums, at + (i * D + dim) * 4, s); }
+    __device__ __forceinline__ void put_ml(int i, float m, float l) const { xwg_store2(p + at / 4 + tile_rows * D + 2 * i, m, l); }
 };
-template <int D>
-__device__ __forceinline__ TaSlot<D> ta_slot(const TreePlanLayout &L, char *plan, const TreeItem &it, int H, int head, int piece)
-{
-    return TaSlot<D>{reinterpret_cast<float *>(plan + L.sums) + ((size_t)max(it.slot + piece, 0) * H + head) * ((size_t)L.tile_rows * (D + 2)), L.tile_rows};
-}
 
 // The tile's last workgroup adds the pieces in order.
 template <int D, bool STACK>
@@ -417,22 +425,23 @@ __device__ __forceinline__ void ta_join(const TreeAttention &P, const TreePlanLa
     if (tid == 0) *last_one = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (unsigned)it.pieces - 1;
     __syncthreads();
     if (!*last_one) return;
-    const float *from = ta_slot<D>(L, plan, it, H, head, 0).p;
-    const size_t step = (size_t)H * L.tile_rows * (D + 2);                 // from piece to piece
+    const TaSlot<D> slot(L, plan, it, H, head, 0);
+    const unsigned step = (unsigned)(H * L.tile_rows * (D + 2) * 4);       // from piece to piece
     for (int e = tid; e < rows * D4; e += kTaThreads) {
         const int i = e / D4, dim = 4 * (e - i * D4);
+        const unsigned at = slot.at + (i * D + dim) * 4;
+        const float *ml_at = slot.p + slot.at / 4 + L.tile_rows * D + 2 * i;
         float M = kTaLowest, l = 0.f;
         f32x4 s = {0.f, 0.f, 0.f, 0.f};
-        constexpr int AT = 8;                              // in flight together (past the last: the last again)
+        constexpr int AT = 12;                             // in flight together (past the last: the last again)
         for (int z = 0; z < it.pieces; z += AT) {
             float2 ml[AT];
             f32x4 a[AT];
 #pragma unroll
             for (int u = 0; u < AT; ++u) {
-                const float *f = from + (size_t)min(z + u, it.pieces - 1) * step;
-                ml[u] = xwg_load2(f + L.tile_rows * D + 2 * i);
-                const float2 lo = xwg_load2(f + i * D + dim), hi = xwg_load2(f + i * D + dim + 2);
-                a[u] = f32x4{lo.x, lo.y, hi.x, hi.y};
+                const int q = min(z + u, it.pieces - 1);
+                ml[u] = xwg_load2(ml_at + (size_t)q * (step / 4));
+                a[u] = ta_load(slot.sums, at + q * step);
             }
 #pragma unroll
             for (int u = 0; u < AT; ++u) {
@@ -684,7 +693,7 @@ __device__ __forceinline__ void ta_narrow(const TreeAttention &P, const TreePlan
         }
     }
     __syncthreads();
-    const TaSlot<D> slot = ta_slot<D>(L, plan, it, P.pg.heads, w.head, it.piece);
+    const TaSlot<D> slot(L, plan, it, P.pg.heads, w.head, it.piece);
     for (int e = tid; e < w.rows * D4; e += kTaThreads) {
         const int i = e / D4, dim = 4 * (e - i * D4);
         float M = wm[i], l = 0.f;
@@ -808,7 +817,7 @@ __device__ __forceinline__ void ta_wide(const TreeAttention &P, const TreePlanLa
         }
     }
     tw_arrive<0>();                                        // nothing is on its way to LDS any more
-    const TaSlot<D> slot = ta_slot<D>(L, plan, it, P.pg.heads, w.head, it.piece);
+    const TaSlot<D> slot(L, plan, it, P.pg.heads, w.head, it.piece);
 #pragma unroll
     for (int j = 0; j < QT; ++j) {
         const int i = wave * RW + 16 * j + col;

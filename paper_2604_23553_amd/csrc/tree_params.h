@@ -54,6 +54,7 @@ struct TreeItem {
 struct TreePlanHead { int items, key, pad[14]; };
 struct TreePlanLayout {
     int tile_rows, want, tiles, work;  // rows of a tile; items aimed at; most tiles; most items
+    int piece_step;                    // positions that pieces are multiples of
     int key;                           // of the sizes that a plan is made for
     size_t items, counters, sums, total;   // byte offsets
 };
