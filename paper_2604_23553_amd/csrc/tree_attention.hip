@@ -538,12 +538,9 @@ struct TaQuery {
     }
 };
 
-// A query tile's 16 rows and 32 positions: scores (of this lane: row lane % 16, positions 4 (lane / 16) .. + 3 of both granules) to weights, and the
-// sums so far to the new maximum.  window: which positions the row sees, where `masked`.  A weight's head is cut off, not rounded, and its
-// remainder, which is exact, is cut off in turn: together 2^-21 of it.
-template <int NT>
-__device__ __forceinline__ void ta_weights(f32x4 (&S)[2], float scale, bool masked, const bool (&good)[2], unsigned window, int kg, float &m_run, float &l_run,
-                                           f32x4 (&O)[NT], ta_f16x8 &ph, ta_f16x8 &pl)
+// A query tile's 16 rows and 32 positions, scores of this lane: row lane % 16, positions 4 (lane / 16) .. + 3 of both granules.
+// What a row does not see is minus infinity, what lies in no page of the pool no number.  window: which positions the row sees, where `masked`
+__device__ __forceinline__ void ta_mask(f32x4 (&S)[2], bool masked, const bool (&good)[2], unsigned window, int kg)
 {
     if (masked) {
 #pragma unroll
@@ -554,6 +551,11 @@ __device__ __forceinline__ void ta_weights(f32x4 (&S)[2], float scale, bool mask
                 S[t][e] = (window >> (16 * t + 4 * kg + e)) & 1 ? s : -INFINITY;
             }
     }
+}
+// the sums so far to the new maximum, where it rises
+template <int NT>
+__device__ __forceinline__ void ta_rise(const f32x4 (&S)[2], float scale, float &m_run, float &l_run, f32x4 (&O)[NT])
+{
     float most = -INFINITY;
 #pragma unroll
     for (int t = 0; t < 2; ++t)
@@ -567,6 +569,10 @@ __device__ __forceinline__ void ta_weights(f32x4 (&S)[2], float scale, bool mask
 #pragma unroll
         for (int t = 0; t < NT; ++t) O[t] *= corr;
     }
+}
+// Weights.  One's head is cut off, not rounded, and its remainder, which is exact, is cut off in turn: together 2^-21 of it.
+__device__ __forceinline__ void ta_weights(const f32x4 (&S)[2], float scale, float m_run, float &l_run, ta_f16x8 &ph, ta_f16x8 &pl)
+{
     const float base = kTaUp - m_run;
     u32x4 hi, lo;
     float sum[2] = {0.f, 0.f};
@@ -651,7 +657,9 @@ __device__ __forceinline__ void ta_narrow(const TreeAttention &P, const TreePlan
         for (int j = 0; j < QT; ++j) {
             unsigned window = ~0u;
             if (masked) window = ta_window(smask[16 * j + col], words, row * kTaRow, it.len, it.nodes);
-            ta_weights(S[j], scale, masked, good, window, kg, m_run[j], l_run[j], O[j], ph[j], pl[j]);
+            ta_mask(S[j], masked, good, window, kg);
+            ta_rise(S[j], scale, m_run[j], l_run[j], O[j]);
+            ta_weights(S[j], scale, m_run[j], l_run[j], ph[j], pl[j]);
         }
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
@@ -775,16 +783,10 @@ __device__ __forceinline__ void ta_wide(const TreeAttention &P, const TreePlanLa
 #pragma unroll
         for (int t = 0; t < NT; ++t) O[j][t] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    int at = 0;
-    for (int row = first; row * kTaRow < it.t1; ++row, at = (at + 1) % kTwRing) {
-        tw_arrive<(kTwRing - 2) * Lds::loads>();
-        const unsigned good = (goods >> (2 * at)) & 3;
-        request(row + kTwRing - 1, (at + kTwRing - 1) % kTwRing, next);    // (the place of the row before this one, which everyone has read)
-        next = w.pages.pick(row + kTwRing);
-        const char *kb = mem + at * Lds::row, *vb = kb + 2 * Lds::granule;
-        const bool two[2] = {(good & 1) != 0, (good & 2) != 0};
-        const bool masked = row * kTaRow + kTaRow > it.len || good != 3;
-        f32x4 S[QT][2];
+    // Scores are a row ahead of the weights: the matrix instructions of one run beside the vector instructions of the other.
+    f32x4 S[QT][2];
+    auto scores = [&](int at, f32x4 (&S)[QT][2]) {
+        const char *kb = mem + at * Lds::row;
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
 #pragma unroll
@@ -798,13 +800,31 @@ __device__ __forceinline__ void ta_wide(const TreeAttention &P, const TreePlanLa
                 for (int j = 0; j < QT; ++j) S[j][t] = Q[j].score(k, s, S[j][t]);
             }
         }
-        ta_f16x8 ph[QT], pl[QT];
+    };
+    tw_arrive<(kTwRing - 2) * Lds::loads>();
+    scores(0, S);
+    int at = 0;
+    for (int row = first; row * kTaRow < it.t1; ++row) {
+        const int ahead = (at + 1) % kTwRing;
+        tw_arrive<(kTwRing - 3) * Lds::loads>();           // (the next row is here)
+        const unsigned good = (goods >> (2 * at)) & 3;
+        request(row + kTwRing - 1, (at + kTwRing - 1) % kTwRing, next);    // (the place of the row before this one, which everyone has read)
+        next = w.pages.pick(row + kTwRing);
+        const char *vb = mem + at * Lds::row + 2 * Lds::granule;
+        const bool two[2] = {(good & 1) != 0, (good & 2) != 0};
+        const bool masked = row * kTaRow + kTaRow > it.len || good != 3;
 #pragma unroll
         for (int j = 0; j < QT; ++j) {
             unsigned window = ~0u;
             if (masked) window = ta_window(smask[wave * RW + 16 * j + col], words, row * kTaRow, it.len, it.nodes);
-            ta_weights(S[j], scale, masked, two, window, kg, m_run[j], l_run[j], O[j], ph[j], pl[j]);
+            ta_mask(S[j], masked, two, window, kg);
+            ta_rise(S[j], scale, m_run[j], l_run[j], O[j]);
         }
+        f32x4 ahead_S[QT][2];
+        scores(ahead, ahead_S);
+        ta_f16x8 ph[QT], pl[QT];
+#pragma unroll
+        for (int j = 0; j < QT; ++j) ta_weights(S[j], scale, m_run[j], l_run[j], ph[j], pl[j]);
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
             const ta_u32x2 v0 = ta_transposed(vb + t * 512, lane), v1 = ta_transposed(vb + Lds::granule + t * 512, lane);
@@ -815,6 +835,11 @@ __device__ __forceinline__ void ta_wide(const TreeAttention &P, const TreePlanLa
                 O[j][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, pl[j], O[j][t], 0, 0, 0);
             }
         }
+#pragma unroll
+        for (int j = 0; j < QT; ++j)
+#pragma unroll
+            for (int t = 0; t < 2; ++t) S[j][t] = ahead_S[j][t];
+        at = ahead;
     }
     tw_arrive<0>();                                        // nothing is on its way to LDS any more
     const TaSlot<D> slot(L, plan, it, P.pg.heads, w.head, it.piece);
