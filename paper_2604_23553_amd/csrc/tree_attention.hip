@@ -785,8 +785,18 @@ __device__ __forceinline__ void ta_wide(const TreeAttention &P, const TreePlanLa
     }
     // Scores are a row ahead of the weights: the matrix instructions of one run beside the vector instructions of the other.
     f32x4 S[QT][2];
-    auto scores = [&](int at, f32x4 (&S)[QT][2]) {
+    u32x4 k[2][KS];
+    auto keys = [&](int at) {
         const char *kb = mem + at * Lds::row;
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int s = 0; s < KS; ++s) {
+                const bool real = D % 32 == 0 || 32 * s + 8 * kg < D;
+                k[t][s] = *reinterpret_cast<const u32x4 *>(kb + t * Lds::granule + (real ? 2 * s + (kg >> 1) : 0) * 512 + col * 32 + (kg & 1) * 16);
+            }
+    };
+    auto scores = [&](f32x4 (&S)[QT][2]) {
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
 #pragma unroll
@@ -794,19 +804,20 @@ __device__ __forceinline__ void ta_wide(const TreeAttention &P, const TreePlanLa
 #pragma unroll
             for (int s = 0; s < KS; ++s) {
                 const bool real = D % 32 == 0 || 32 * s + 8 * kg < D;
-                u32x4 k = *reinterpret_cast<const u32x4 *>(kb + t * Lds::granule + (real ? 2 * s + (kg >> 1) : 0) * 512 + col * 32 + (kg & 1) * 16);
-                if (!real) k = u32x4{0u, 0u, 0u, 0u};
+                const u32x4 x = real ? k[t][s] : u32x4{0u, 0u, 0u, 0u};
 #pragma unroll
-                for (int j = 0; j < QT; ++j) S[j][t] = Q[j].score(k, s, S[j][t]);
+                for (int j = 0; j < QT; ++j) S[j][t] = Q[j].score(x, s, S[j][t]);
             }
         }
     };
     tw_arrive<(kTwRing - 2) * Lds::loads>();
-    scores(0, S);
+    keys(0);
+    scores(S);
     int at = 0;
     for (int row = first; row * kTaRow < it.t1; ++row) {
         const int ahead = (at + 1) % kTwRing;
         tw_arrive<(kTwRing - 3) * Lds::loads>();           // (the next row is here)
+        keys(ahead);
         const unsigned good = (goods >> (2 * at)) & 3;
         request(row + kTwRing - 1, (at + kTwRing - 1) % kTwRing, next);    // (the place of the row before this one, which everyone has read)
         next = w.pages.pick(row + kTwRing);
@@ -821,7 +832,7 @@ __device__ __forceinline__ void ta_wide(const TreeAttention &P, const TreePlanLa
             ta_rise(S[j], scale, m_run[j], l_run[j], O[j]);
         }
         f32x4 ahead_S[QT][2];
-        scores(ahead, ahead_S);
+        scores(ahead_S);
         ta_f16x8 ph[QT], pl[QT];
 #pragma unroll
         for (int j = 0; j < QT; ++j) ta_weights(S[j], scale, m_run[j], l_run[j], ph[j], pl[j]);
