@@ -27,7 +27,9 @@ typedef unsigned ta_u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kTaThreads = 256, kTaWaves = kTaThreads / 64, kTaRow = 32, kTaStep = kTaRow * kTaWaves;
 constexpr int kTaWhole = 256;                              // positions that are not cut
+constexpr int kTaWgsWide = 512;
 constexpr int kTaWgs = 512;                                // workgroups that the pieces aim at
+constexpr int kTaLastJoins = 32;                           // up to so many query rows to a tile its last workgroup adds the pieces
 constexpr float kTaLowest = -3.402823466e38f;
 
 // ---- the plan --------------------------------------------------------------------------------------
@@ -38,11 +40,12 @@ TreePlanLayout tree_plan_layout(const PageDims &pg, int n_heads, int requests, i
     L.tile_rows = tree_tile_rows((int)(group * max_nodes));
     const long long each = (group * max_nodes + L.tile_rows - 1) / L.tile_rows * requests, all = group * max_rows / L.tile_rows + requests;
     L.tiles = (int)(each < all ? each : all);
-    L.want = (kTaWgs + pg.heads - 1) / pg.heads;
+    L.want = ((L.tile_rows <= kTaLastJoins ? kTaWgs : kTaWgsWide) + pg.heads - 1) / pg.heads;
     L.work = L.want + L.tiles;                             // (pieces of a tile: its share of `want`, to the nearest whole number, and one at least)
     L.piece_step = L.tile_rows <= 32 ? kTaStep : kTaRow;
     size_t o = align_up(sizeof(TreePlanHead), 256);
     L.items = o; o = align_up(o + (size_t)L.work * sizeof(TreeItem), 256);
+    L.cut = o; o = align_up(o + (size_t)L.want * sizeof(int), 256);
     L.counters = o; o = align_up(o + (size_t)L.tiles * pg.heads * 4, 256);
     // tiles of more than one piece have less than twice `want` of them in all
     L.sums = o; o = align_up(o + (size_t)2 * L.want * pg.heads * L.tile_rows * (pg.d + 2) * 4, 256);
@@ -105,7 +108,8 @@ __device__ __forceinline__ void tree_masks(const PageDims &pg, const TreeBatch &
 __device__ __forceinline__ void tree_work(const PageDims &pg, const TreeBatch &b, int group, const TreePlanLayout &L, char *plan)
 {
     __shared__ int items[kTreeMaxRequests], multi[kTreeMaxRequests], tiles[kTreeMaxRequests];     // running sums
-    __shared__ int wave_part[3][kTaWaves];
+    __shared__ int wave_part[3][kTaWaves], cuts;
+    if (threadIdx.x == 0) cuts = 0;
     __shared__ long long wave_total[kTaWaves];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, R = b.requests, each = (R + kTaThreads - 1) / kTaThreads;
     const int lo = min(tid * each, R), hi = min(lo + each, R);
@@ -156,6 +160,7 @@ __device__ __forceinline__ void tree_work(const PageDims &pg, const TreeBatch &b
         reinterpret_cast<TreePlanHead *>(plan)->key = L.key;
     }
     TreeItem *list = reinterpret_cast<TreeItem *>(plan + L.items);
+    int *cut = reinterpret_cast<int *>(plan + L.cut);
     for (int i = tid; i < n_items; i += kTaThreads) {
         int a = 0, z = R - 1;                              // the first request whose sum is above i
         while (a < z) {
@@ -176,9 +181,12 @@ __device__ __forceinline__ void tree_work(const PageDims &pg, const TreeBatch &b
         it.t0 = it.piece * size;
         it.t1 = min(x, it.t0 + size);
         it.counter = t0 + it.tile;
+        if (it.pieces > 1 && it.piece == 0) cut[atomicAdd(&cuts, 1)] = i;              // (at most want / 1.5; in any order)
         it.pad = 0;
         list[i] = it;
     }
+    __syncthreads();
+    if (tid == 0) reinterpret_cast<TreePlanHead *>(plan)->cuts = cuts;
     unsigned *counters = reinterpret_cast<unsigned *>(plan + L.counters);
     for (int i = tid; i < L.tiles * pg.heads; i += kTaThreads) counters[i] = 0u;
 }
@@ -915,7 +923,45 @@ __global__ void __launch_bounds__(kTaThreads, 2) k_tree_attention(TreeAttention 
     } else {
         if constexpr (TQ >= 128) ta_wide<D, TQ, 2, STACK>(P, L, plan, w, ta_mem, smask);
     }
-    if (w.it.pieces > 1) ta_join<D, STACK>(P, L, plan, w.it, P.pg.heads, w.head, w.rows, &last_one);
+    if constexpr (TQ <= kTaLastJoins)
+        if (w.it.pieces > 1) ta_join<D, STACK>(P, L, plan, w.it, P.pg.heads, w.head, w.rows, &last_one);
+}
+
+// The pieces of many query rows are added by a launch of its own, 1024 sums to a workgroup: for one workgroup they are up to 16384.
+template <int D, int TQ, bool STACK>
+__global__ void __launch_bounds__(kTaThreads) k_tree_join(TreeAttention P, TreePlanLayout L, const char *plan)
+{
+    constexpr int D4 = D / 4, CHUNKS = (TQ * D4 + kTaThreads - 1) / kTaThreads;
+    const int H = P.pg.heads, b = (int)blockIdx.x / CHUNKS, chunk = (int)blockIdx.x - b * CHUNKS, k = b / H, head = b - k * H;
+    const TreePlanHead &plan_head = *reinterpret_cast<const TreePlanHead *>(plan);
+    if (plan_head.key != L.key || k >= plan_head.cuts) return;
+    const TreeItem it = reinterpret_cast<const TreeItem *>(plan + L.items)[reinterpret_cast<const int *>(plan + L.cut)[k]];
+    const int e = chunk * kTaThreads + (int)threadIdx.x, i = e / D4, dim = 4 * (e - i * D4);
+    if (i >= min(TQ, it.nodes * P.group - it.tile * TQ)) return;
+    const size_t step = (size_t)H * TQ * (D + 2);          // from piece to piece
+    const float *at = reinterpret_cast<const float *>(plan + L.sums) + ((size_t)it.slot * H + head) * (TQ * (D + 2));
+    float M = kTaLowest, l = 0.f;
+    f32x4 s = {0.f, 0.f, 0.f, 0.f};
+    constexpr int AT = 8;                                  // in flight together (past the last: the last again)
+    for (int z = 0; z < it.pieces; z += AT) {
+        float2 ml[AT];
+        f32x4 a[AT];
+#pragma unroll
+        for (int u = 0; u < AT; ++u) {
+            const float *f = at + (size_t)min(z + u, it.pieces - 1) * step;
+            ml[u] = *reinterpret_cast<const float2 *>(f + TQ * D + 2 * i);
+            a[u] = *as_global(reinterpret_cast<const f32x4 *>(f + i * D + dim));
+        }
+#pragma unroll
+        for (int u = 0; u < AT; ++u) {
+            if (z + u >= it.pieces) continue;              // (uniform)
+            const float mn = fmaxf(M, ml[u].x), c0 = __builtin_amdgcn_exp2f(M - mn), c1 = __builtin_amdgcn_exp2f(ml[u].x - mn);
+            l = l * c0 + ml[u].y * c1;
+            s = s * c0 + a[u] * c1;
+            M = mn;
+        }
+    }
+    ta_deliver<D, STACK>(P, it, head, it.tile * TQ + i, dim, s, l);
 }
 
 template <int D, int TQ, bool STACK>
@@ -927,6 +973,10 @@ static hipError_t launch_tile(const TreeAttention &P, const TreePlanLayout &L, c
         if (e != hipSuccess) return e;
     }
     hipLaunchKernelGGL((k_tree_attention<D, TQ, STACK>), dim3((unsigned)L.work * P.pg.heads), dim3(kTaThreads), lds, s, P, L, plan);
+    if constexpr (TQ > kTaLastJoins) {
+        constexpr int chunks = (TQ * D / 4 + kTaThreads - 1) / kTaThreads;
+        hipLaunchKernelGGL((k_tree_join<D, TQ, STACK>), dim3((unsigned)L.want * P.pg.heads * chunks), dim3(kTaThreads), 0, s, P, L, plan);
+    }
     return hipGetLastError();
 }
 template <int D, bool STACK>

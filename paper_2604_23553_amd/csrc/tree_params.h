@@ -51,12 +51,12 @@ struct TreeItem {
     int tile, piece, pieces, slot;     // slot: the tile's first place among the sums, one for each piece; -1 with a single piece
     int t0, t1, counter, pad;          // positions; the tile's number
 };
-struct TreePlanHead { int items, key, pad[14]; };
+struct TreePlanHead { int items, key, cuts, pad[13]; };       // cuts: tiles that have several pieces, listed behind the items
 struct TreePlanLayout {
     int tile_rows, want, tiles, work;  // rows of a tile; items aimed at; most tiles; most items
     int piece_step;                    // positions that pieces are multiples of
     int key;                           // of the sizes that a plan is made for
-    size_t items, counters, sums, total;   // byte offsets
+    size_t items, cut, counters, sums, total;   // byte offsets
 };
 CFPP_HD int tree_tile_rows(int max_rows_of_request) { return max_rows_of_request <= 16 ? 16 : max_rows_of_request <= 32 ? 32 : max_rows_of_request <= 64 ? 64 : 128; }
 TreePlanLayout tree_plan_layout(const PageDims &pg, int n_heads, int requests, int max_rows, int max_nodes, int stride);
