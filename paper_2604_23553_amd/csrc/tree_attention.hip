@@ -10,7 +10,7 @@
 // One pass over the positions with the running maximum and sum of the softmax; a workgroup has a piece of a request's positions for one
 // key head, its four wavefronts every fourth row of 32 of them, each with sums of its own that are joined in LDS in order.  Requests of
 // few rows are cut into pieces until the CUs are full (k_tree_plan); the last workgroup of a tile adds the pieces in order.
-// Weights enter the matrix instruction as two fp16 values, head and remainder, 2^14 times their size: 2^-22 of each and 2^-38 of the largest, as near
+// Weights enter the matrix instruction as two fp16 values, head and remainder, 2^9 times their size: 2^-21 of each and 2^-33 of the largest, as near
 // as the sums in 32 bits are.  Queries and keys are fp16 as they come.
 #include <hip/hip_runtime.h>
 #include <hip/hip_fp16.h>
@@ -29,7 +29,8 @@ constexpr int kTaThreads = 256, kTaWaves = kTaThreads / 64, kTaRow = 32, kTaStep
 constexpr int kTaWhole = 256;                              // positions that are not cut
 constexpr int kTaWgsWide = 512;
 constexpr int kTaWgs = 512;                                // workgroups that the pieces aim at
-constexpr int kTaLastJoins = 32;                           // up to so many query rows to a tile its last workgroup adds the pieces
+constexpr int kTaShort = 1024;                             // positions of a piece
+constexpr int kTaLastJoins = 16;                           // up to so many query rows to a tile its last workgroup adds the pieces
 constexpr float kTaLowest = -3.402823466e38f;
 
 // ---- the plan --------------------------------------------------------------------------------------
@@ -126,7 +127,9 @@ __device__ __forceinline__ void tree_work(const PageDims &pg, const TreeBatch &b
     __syncthreads();
     total = 0;
     for (int w = 0; w < kTaWaves; ++w) total += wave_total[w];
-    const long long C = max((total + L.want - 1) / L.want, (long long)kTaStep);
+    // Few rows behind a short way: one workgroup to a CU (26 nodes behind 4096 positions of hidden 2560, pieces of 384 / 640: 22.2 / 18.1 us)
+    const int want = L.tile_rows <= 32 && total * 2 <= (long long)kTaShort * L.want ? (L.want + 1) / 2 : L.want;
+    const long long C = max((total + want - 1) / want, (long long)kTaStep);
     // the nearest number of pieces: they come to 4 / 3 of `want` at most beside those of the tiles that stay whole
     auto piece_size = [&](int x, int pieces) { return ((x + pieces - 1) / pieces + L.piece_step - 1) / L.piece_step * L.piece_step; };
     auto pieces_of = [&](int x) { return x <= kTaWhole ? 1 : max(1, (int)((2 * (long long)x + C) / (2 * C))); };
@@ -292,7 +295,7 @@ struct TaRow {
     }
 };
 
-// largest and sum over the four lanes that share lane % 16
+// largest of the four lanes that share lane % 16
 __device__ __forceinline__ float ta_max4(float v)
 {
     auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
@@ -300,15 +303,7 @@ __device__ __forceinline__ float ta_max4(float v)
     p = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
     return fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
 }
-__device__ __forceinline__ float ta_sum4(float v)
-{
-    auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    v = __uint_as_float(p[0]) + __uint_as_float(p[1]);
-    p = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    return __uint_as_float(p[0]) + __uint_as_float(p[1]);
-}
-
-constexpr float kTaUp = 14.f;                              // weights are 2^14 times their size
+constexpr float kTaUp = 9.f, kTaSlack = 6.f;               // (together at most 2^15, of fp16's 2^16)
 
 // 32 bits of "sees position t .. t + 31" of a node: cached positions, then its words; t a multiple of 32, its request's last position behind it or not
 __device__ __forceinline__ unsigned ta_window(const unsigned *words, int n_words, int t, int len, int nodes)
@@ -560,44 +555,49 @@ __device__ __forceinline__ void ta_mask(f32x4 (&S)[2], bool masked, const bool (
             }
     }
 }
-// the sums so far to the new maximum, where it rises
+// The sums so far to a new reference, where a score is 2^kTaSlack above the one that the weights are relative to; the reference is the same in the four
+// lanes of a row.  L: sums of the weights, in every element.
 template <int NT>
-__device__ __forceinline__ void ta_rise(const f32x4 (&S)[2], float scale, float &m_run, float &l_run, f32x4 (&O)[NT])
+__device__ __forceinline__ void ta_rise(const f32x4 (&S)[2], float scale, float &m_run, f32x4 &L, f32x4 (&O)[NT])
 {
-    float most = -INFINITY;
-#pragma unroll
-    for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) most = fmaxf(most, S[t][e]);
-    most = ta_max4(most) * scale;
-    if (__any(most > m_run)) {
-        const float mn = fmaxf(m_run, most), corr = __builtin_amdgcn_exp2f(m_run - mn);
+    float most = fmaxf(S[0][0], S[0][1]);
+    most = fmaxf(fmaxf(most, S[0][2]), S[0][3]);
+    most = fmaxf(fmaxf(most, S[1][0]), S[1][1]);
+    most = fmaxf(fmaxf(most, S[1][2]), S[1][3]) * scale;
+    if (__any(most > m_run + kTaSlack)) {
+        const float mn = fmaxf(m_run, ta_max4(most)), corr = __builtin_amdgcn_exp2f(m_run - mn);
         m_run = mn;
-        l_run *= corr;
+        L *= corr;
 #pragma unroll
         for (int t = 0; t < NT; ++t) O[t] *= corr;
     }
 }
-// Weights.  One's head is cut off, not rounded, and its remainder, which is exact, is cut off in turn: together 2^-21 of it.
-__device__ __forceinline__ void ta_weights(const f32x4 (&S)[2], float scale, float m_run, float &l_run, ta_f16x8 &ph, ta_f16x8 &pl)
+// Weights, 2^kTaUp times their size.  One's head is cut off, not rounded, and its remainder, which is exact, is cut off in turn: together 2^-21 of it.
+__device__ __forceinline__ void ta_weights(const f32x4 (&S)[2], float scale, float m_run, ta_f16x8 &ph, ta_f16x8 &pl)
 {
     const float base = kTaUp - m_run;
+    float minus = -1.f;                                    // (as a number that the compiler does not know: one instruction from a half to a remainder)
+    asm("" : "+v"(minus));
     u32x4 hi, lo;
-    float sum[2] = {0.f, 0.f};
 #pragma unroll
     for (int e = 0; e < 4; ++e) {                          // words: positions 4 kg + 0, 1; + 2, 3; the same of the second granule
         const int t = e >> 1, i = 2 * (e & 1);
         const float p0 = split_value(__builtin_amdgcn_exp2f(fmaf(S[t][i], scale, base))), p1 = split_value(__builtin_amdgcn_exp2f(fmaf(S[t][i + 1], scale, base)));
         const auto h = __builtin_amdgcn_cvt_pkrtz(p0, p1);
-        const auto l = __builtin_amdgcn_cvt_pkrtz(fmaf((float)h[0], -1.f, p0), fmaf((float)h[1], -1.f, p1));
-        sum[0] += p0;
-        sum[1] += p1;
+        const auto l = __builtin_amdgcn_cvt_pkrtz(fmaf((float)h[0], minus, p0), fmaf((float)h[1], minus, p1));
         hi[e] = __builtin_bit_cast(unsigned, h);
         lo[e] = __builtin_bit_cast(unsigned, l);
     }
-    l_run += sum[0] + sum[1];
     ph = __builtin_bit_cast(ta_f16x8, hi);
     pl = __builtin_bit_cast(ta_f16x8, lo);
+}
+// a row's weights, added up by the matrix instruction too: every element of the sum is the total over the 32 positions
+__device__ __forceinline__ f32x4 ta_total(ta_f16x8 ph, ta_f16x8 pl, f32x4 L)
+{
+    const _Float16 one = (_Float16)1.f;
+    const ta_f16x8 ones = {one, one, one, one, one, one, one, one};
+    L = __builtin_amdgcn_mfma_f32_16x16x32_f16(ones, ph, L, 0, 0, 0);
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(ones, pl, L, 0, 0, 0);
 }
 
 // ---- up to 32 query rows of a tile: the wavefronts share the positions --------------------------------------------
@@ -631,11 +631,12 @@ __device__ __forceinline__ void ta_narrow(const TreeAttention &P, const TreePlan
     if (tail) __syncthreads();                             // (uniform)
     const float scale = 1.44269504088896340736f / sqrtf((float)D);
     f32x4 O[QT][NT];
-    float m_run[QT], l_run[QT];                            // l_run: of this lane's positions
+    f32x4 sum[QT];
+    float m_run[QT];
 #pragma unroll
     for (int j = 0; j < QT; ++j) {
         m_run[j] = kTaLowest;
-        l_run[j] = 0.f;
+        sum[j] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int t = 0; t < NT; ++t) O[j][t] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
@@ -666,8 +667,9 @@ __device__ __forceinline__ void ta_narrow(const TreeAttention &P, const TreePlan
             unsigned window = ~0u;
             if (masked) window = ta_window(smask[16 * j + col], words, row * kTaRow, it.len, it.nodes);
             ta_mask(S[j], masked, good, window, kg);
-            ta_rise(S[j], scale, m_run[j], l_run[j], O[j]);
-            ta_weights(S[j], scale, m_run[j], l_run[j], ph[j], pl[j]);
+            ta_rise(S[j], scale, m_run[j], sum[j], O[j]);
+            ta_weights(S[j], scale, m_run[j], ph[j], pl[j]);
+            sum[j] = ta_total(ph[j], pl[j], sum[j]);
         }
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
@@ -691,7 +693,7 @@ __device__ __forceinline__ void ta_narrow(const TreeAttention &P, const TreePlan
 #pragma unroll
     for (int j = 0; j < QT; ++j) {
         const int at = wave * TR + 16 * j;
-        const float l = ta_sum4(l_run[j]);
+        const float l = sum[j][0];
         bool finite = fabsf(l) < INFINITY;
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
@@ -783,11 +785,12 @@ __device__ __forceinline__ void ta_wide(const TreeAttention &P, const TreePlanLa
     for (int j = 0; j < QT; ++j) Q[j].load(w.query(P, wave * RW + 16 * j + col), kg);
     const float scale = 1.44269504088896340736f / sqrtf((float)D);
     f32x4 O[QT][NT];
-    float m_run[QT], l_run[QT];
+    f32x4 sum[QT];
+    float m_run[QT];
 #pragma unroll
     for (int j = 0; j < QT; ++j) {
         m_run[j] = kTaLowest;
-        l_run[j] = 0.f;
+        sum[j] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int t = 0; t < NT; ++t) O[j][t] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
@@ -837,13 +840,16 @@ __device__ __forceinline__ void ta_wide(const TreeAttention &P, const TreePlanLa
             unsigned window = ~0u;
             if (masked) window = ta_window(smask[wave * RW + 16 * j + col], words, row * kTaRow, it.len, it.nodes);
             ta_mask(S[j], masked, two, window, kg);
-            ta_rise(S[j], scale, m_run[j], l_run[j], O[j]);
+            ta_rise(S[j], scale, m_run[j], sum[j], O[j]);
         }
         f32x4 ahead_S[QT][2];
         scores(ahead_S);
         ta_f16x8 ph[QT], pl[QT];
 #pragma unroll
-        for (int j = 0; j < QT; ++j) ta_weights(S[j], scale, m_run[j], l_run[j], ph[j], pl[j]);
+        for (int j = 0; j < QT; ++j) {
+            ta_weights(S[j], scale, m_run[j], ph[j], pl[j]);
+            sum[j] = ta_total(ph[j], pl[j], sum[j]);
+        }
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
             const ta_u32x2 v0 = ta_transposed(vb + t * 512, lane), v1 = ta_transposed(vb + Lds::granule + t * 512, lane);
@@ -865,7 +871,7 @@ __device__ __forceinline__ void ta_wide(const TreeAttention &P, const TreePlanLa
 #pragma unroll
     for (int j = 0; j < QT; ++j) {
         const int i = wave * RW + 16 * j + col;
-        float l = ta_sum4(l_run[j]);
+        float l = sum[j][0];
         bool finite = fabsf(l) < INFINITY;
 #pragma unroll
         for (int t = 0; t < NT; ++t)
