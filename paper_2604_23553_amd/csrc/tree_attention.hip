@@ -807,19 +807,20 @@ __device__ __forceinline__ void ta_wide(const TreeAttention &P, const TreePlanLa
                 k[t][s] = *reinterpret_cast<const u32x4 *>(kb + t * Lds::granule + (real ? 2 * s + (kg >> 1) : 0) * 512 + col * 32 + (kg & 1) * 16);
             }
     };
-    auto scores = [&](f32x4 (&S)[QT][2]) {
+    auto scores = [&](f32x4 (&S)[QT][2]) {                 // (the sums side by side: a matrix instruction does not wait for the one before)
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
+        for (int t = 0; t < 2; ++t)
 #pragma unroll
             for (int j = 0; j < QT; ++j) S[j][t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int s = 0; s < KS; ++s) {
+        for (int s = 0; s < KS; ++s)
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
                 const bool real = D % 32 == 0 || 32 * s + 8 * kg < D;
                 const u32x4 x = real ? k[t][s] : u32x4{0u, 0u, 0u, 0u};
 #pragma unroll
                 for (int j = 0; j < QT; ++j) S[j][t] = Q[j].score(x, s, S[j][t]);
             }
-        }
     };
     tw_arrive<(kTwRing - 2) * Lds::loads>();
     keys(0);
@@ -851,14 +852,19 @@ __device__ __forceinline__ void ta_wide(const TreeAttention &P, const TreePlanLa
             sum[j] = ta_total(ph[j], pl[j], sum[j]);
         }
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            const ta_u32x2 v0 = ta_transposed(vb + t * 512, lane), v1 = ta_transposed(vb + Lds::granule + t * 512, lane);
-            const ta_f16x8 v = __builtin_bit_cast(ta_f16x8, u32x4{v0[0], v0[1], v1[0], v1[1]});
+        for (int t = 0; t < NT; t += 2) {                  // (NT is 4, 5 or 8)
+            ta_f16x8 v[2];
 #pragma unroll
-            for (int j = 0; j < QT; ++j) {
-                O[j][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, ph[j], O[j][t], 0, 0, 0);
-                O[j][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, pl[j], O[j][t], 0, 0, 0);
+            for (int u = 0; u < 2 && t + u < NT; ++u) {
+                const ta_u32x2 v0 = ta_transposed(vb + (t + u) * 512, lane), v1 = ta_transposed(vb + Lds::granule + (t + u) * 512, lane);
+                v[u] = __builtin_bit_cast(ta_f16x8, u32x4{v0[0], v0[1], v1[0], v1[1]});
             }
+#pragma unroll
+            for (int part = 0; part < 2; ++part)
+#pragma unroll
+                for (int u = 0; u < 2 && t + u < NT; ++u)
+#pragma unroll
+                    for (int j = 0; j < QT; ++j) O[j][t + u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v[u], part ? pl[j] : ph[j], O[j][t + u], 0, 0, 0);
         }
 #pragma unroll
         for (int j = 0; j < QT; ++j)
