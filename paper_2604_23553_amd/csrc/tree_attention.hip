@@ -210,16 +210,15 @@ hipError_t launch_tree_plan(const PageDims &pg, const TreeBatch &b, int n_heads,
 
 // ---- the attention -----------------------------------------------------------------------------------
 // A granule of 16 positions lies in one page.
-struct TaPlace { size_t at; bool good; };                  // elements into the K or V half of the pool
-struct TaPick { int page[2], in[2]; };                     // of a row's granules: table entries, granules inside of their pages
+struct TaPick { int page, in; };                           // table entry, granule inside of its page
 
 struct TaPages {
     const int *table;
     int page16, n_pages, last;                             // last: the piece's last granule
     unsigned inv;
     size_t per_page, head;
-    // Rows are looked up well ahead of their request, by scalar loads: a vector load's wait would wait for the rows that are on their way too.
-    __device__ __forceinline__ void look(int granule, int &page, int &in) const
+    // Granules are looked up well ahead of their request, by scalar loads: a vector load's wait would wait for the rows that are on their way too.
+    __device__ __forceinline__ TaPick pick(int granule) const
     {
         const int g = min(granule, last);
         // g / page16: inv is ceil(2^32 / page16), so the product is at most one too large
@@ -227,24 +226,20 @@ struct TaPages {
         if (page16 == 1) p = g;
         else if (p * page16 > g) --p;
         p = __builtin_amdgcn_readfirstlane(p);
-        page = reinterpret_cast<const __attribute__((address_space(4))) int *>(reinterpret_cast<uintptr_t>(table))[p];
-        in = g - p * page16;
+        return TaPick{reinterpret_cast<const __attribute__((address_space(4))) int *>(reinterpret_cast<uintptr_t>(table))[p], g - p * page16};
     }
-    __device__ __forceinline__ TaPick pick(int row) const
+    // elements into the K or V half of the pool; an entry outside of it is read as the last page (bad() tells)
+    __device__ __forceinline__ size_t place(const TaPick &k) const
     {
-        TaPick k;
-        look(2 * row, k.page[0], k.in[0]);
-        look(2 * row + 1, k.page[1], k.in[1]);
-        return k;
+        return (size_t)min((unsigned)k.page, (unsigned)n_pages - 1u) * per_page + head + (size_t)k.in * 256;
     }
-    __device__ __forceinline__ TaPlace place(int page, int in) const
+    // whether an entry of the granules first .. last lies outside the pool (the same in all lanes)
+    __device__ __forceinline__ bool bad(int first, int lane) const
     {
-        TaPlace w;
-        w.good = (unsigned)page < (unsigned)n_pages;
-        w.at = (size_t)(w.good ? page : 0) * per_page + head + (size_t)in * 256;
-        return w;
+        bool b = false;
+        for (int p = first / page16 + lane; p <= last / page16; p += 64) b = b || (unsigned)table[p] >= (unsigned)n_pages;
+        return __any(b);
     }
-    __device__ __forceinline__ TaPlace place(const TaPick &k, int t) const { return place(k.page[t], k.in[t]); }
 };
 
 constexpr int ta_granule(int D) { return D * 32; }         // bytes of 16 positions of K or V: [d / 16][16][16] fp16
@@ -262,24 +257,18 @@ template <int D>
 struct TaRow {
     static constexpr int KS = (D + 31) / 32, PG = 2 * D, UN = 2 * PG / 64;             // PG: pieces of 16 bytes to a granule
     u32x4 k[2][KS], v[UN];
-    bool good[2];
-    __device__ __forceinline__ void request(const __half *K, const __half *V, const TaPages &pages, unsigned slab, const TaPick &pick, int lane)
+    __device__ __forceinline__ void request(const __half *K, const __half *V, const TaPages &pages, unsigned slab, const TaPick (&pick)[2], int lane)
     {
         const int n = lane & 15, kg = lane >> 4;
-        TaPlace w[2];
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            w[t] = pages.place(pick, t);
-            good[t] = w[t].good;
-        }
+        const size_t w[2] = {pages.place(pick[0]), pages.place(pick[1])};
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
-            for (int s = 0; s < KS; ++s) k[t][s] = load16_stream(K + w[t].at + (unsigned)min(2 * s + (kg >> 1), D / 16 - 1) * slab + n * 16u + (kg & 1) * 8u);
+            for (int s = 0; s < KS; ++s) k[t][s] = load16_stream(K + w[t] + (unsigned)min(2 * s + (kg >> 1), D / 16 - 1) * slab + n * 16u + (kg & 1) * 8u);
 #pragma unroll
         for (int u = 0; u < UN; ++u) {
             const int e = lane + 64 * u, t = PG % 64 == 0 ? (64 * u) / PG : e >= PG, i = e - t * PG;
-            v[u] = load16_stream(V + (t ? w[1].at : w[0].at) + (unsigned)(i >> 5) * slab + (i & 31) * 8u);
+            v[u] = load16_stream(V + (t ? w[1] : w[0]) + (unsigned)(i >> 5) * slab + (i & 31) * 8u);
         }
         __builtin_amdgcn_sched_barrier(0);
     }
@@ -289,7 +278,7 @@ struct TaRow {
 #pragma unroll
         for (int u = 0; u < UN; ++u) {
             const int e = lane + 64 * u, t = PG % 64 == 0 ? (64 * u) / PG : e >= PG, i = e - t * PG;
-            const bool ok = (t ? good[1] : good[0]) && row * kTaRow + 16 * t + ((i >> 1) & 15) < end;
+            const bool ok = row * kTaRow + 16 * t + ((i >> 1) & 15) < end;
             *reinterpret_cast<u32x4 *>(vt + e * 16) = ok ? v[u] : u32x4{0u, 0u, 0u, 0u};
         }
     }
@@ -341,19 +330,19 @@ __device__ __forceinline__ void ta_alone(const TreeAttention &P, const TreeItem 
         for (int t = row * kTaRow; t < min(row * kTaRow + kTaRow, it.t1); ++t) {
             const int node = t - it.len;
             if (node >= 0 && !((mask[node >> 5] >> (node & 31)) & 1)) continue;        // (uniform)
-            int page, in16;
-            pages.look(t >> 4, page, in16);
-            const TaPlace w = pages.place(page, in16);
+            const TaPick pick = pages.pick(t >> 4);
+            const size_t w = pages.place(pick);
+            const bool good = (unsigned)pick.page < (unsigned)pages.n_pages;
             const unsigned in = (unsigned)(t & 15) * 16u;
             float s = 0.f;
 #pragma unroll
-            for (int e = 0; e < NE; ++e) s = lane + 64 * e < D ? fmaf(qs[e], __half2float(K[w.at + at[e] + in]), s) : s;
-            s = w.good ? wave_sum(s) * scale : NAN;
+            for (int e = 0; e < NE; ++e) s = lane + 64 * e < D ? fmaf(qs[e], __half2float(K[w + at[e] + in]), s) : s;
+            s = good ? wave_sum(s) * scale : NAN;
             const float mn = fmaxf(m, s), corr = __builtin_amdgcn_exp2f(m - mn), p = __builtin_amdgcn_exp2f(s - (mn - kTaUp));
             m = mn;
             l = l * corr + p;
 #pragma unroll
-            for (int e = 0; e < NE; ++e) o[e] = fmaf(p, w.good ? __half2float(V[w.at + at[e] + in]) : 0.f, o[e] * corr);
+            for (int e = 0; e < NE; ++e) o[e] = fmaf(p, good ? __half2float(V[w + at[e] + in]) : 0.f, o[e] * corr);
         }
     }
 #pragma unroll
@@ -542,18 +531,13 @@ struct TaQuery {
 };
 
 // A query tile's 16 rows and 32 positions, scores of this lane: row lane % 16, positions 4 (lane / 16) .. + 3 of both granules.
-// What a row does not see is minus infinity, what lies in no page of the pool no number.  window: which positions the row sees, where `masked`
-__device__ __forceinline__ void ta_mask(f32x4 (&S)[2], bool masked, const bool (&good)[2], unsigned window, int kg)
+// What a row does not see is minus infinity.  window: which positions the row sees
+__device__ __forceinline__ void ta_mask(f32x4 (&S)[2], unsigned window, int kg)
 {
-    if (masked) {
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
+    for (int t = 0; t < 2; ++t)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float s = good[t] ? S[t][e] : NAN;
-                S[t][e] = (window >> (16 * t + 4 * kg + e)) & 1 ? s : -INFINITY;
-            }
-    }
+        for (int e = 0; e < 4; ++e) S[t][e] = (window >> (16 * t + 4 * kg + e)) & 1 ? S[t][e] : -INFINITY;
 }
 // The sums so far to a new reference, where a score is 2^kTaSlack above the one that the weights are relative to; the reference is the same in the four
 // lanes of a row.  L: sums of the weights, in every element.
@@ -621,8 +605,12 @@ __device__ __forceinline__ void ta_narrow(const TreeAttention &P, const TreePlan
     TaRow<D> r[AHEAD];
     const int row0 = it.t0 / kTaRow + wave;
 #pragma unroll
-    for (int a = 0; a < AHEAD; ++a) r[a].request(w.K, w.V, w.pages, w.slab, w.pages.pick(row0 + a * W), lane);
-    TaPick next = w.pages.pick(row0 + AHEAD * W);
+    for (int a = 0; a < AHEAD; ++a) {
+        const TaPick at[2] = {w.pages.pick(2 * (row0 + a * W)), w.pages.pick(2 * (row0 + a * W) + 1)};
+        r[a].request(w.K, w.V, w.pages, w.slab, at, lane);
+    }
+    TaPick next[2] = {w.pages.pick(2 * (row0 + AHEAD * W)), w.pages.pick(2 * (row0 + AHEAD * W) + 1)};
+    const bool bad = w.pages.bad(it.t0 >> 4, lane);
     const bool tail = it.t1 > it.len;
     if (tail) w.masks(P, smask);
     TaQuery<D, STACK> Q[QT];
@@ -657,16 +645,14 @@ __device__ __forceinline__ void ta_narrow(const TreeAttention &P, const TreePlan
                 for (int j = 0; j < QT; ++j) S[j][t] = Q[j].score(k, s, S[j][t]);
             }
         }
-        const bool good[2] = {r.good[0], r.good[1]};
         r.request(w.K, w.V, w.pages, w.slab, next, lane);
-        next = w.pages.pick(row + (AHEAD + 1) * W);
-        const bool masked = row * kTaRow + kTaRow > it.len || !good[0] || !good[1];    // (uniform)
+        next[0] = w.pages.pick(2 * (row + (AHEAD + 1) * W));
+        next[1] = w.pages.pick(2 * (row + (AHEAD + 1) * W) + 1);
+        const bool masked = row * kTaRow + kTaRow > it.len;                // (uniform)
         ta_f16x8 ph[QT], pl[QT];                           // element 4 t + e: position 16 t + 4 kg + e
 #pragma unroll
         for (int j = 0; j < QT; ++j) {
-            unsigned window = ~0u;
-            if (masked) window = ta_window(smask[16 * j + col], words, row * kTaRow, it.len, it.nodes);
-            ta_mask(S[j], masked, good, window, kg);
+            if (masked) ta_mask(S[j], ta_window(smask[16 * j + col], words, row * kTaRow, it.len, it.nodes), kg);
             ta_rise(S[j], scale, m_run[j], sum[j], O[j]);
             ta_weights(S[j], scale, m_run[j], ph[j], pl[j]);
             sum[j] = ta_total(ph[j], pl[j], sum[j]);
@@ -694,7 +680,7 @@ __device__ __forceinline__ void ta_narrow(const TreeAttention &P, const TreePlan
     for (int j = 0; j < QT; ++j) {
         const int at = wave * TR + 16 * j;
         const float l = sum[j][0];
-        bool finite = fabsf(l) < INFINITY;
+        bool finite = fabsf(l) < INFINITY && !bad;
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
 #pragma unroll
@@ -762,12 +748,9 @@ __device__ __forceinline__ void ta_wide(const TreeAttention &P, const TreePlanLa
     const __half *half = wave < 2 ? w.K : w.V;
     const int mine = wave & 1, last_n = (it.t1 - 1) & 15;
     const unsigned base = lds_address(mem);
-    unsigned goods = 0;                                    // bits 2 i, 2 i + 1: the granules of the ring's row i lie in pages of the pool
     auto request = [&](int row, int at, const TaPick &pick) {
-        const TaPlace p0 = w.pages.place(pick, 0), p1 = w.pages.place(pick, 1), p = mine ? p1 : p0;
-        goods = (goods & ~(3u << (2 * at))) | ((unsigned)p0.good | (unsigned)p1.good << 1) << (2 * at);
         const int n = min((lane & 31) >> 1, 2 * row + mine < w.pages.last ? 15 : last_n);
-        const i32x4 rsrc = dma_rsrc(half + p.at, 0x7fffffffu);
+        const i32x4 rsrc = dma_rsrc(half + w.pages.place(pick), 0x7fffffffu);
         const unsigned to = base + at * Lds::row + wave * Lds::granule;
 #pragma unroll
         for (int u = 0; u < Lds::loads; ++u) {
@@ -777,8 +760,9 @@ __device__ __forceinline__ void ta_wide(const TreeAttention &P, const TreePlanLa
     };
     const int first = it.t0 / kTaRow;
 #pragma unroll
-    for (int a = 0; a < kTwRing - 1; ++a) request(first + a, a, w.pages.pick(first + a));
-    TaPick next = w.pages.pick(first + kTwRing - 1);
+    for (int a = 0; a < kTwRing - 1; ++a) request(first + a, a, w.pages.pick(2 * (first + a) + mine));
+    TaPick next = w.pages.pick(2 * (first + kTwRing - 1) + mine);
+    const bool bad = w.pages.bad(it.t0 >> 4, lane);
     if (it.t1 > it.len) w.masks(P, smask);
     TaQuery<D, STACK> Q[QT];
 #pragma unroll
@@ -830,17 +814,13 @@ __device__ __forceinline__ void ta_wide(const TreeAttention &P, const TreePlanLa
         const int ahead = (at + 1) % kTwRing;
         tw_arrive<(kTwRing - 3) * Lds::loads>();           // (the next row is here)
         keys(ahead);
-        const unsigned good = (goods >> (2 * at)) & 3;
         request(row + kTwRing - 1, (at + kTwRing - 1) % kTwRing, next);    // (the place of the row before this one, which everyone has read)
-        next = w.pages.pick(row + kTwRing);
+        next = w.pages.pick(2 * (row + kTwRing) + mine);
         const char *vb = mem + at * Lds::row + 2 * Lds::granule;
-        const bool two[2] = {(good & 1) != 0, (good & 2) != 0};
-        const bool masked = row * kTaRow + kTaRow > it.len || good != 3;
+        const bool masked = row * kTaRow + kTaRow > it.len;                // (uniform)
 #pragma unroll
         for (int j = 0; j < QT; ++j) {
-            unsigned window = ~0u;
-            if (masked) window = ta_window(smask[wave * RW + 16 * j + col], words, row * kTaRow, it.len, it.nodes);
-            ta_mask(S[j], masked, two, window, kg);
+            if (masked) ta_mask(S[j], ta_window(smask[wave * RW + 16 * j + col], words, row * kTaRow, it.len, it.nodes), kg);
             ta_rise(S[j], scale, m_run[j], sum[j], O[j]);
         }
         f32x4 ahead_S[QT][2];
@@ -878,7 +858,7 @@ __device__ __forceinline__ void ta_wide(const TreeAttention &P, const TreePlanLa
     for (int j = 0; j < QT; ++j) {
         const int i = wave * RW + 16 * j + col;
         float l = sum[j][0];
-        bool finite = fabsf(l) < INFINITY;
+        bool finite = fabsf(l) < INFINITY && !bad;
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
