@@ -228,17 +228,17 @@ struct TaPages {
         p = __builtin_amdgcn_readfirstlane(p);
         return TaPick{reinterpret_cast<const __attribute__((address_space(4))) int *>(reinterpret_cast<uintptr_t>(table))[p], g - p * page16};
     }
-    // elements into the K or V half of the pool; an entry outside of it is read as the last page (bad() tells)
+    // elements into the K or V half of the pool; an entry outside of it is read as the last page (largest() tells)
     __device__ __forceinline__ size_t place(const TaPick &k) const
     {
         return (size_t)min((unsigned)k.page, (unsigned)n_pages - 1u) * per_page + head + (size_t)k.in * 256;
     }
-    // whether an entry of the granules first .. last lies outside the pool (the same in all lanes)
-    __device__ __forceinline__ bool bad(int first, int lane) const
+    // the largest of this lane's entries of the granules first .. last: n_pages or more where one lies outside the pool
+    __device__ __forceinline__ unsigned largest(int first, int lane) const
     {
-        bool b = false;
-        for (int p = first / page16 + lane; p <= last / page16; p += 64) b = b || (unsigned)table[p] >= (unsigned)n_pages;
-        return __any(b);
+        unsigned most = 0;
+        for (int p = first / page16 + lane; p <= last / page16; p += 64) most = max(most, (unsigned)table[p]);
+        return most;
     }
 };
 
@@ -309,40 +309,68 @@ __device__ __forceinline__ unsigned ta_window(const unsigned *words, int n_words
     return __funnelshift_r(word(w), word(w + 1), sh);
 }
 
-// One wavefront, one query row: its sums over rows row0, row0 + STEP .. of the piece in fp32, position by position, unseen ones left out
+// One wavefront, one query row: its sums over rows row0, row0 + STEP .. of the piece in fp32, unseen positions left out: a lane has a position and half
+// of the dimensions for the scores, then the lanes have the dimensions
 template <int D, int STEP, class T>
 __device__ __forceinline__ void ta_alone(const TreeAttention &P, const TreeItem &it, const TaPages &pages, const __half *K, const __half *V, const unsigned *mask,
                                          const T *q, int row0, int lane, float *o_out, float *m_out, float *l_out)
 {
-    constexpr int NE = (D + 63) / 64;
+    constexpr int NE = (D + 63) / 64, NS = D / 16, AT = 8;
     const float scale = 1.44269504088896340736f / sqrtf((float)D);
     const unsigned slab = (unsigned)P.pg.page * 16u;
-    float qs[NE], o[NE], m = kTaLowest, l = 0.f;
+    const int n = lane & 15, t1 = (lane >> 4) & 1, upper = lane >> 5;      // position 16 t1 + n of the row; slabs of the upper half
+    float o[NE], m = kTaLowest, l = 0.f;
     unsigned at[NE];
 #pragma unroll
     for (int e = 0; e < NE; ++e) {
         const int dim = min(lane + 64 * e, D - 1);
         at[e] = (unsigned)(dim >> 4) * slab + (dim & 15);
-        qs[e] = lane + 64 * e < D ? (float)q[dim] : 0.f;
         o[e] = 0.f;
     }
     for (int row = row0; row * kTaRow < it.t1; row += STEP) {
-        for (int t = row * kTaRow; t < min(row * kTaRow + kTaRow, it.t1); ++t) {
-            const int node = t - it.len;
-            if (node >= 0 && !((mask[node >> 5] >> (node & 31)) & 1)) continue;        // (uniform)
-            const TaPick pick = pages.pick(t >> 4);
-            const size_t w = pages.place(pick);
-            const bool good = (unsigned)pick.page < (unsigned)pages.n_pages;
-            const unsigned in = (unsigned)(t & 15) * 16u;
-            float s = 0.f;
+        const int t = row * kTaRow + (lane & 31), node = t - it.len;
+        const bool sees = t < it.t1 && (node < 0 || ((mask[max(node, 0) >> 5] >> (node & 31)) & 1));
+        const unsigned long long seen = __ballot(sees);
+        if (!seen) continue;                               // (uniform)
+        const TaPick pick[2] = {pages.pick(2 * row), pages.pick(2 * row + 1)};
+        const size_t w[2] = {pages.place(pick[0]), pages.place(pick[1])};
+        const bool good[2] = {(unsigned)pick[0].page < (unsigned)pages.n_pages, (unsigned)pick[1].page < (unsigned)pages.n_pages};
+        const __half *k = K + (t1 ? w[1] : w[0]) + n * 16;
+        float s = 0.f;
+        for (int sl = upper * ((NS + 1) / 2); sl < (upper ? NS : (NS + 1) / 2); ++sl)
 #pragma unroll
-            for (int e = 0; e < NE; ++e) s = lane + 64 * e < D ? fmaf(qs[e], __half2float(K[w + at[e] + in]), s) : s;
-            s = good ? wave_sum(s) * scale : NAN;
-            const float mn = fmaxf(m, s), corr = __builtin_amdgcn_exp2f(m - mn), p = __builtin_amdgcn_exp2f(s - (mn - kTaUp));
-            m = mn;
-            l = l * corr + p;
+            for (int h = 0; h < 2; ++h) {
+                const u32x4 x = load16(k + (unsigned)sl * slab + h * 8);
 #pragma unroll
-            for (int e = 0; e < NE; ++e) o[e] = fmaf(p, good ? __half2float(V[w + at[e] + in]) : 0.f, o[e] * corr);
+                for (int e = 0; e < 4; ++e) {
+                    const float2 f = unpack_h2(x[e]);
+                    s = fmaf((float)q[sl * 16 + h * 8 + 2 * e], f.x, s);
+                    s = fmaf((float)q[sl * 16 + h * 8 + 2 * e + 1], f.y, s);
+                }
+            }
+        s += __shfl_xor(s, 32, 64);
+        s = !sees ? -INFINITY : (t1 ? good[1] : good[0]) ? s * scale : NAN;
+        const float mn = fmaxf(m, wave_max(s)), corr = __builtin_amdgcn_exp2f(m - mn), p = sees ? __builtin_amdgcn_exp2f(s - (mn - kTaUp)) : 0.f;
+        m = mn;
+        l = l * corr + wave_sum(upper ? 0.f : p);
+#pragma unroll
+        for (int e = 0; e < NE; ++e) o[e] *= corr;
+#pragma unroll 1
+        for (int i0 = 0; i0 < kTaRow; i0 += AT) {
+            const __half *v = V + (i0 < 16 ? w[0] : w[1]) + (i0 & 15) * 16;
+            const bool ok = i0 < 16 ? good[0] : good[1];
+            float x[AT][NE];
+#pragma unroll
+            for (int i = 0; i < AT; ++i)
+#pragma unroll
+                for (int e = 0; e < NE; ++e) x[i][e] = __half2float(v[at[e] + i * 16u]);
+#pragma unroll
+            for (int i = 0; i < AT; ++i) {
+                const float pi = readlane_f(p, i0 + i);
+                if ((seen >> (i0 + i)) & 1)                // (uniform)
+#pragma unroll
+                    for (int e = 0; e < NE; ++e) o[e] = fmaf(pi, ok ? x[i][e] : 0.f, o[e]);
+            }
         }
     }
 #pragma unroll
@@ -610,7 +638,7 @@ __device__ __forceinline__ void ta_narrow(const TreeAttention &P, const TreePlan
         r[a].request(w.K, w.V, w.pages, w.slab, at, lane);
     }
     TaPick next[2] = {w.pages.pick(2 * (row0 + AHEAD * W)), w.pages.pick(2 * (row0 + AHEAD * W) + 1)};
-    const bool bad = w.pages.bad(it.t0 >> 4, lane);
+    const unsigned entries = w.pages.largest(it.t0 >> 4, lane);
     const bool tail = it.t1 > it.len;
     if (tail) w.masks(P, smask);
     TaQuery<D, STACK> Q[QT];
@@ -675,16 +703,20 @@ __device__ __forceinline__ void ta_narrow(const TreeAttention &P, const TreePlan
             if ((row + a * W) * kTaRow < it.t1) step(r[a], row + a * W);               // (uniform)
     // The wavefronts' sums: [wave][row][D], maxima and weights [wave][row], in the place of V
     float *wp = reinterpret_cast<float *>(mem), *wm = wp + W * TR * D, *wl = wm + W * TR;
+    const bool bad = __any(entries >= (unsigned)w.pages.n_pages);
     __syncthreads();                                       // V has been read
 #pragma unroll
     for (int j = 0; j < QT; ++j) {
         const int at = wave * TR + 16 * j;
         const float l = sum[j][0];
-        bool finite = fabsf(l) < INFINITY && !bad;
+        // A sum of weights that is no number is the answer: a score that the row sees is none, or plus infinity.  (But queries in 32 bits meet an infinite
+        // key in two parts, of which one may be zero.)
+        const bool none = !STACK && l != l;
+        bool finite = (STACK ? fabsf(l) < INFINITY : true) && !bad;
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) finite = finite && fabsf(O[j][t][e]) < INFINITY;
+            for (int e = 0; e < 4; ++e) finite = finite && (none || fabsf(O[j][t][e]) < INFINITY);
             *reinterpret_cast<f32x4 *>(wp + (at + col) * D + 16 * t + 4 * kg) = O[j][t];
         }
         if (kg == 0) { wm[at + col] = m_run[j]; wl[at + col] = l; }
@@ -759,10 +791,10 @@ __device__ __forceinline__ void ta_wide(const TreeAttention &P, const TreePlanLa
         }
     };
     const int first = it.t0 / kTaRow;
+    const bool bad = __any(w.pages.largest(it.t0 >> 4, lane) >= (unsigned)w.pages.n_pages);
 #pragma unroll
     for (int a = 0; a < kTwRing - 1; ++a) request(first + a, a, w.pages.pick(2 * (first + a) + mine));
     TaPick next = w.pages.pick(2 * (first + kTwRing - 1) + mine);
-    const bool bad = w.pages.bad(it.t0 >> 4, lane);
     if (it.t1 > it.len) w.masks(P, smask);
     TaQuery<D, STACK> Q[QT];
 #pragma unroll
@@ -858,11 +890,14 @@ __device__ __forceinline__ void ta_wide(const TreeAttention &P, const TreePlanLa
     for (int j = 0; j < QT; ++j) {
         const int i = wave * RW + 16 * j + col;
         float l = sum[j][0];
-        bool finite = fabsf(l) < INFINITY && !bad;
+        // A sum of weights that is no number is the answer: a score that the row sees is none, or plus infinity.  (But queries in 32 bits meet an infinite
+        // key in two parts, of which one may be zero.)
+        const bool none = !STACK && l != l;
+        bool finite = (STACK ? fabsf(l) < INFINITY : true) && !bad;
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) finite = finite && fabsf(O[j][t][e]) < INFINITY;
+            for (int e = 0; e < 4; ++e) finite = finite && (none || fabsf(O[j][t][e]) < INFINITY);
         const unsigned long long again = __ballot(!finite);
         if (again) {                                       // (uniform) rows worked out once more, through LDS that no one needs now
             float *o = reinterpret_cast<float *>(mem) + wave * 16 * (D + 2);
