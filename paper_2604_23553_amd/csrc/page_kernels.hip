@@ -11,13 +11,15 @@ namespace cfpp {
 // target_r = ceil((len_r + count_r) / page); a request takes target - held pages from the end of the free list or gives back
 // held - target.  Three running sums over the requests (pages taken, pages given back, rows) say which entry of the free list and
 // which rows are whose.  One workgroup has all requests: every sum needs all of the ones before it, and 4096 requests are four to a thread.
-constexpr int kTablesThreads = 1024, kTablesEach = kTreeMaxRequests / kTablesThreads;
+constexpr int kTablesEach = 4;           // requests of a thread
+constexpr int kTablesRows = 4096;        // rows whose slots it writes itself
 constexpr int kSumMost = 1 << 28;      // sums stop here: more than any pool's pages or batch's rows, and two of them still fit 32 bits
 
 __device__ __forceinline__ int add_most(int a, int b) { return min(a + b, kSumMost); }
 
 // Running sums of three values a thread over the workgroup; v: this thread's, on return the sums of the threads before it.
-__device__ __forceinline__ void block_sums(int (&v)[3], int (*part)[kTablesThreads / 64], int tid)
+template <int WAVES>
+__device__ __forceinline__ void block_sums(int (&v)[3], int (*part)[WAVES], int tid)
 {
     const int lane = tid & 63, wave = tid >> 6;
     int own[3];
@@ -59,9 +61,11 @@ __device__ __forceinline__ int slot_of(const TablesParams &P, int r, int at)
     return P.b.table[(size_t)r * P.b.stride + at / P.pg.page] * P.pg.page + at % P.pg.page;
 }
 
-__global__ void __launch_bounds__(kTablesThreads) k_page_tables(TablesParams P)
+template <int THREADS, bool SLOTS>
+__global__ void __launch_bounds__(THREADS) k_page_tables(TablesParams P)
 {
-    __shared__ int taken[kTreeMaxRequests], given[kTreeMaxRequests], rows[kTreeMaxRequests], part[3][kTablesThreads / 64];
+    constexpr int MOST = THREADS * kTablesEach;
+    __shared__ int taken[MOST], given[MOST], rows[MOST], part[3][THREADS / 64];
     const int R = P.b.requests, tid = threadIdx.x;
     const int F = max(0, min(*P.free_count, P.pg.n_pages));
     int target[kTablesEach], held[kTablesEach], sum[3] = {0, 0, 0};
@@ -83,7 +87,7 @@ __global__ void __launch_bounds__(kTablesThreads) k_page_tables(TablesParams P)
         }
         sum[2] = add_most(sum[2], count[k]);
     }
-    block_sums(sum, part, tid);
+    block_sums<THREADS / 64>(sum, part, tid);
     int row = sum[2];
     sum[0] = sum[1] = sum[2] = 0;
 #pragma unroll
@@ -99,7 +103,7 @@ __global__ void __launch_bounds__(kTablesThreads) k_page_tables(TablesParams P)
         sum[1] = add_most(sum[1], surplus[k]);
     }
     __syncthreads();                                       // part has been read
-    block_sums(sum, part, tid);
+    block_sums<THREADS / 64>(sum, part, tid);
     int before = sum[0], back = sum[1];
 #pragma unroll
     for (int k = 0; k < kTablesEach; ++k) {
@@ -128,20 +132,31 @@ __global__ void __launch_bounds__(kTablesThreads) k_page_tables(TablesParams P)
             else lo = mid + 1;
         }
         T = lo > 0 ? taken[lo - 1] : 0;
-        for (int i = tid; i < T; i += kTablesThreads) {
+        for (int i = tid; i < T; i += THREADS) {
             const int r = find_above(taken, lo, i), k = i - (r > 0 ? taken[r - 1] : 0);
             P.b.table[(size_t)r * P.b.stride + max(0, min(P.held[r], P.b.stride)) + k] = P.free_pages[F - 1 - i];
         }
     }
     __syncthreads();                                       // every taken entry of the list has been read
     const int G = R > 0 ? given[R - 1] : 0;
-    for (int i = tid; i < G; i += kTablesThreads) {
+    for (int i = tid; i < G; i += THREADS) {
         const int r = find_above(given, R, i), first = r > 0 ? given[r - 1] : 0, n = given[r] - first;
         int *entry = P.b.table + (size_t)r * P.b.stride + max(0, min(P.held[r], P.b.stride)) - n + (i - first);
         if (F - T + i < P.pg.n_pages) P.free_pages[F - T + i] = *entry;
         *entry = -1;
     }
-    __syncthreads();                                       // held has been read
+    __syncthreads();                                       // held has been read, the block tables are written
+    if constexpr (SLOTS) {
+        for (int i = tid; i < P.b.max_rows; i += THREADS) {
+            int slot = -1;
+            if (i < rows[R - 1]) {
+                const int r = find_above(rows, R, i);
+                // (a request is granted what it asks for or nothing)
+                if (P.granted[r]) slot = slot_of(P, r, P.b.lens[r] + i - (r > 0 ? rows[r - 1] : 0));
+            }
+            P.b.slots[i] = slot;
+        }
+    }
 #pragma unroll
     for (int k = 0; k < kTablesEach; ++k) {
         const int r = tid * kTablesEach + k;
@@ -165,14 +180,21 @@ __global__ void __launch_bounds__(256) k_page_slots(TablesParams P)
 
 hipError_t launch_page_tables(const TablesParams &P, hipStream_t s)
 {
-    hipLaunchKernelGGL(k_page_tables, dim3(1), dim3(kTablesThreads), 0, s, P);
+    const bool few = P.b.requests <= 256 * kTablesEach;
+    if (P.b.max_rows <= kTablesRows) {
+        if (few) hipLaunchKernelGGL((k_page_tables<256, true>), dim3(1), dim3(256), 0, s, P);
+        else hipLaunchKernelGGL((k_page_tables<1024, true>), dim3(1), dim3(1024), 0, s, P);
+        return hipGetLastError();
+    }
+    if (few) hipLaunchKernelGGL((k_page_tables<256, false>), dim3(1), dim3(256), 0, s, P);
+    else hipLaunchKernelGGL((k_page_tables<1024, false>), dim3(1), dim3(1024), 0, s, P);
     hipLaunchKernelGGL(k_page_slots, dim3(P.b.requests + 1), dim3(256), 0, s, P);
     return hipGetLastError();
 }
 
 // ---- append ------------------------------------------------------------------------------------
-// 16 bytes a thread.  Rows [row][head][d]: neighbouring threads have neighbouring pieces of a row, whole lines are read and records of 32 bytes
-// written.  `from`: where the pieces of K and V rows lie.
+// A wavefront has 8 rows and 128 bytes of each, 16 to a lane: whole lines are read, and where the rows' slots follow one another 256 bytes in a
+// run are written.  `from`: where the pieces of K and V rows lie.
 struct AppendFrom {
     const __half *k, *v;
     long long row, head;       // halves from row to row, from head to head
@@ -180,25 +202,23 @@ struct AppendFrom {
 };
 __global__ void __launch_bounds__(256) k_page_append(PageDims pg, __half *pool, AppendFrom from, const int *slots, int n_rows)
 {
-    const int d8 = pg.d / 8, per = pg.heads * d8;
-    const long long n = 2LL * n_rows * per;
-    const size_t which = page_which_elems(pg);
-    for (long long i = blockIdx.x * 256LL + threadIdx.x; i < n; i += gridDim.x * 256LL) {
-        const long long rw = i / per;
-        const int piece = (int)(i - rw * per), row = (int)(rw >> 1), w = (int)(rw & 1);
-        const int slot = slots[row];
-        if (slot < 0 || slot >= pg.n_pages * pg.page) continue;
-        const int page = slot / pg.page, at = slot - page * pg.page, head = piece / d8, pc = piece - head * d8;
-        const u32x4 x = load16((w ? from.v : from.k) + row * from.row + head * from.head + (long long)(pc >> 1) * from.slab + (pc & 1) * 8);
-        __half *to = pool + w * which + ((size_t)page * pg.heads + head) * page_head_elems(pg) + ((size_t)(pc >> 1) * pg.page + at) * 16 + (pc & 1) * 8;
-        *as_global(reinterpret_cast<u32x4 *>(to)) = x;
-    }
+    const int d8 = pg.d / 8, per = pg.heads * d8, groups = (per + 7) / 8, lane = threadIdx.x & 63;
+    const long long unit = blockIdx.x * 4LL + (threadIdx.x >> 6);
+    const int set = (int)(unit / (2 * groups)), g = (int)(unit - (long long)set * (2 * groups)), w = g >= groups;
+    const int row = set * 8 + (lane >> 3), piece = (g - w * groups) * 8 + (lane & 7);
+    if (row >= n_rows || piece >= per) return;
+    const int slot = slots[row];
+    const int page = slot / pg.page, at = slot - page * pg.page, head = piece / d8, pc = piece - head * d8;
+    const u32x4 x = load16((w ? from.v : from.k) + row * from.row + head * from.head + (long long)(pc >> 1) * from.slab + (pc & 1) * 8);
+    if (slot < 0 || slot >= pg.n_pages * pg.page) return;
+    __half *to = pool + w * page_which_elems(pg) + ((size_t)page * pg.heads + head) * page_head_elems(pg) + ((size_t)(pc >> 1) * pg.page + at) * 16 + (pc & 1) * 8;
+    *as_global(reinterpret_cast<u32x4 *>(to)) = x;
 }
 
 static hipError_t append(const PageDims &pg, __half *pool, const AppendFrom &from, const int *slots, int n_rows, hipStream_t s)
 {
-    const long long n = 2LL * n_rows * (pg.heads * pg.d / 8), wgs = (n + 255) / 256;
-    hipLaunchKernelGGL(k_page_append, dim3((unsigned)(wgs < 8192 ? wgs : 8192)), dim3(256), 0, s, pg, pool, from, slots, n_rows);
+    const long long units = (long long)((n_rows + 7) / 8) * 2 * ((pg.heads * (pg.d / 8) + 7) / 8);
+    hipLaunchKernelGGL(k_page_append, dim3((unsigned)((units + 3) / 4)), dim3(256), 0, s, pg, pool, from, slots, n_rows);
     return hipGetLastError();
 }
 hipError_t launch_page_append(const PageDims &pg, __half *pool, const __half *k, const __half *v, long long row_stride, const int *slots,
@@ -292,7 +312,7 @@ __global__ void __launch_bounds__(256) k_tree_accept(AcceptParams P, int n_layer
         const int page = sl / P.pg.page, off = sl - page * P.pg.page, head = piece / (P.pg.d / 8), pc = piece - head * (P.pg.d / 8);
         return as_global(reinterpret_cast<u32x4 *>(pool + ((size_t)page * P.pg.heads + head) * page_head_elems(P.pg) + ((size_t)(pc >> 1) * P.pg.page + off) * 16 + (pc & 1) * 8));
     };
-    constexpr int EACH = 4;
+    constexpr int EACH = 8;
     for (int i0 = 0; i0 < total; i0 += 256 * EACH) {
         u32x4 x[EACH];
         bool moves[EACH];
