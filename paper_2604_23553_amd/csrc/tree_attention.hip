@@ -108,7 +108,8 @@ __device__ __forceinline__ void tree_masks(const PageDims &pg, const TreeBatch &
 // wavefronts take at a time, so that all pieces come to about `want`.
 __device__ __forceinline__ void tree_work(const PageDims &pg, const TreeBatch &b, int group, const TreePlanLayout &L, char *plan)
 {
-    __shared__ int items[kTreeMaxRequests], multi[kTreeMaxRequests], tiles[kTreeMaxRequests];     // running sums
+    extern __shared__ int tp_sums[];                       // running sums, [3][requests]
+    int *items = tp_sums, *multi = tp_sums + b.requests, *tiles = tp_sums + 2 * b.requests;
     __shared__ int wave_part[3][kTaWaves], cuts;
     if (threadIdx.x == 0) cuts = 0;
     __shared__ long long wave_total[kTaWaves];
@@ -173,8 +174,9 @@ __device__ __forceinline__ void tree_work(const PageDims &pg, const TreeBatch &b
         }
         const int r = a, t0 = r > 0 ? tiles[r - 1] : 0, n_tiles = tiles[r] - t0, at = i - (r > 0 ? items[r - 1] : 0);
         TreeItem it;
-        it.request = r;
-        it.nodes = tree_rows(pg, b, r, it.first);
+        it.request = r;                                    // (one that takes part: it has items)
+        it.first = b.row_start[r];
+        it.nodes = b.row_start[r + 1] - it.first;
         it.len = b.lens[r];
         it.pieces = (items[r] - (r > 0 ? items[r - 1] : 0)) / n_tiles;
         it.piece = at / n_tiles;                           // (the tiles of a piece follow one another: they read the same rows)
@@ -204,7 +206,7 @@ __global__ void __launch_bounds__(kTaThreads) k_tree_plan(PageDims pg, TreeBatch
 hipError_t launch_tree_plan(const PageDims &pg, const TreeBatch &b, int n_heads, char *plan, hipStream_t s)
 {
     const TreePlanLayout L = tree_plan_layout(pg, n_heads, b.requests, b.max_rows, b.max_nodes, b.stride);
-    hipLaunchKernelGGL(k_tree_plan, dim3(b.requests + 1), dim3(kTaThreads), 0, s, pg, b, n_heads / pg.heads, L, plan);
+    hipLaunchKernelGGL(k_tree_plan, dim3(b.requests + 1), dim3(kTaThreads), 3 * b.requests * sizeof(int), s, pg, b, n_heads / pg.heads, L, plan);
     return hipGetLastError();
 }
 
@@ -954,41 +956,45 @@ __global__ void __launch_bounds__(kTaThreads, 2) k_tree_attention(TreeAttention 
         if (w.it.pieces > 1) ta_join<D, STACK>(P, L, plan, w.it, P.pg.heads, w.head, w.rows, &last_one);
 }
 
-// The pieces of many query rows are added by a launch of its own, 1024 sums to a workgroup: for one workgroup they are up to 16384.
+// The pieces of many query rows are added by a launch of its own, 1024 sums to a workgroup at a time: for one workgroup they are up to 16384.
+constexpr int kTaJoinWgs = 1024;
 template <int D, int TQ, bool STACK>
 __global__ void __launch_bounds__(kTaThreads) k_tree_join(TreeAttention P, TreePlanLayout L, const char *plan)
 {
     constexpr int D4 = D / 4, CHUNKS = (TQ * D4 + kTaThreads - 1) / kTaThreads;
-    const int H = P.pg.heads, b = (int)blockIdx.x / CHUNKS, chunk = (int)blockIdx.x - b * CHUNKS, k = b / H, head = b - k * H;
+    const int H = P.pg.heads;
     const TreePlanHead &plan_head = *reinterpret_cast<const TreePlanHead *>(plan);
-    if (plan_head.key != L.key || k >= plan_head.cuts) return;
-    const TreeItem it = reinterpret_cast<const TreeItem *>(plan + L.items)[reinterpret_cast<const int *>(plan + L.cut)[k]];
-    const int e = chunk * kTaThreads + (int)threadIdx.x, i = e / D4, dim = 4 * (e - i * D4);
-    if (i >= min(TQ, it.nodes * P.group - it.tile * TQ)) return;
+    if (plan_head.key != L.key) return;
     const size_t step = (size_t)H * TQ * (D + 2);          // from piece to piece
-    const float *at = reinterpret_cast<const float *>(plan + L.sums) + ((size_t)it.slot * H + head) * (TQ * (D + 2));
-    float M = kTaLowest, l = 0.f;
-    f32x4 s = {0.f, 0.f, 0.f, 0.f};
-    constexpr int AT = 8;                                  // in flight together (past the last: the last again)
-    for (int z = 0; z < it.pieces; z += AT) {
-        float2 ml[AT];
-        f32x4 a[AT];
+    for (int unit = blockIdx.x; unit < plan_head.cuts * H * CHUNKS; unit += gridDim.x) {
+        const int b = unit / CHUNKS, chunk = unit - b * CHUNKS, k = b / H, head = b - k * H;
+        const TreeItem it = reinterpret_cast<const TreeItem *>(plan + L.items)[reinterpret_cast<const int *>(plan + L.cut)[k]];
+        const int e = chunk * kTaThreads + (int)threadIdx.x, i = e / D4, dim = 4 * (e - i * D4);
+        if (i >= min(TQ, it.nodes * P.group - it.tile * TQ)) continue;
+        const float *at = reinterpret_cast<const float *>(plan + L.sums) + ((size_t)it.slot * H + head) * (TQ * (D + 2));
+        float M = kTaLowest, l = 0.f;
+        f32x4 s = {0.f, 0.f, 0.f, 0.f};
+        constexpr int AT = 8;                              // in flight together (past the last: the last again)
+        for (int z = 0; z < it.pieces; z += AT) {
+            float2 ml[AT];
+            f32x4 a[AT];
 #pragma unroll
-        for (int u = 0; u < AT; ++u) {
-            const float *f = at + (size_t)min(z + u, it.pieces - 1) * step;
-            ml[u] = *reinterpret_cast<const float2 *>(f + TQ * D + 2 * i);
-            a[u] = *as_global(reinterpret_cast<const f32x4 *>(f + i * D + dim));
-        }
+            for (int u = 0; u < AT; ++u) {
+                const float *f = at + (size_t)min(z + u, it.pieces - 1) * step;
+                ml[u] = *reinterpret_cast<const float2 *>(f + TQ * D + 2 * i);
+                a[u] = *as_global(reinterpret_cast<const f32x4 *>(f + i * D + dim));
+            }
 #pragma unroll
-        for (int u = 0; u < AT; ++u) {
-            if (z + u >= it.pieces) continue;              // (uniform)
-            const float mn = fmaxf(M, ml[u].x), c0 = __builtin_amdgcn_exp2f(M - mn), c1 = __builtin_amdgcn_exp2f(ml[u].x - mn);
-            l = l * c0 + ml[u].y * c1;
-            s = s * c0 + a[u] * c1;
-            M = mn;
+            for (int u = 0; u < AT; ++u) {
+                if (z + u >= it.pieces) continue;          // (uniform)
+                const float mn = fmaxf(M, ml[u].x), c0 = __builtin_amdgcn_exp2f(M - mn), c1 = __builtin_amdgcn_exp2f(ml[u].x - mn);
+                l = l * c0 + ml[u].y * c1;
+                s = s * c0 + a[u] * c1;
+                M = mn;
+            }
         }
+        ta_deliver<D, STACK>(P, it, head, it.tile * TQ + i, dim, s, l);
     }
-    ta_deliver<D, STACK>(P, it, head, it.tile * TQ + i, dim, s, l);
 }
 
 template <int D, int TQ, bool STACK>
@@ -1001,8 +1007,7 @@ static hipError_t launch_tile(const TreeAttention &P, const TreePlanLayout &L, c
     }
     hipLaunchKernelGGL((k_tree_attention<D, TQ, STACK>), dim3((unsigned)L.work * P.pg.heads), dim3(kTaThreads), lds, s, P, L, plan);
     if constexpr (TQ > kTaLastJoins) {
-        constexpr int chunks = (TQ * D / 4 + kTaThreads - 1) / kTaThreads;
-        hipLaunchKernelGGL((k_tree_join<D, TQ, STACK>), dim3((unsigned)L.want * P.pg.heads * chunks), dim3(kTaThreads), 0, s, P, L, plan);
+        hipLaunchKernelGGL((k_tree_join<D, TQ, STACK>), dim3(kTaJoinWgs), dim3(kTaThreads), 0, s, P, L, plan);
     }
     return hipGetLastError();
 }
