@@ -404,7 +404,7 @@ typedef struct cfpp_tree_batch {
     int32_t n_requests;         /* 1 .. 4096                                               */
     int32_t max_rows;           /* rows that the arrays hold, 1 .. 2^20                    */
     int32_t max_nodes;          /* most nodes of a request, 1 .. 256                       */
-    int32_t table_stride;       /* entries of a request's block table; times page_len < 2^31 */
+    int32_t table_stride;       /* entries of a request's block table; times page_len at most 2^30 */
     const int32_t *lens;        /* [n_requests]                                            */
     int32_t *row_start;         /* [n_requests + 1]         written by cfpp_page_tables    */
     int32_t *block_table;       /* [n_requests][table_stride]  pages, by position / page_len */
@@ -473,8 +473,8 @@ cfpp_status cfpp_page_append(const cfpp_pages *pages, void *kv_pool, const void 
  *             elements, multiples of 8.  out must not overlap q
  *   n_heads : query heads; n_heads / n_kv_heads consecutive ones share a key head
  * Reads lens, row_start, block_table, masks and the plan, which must have been made with
- * the same pages, n_heads and batch sizes; uses the plan's memory, so calls with one
- * plan belong on one stream. */
+ * the same pages, n_heads and batch sizes (else nothing is written); uses the plan's
+ * memory, so calls with one plan belong on one stream. */
 cfpp_status cfpp_tree_attention(const cfpp_pages *pages, const void *kv_pool,
                                 const cfpp_tree_batch *batch, const void *q, int64_t q_stride,
                                 int32_t n_heads, void *out, int64_t out_stride, cfpp_stream stream);

@@ -1105,8 +1105,8 @@ static cfpp_status tree_batch(const cfpp_pages *p, const cfpp_tree_batch *b, Tre
     if (st != CFPP_OK) return st;
     if (!b) return fail(CFPP_EINVAL, "batch is NULL");
     if ((st = check_tree_sizes(b->n_requests, b->max_rows, b->max_nodes)) != CFPP_OK) return st;
-    if (b->table_stride <= 0 || (long long)b->table_stride * p->page_len > 0x7fffffffll)
-        return fail(CFPP_EINVAL, "table_stride %d: positive, and at most 2^31 - 1 positions", b->table_stride);
+    if (b->table_stride <= 0 || (long long)b->table_stride * p->page_len > 1ll << 30)
+        return fail(CFPP_EINVAL, "table_stride %d: positive, and at most 2^30 positions", b->table_stride);
     if (!aligned4(b->lens) || !aligned4(b->row_start)) return fail(CFPP_EINVAL, "lens or row_start is NULL or misaligned");
     t->requests = b->n_requests; t->max_rows = b->max_rows; t->max_nodes = b->max_nodes; t->stride = b->table_stride;
     t->lens = b->lens; t->row_start = b->row_start; t->table = b->block_table; t->slots = b->slots;

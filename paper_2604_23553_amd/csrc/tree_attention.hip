@@ -47,8 +47,8 @@ TreePlanLayout tree_plan_layout(const PageDims &pg, int n_heads, int requests, i
     size_t o = align_up(sizeof(TreePlanHead), 256);
     L.items = o; o = align_up(o + (size_t)L.work * sizeof(TreeItem), 256);
     L.cut = o; o = align_up(o + (size_t)L.want * sizeof(int), 256);
-    L.counters = o; o = align_up(o + (size_t)L.tiles * pg.heads * 4, 256);
-    // tiles of more than one piece have less than twice `want` of them in all
+    // tiles of more than one piece have less than twice `want` of them in all; the first one's number names the tile
+    L.counters = o; o = align_up(o + (size_t)2 * L.want * pg.heads * 4, 256);
     L.sums = o; o = align_up(o + (size_t)2 * L.want * pg.heads * L.tile_rows * (pg.d + 2) * 4, 256);
     L.total = o;
     // what the plan depends on, as one number
@@ -185,15 +185,14 @@ __device__ __forceinline__ void tree_work(const PageDims &pg, const TreeBatch &b
         const int x = it.len + it.nodes, size = piece_size(x, pieces_of(x));
         it.t0 = it.piece * size;
         it.t1 = min(x, it.t0 + size);
-        it.counter = t0 + it.tile;
         if (it.pieces > 1 && it.piece == 0) cut[atomicAdd(&cuts, 1)] = i;              // (at most want / 1.5; in any order)
-        it.pad = 0;
+        it.pad[0] = it.pad[1] = 0;
         list[i] = it;
     }
     __syncthreads();
     if (tid == 0) reinterpret_cast<TreePlanHead *>(plan)->cuts = cuts;
     unsigned *counters = reinterpret_cast<unsigned *>(plan + L.counters);
-    for (int i = tid; i < L.tiles * pg.heads; i += kTaThreads) counters[i] = 0u;
+    for (int i = tid; i < 2 * L.want * pg.heads; i += kTaThreads) counters[i] = 0u;
 }
 
 __global__ void __launch_bounds__(kTaThreads) k_tree_plan(PageDims pg, TreeBatch b, int group, TreePlanLayout L, char *plan)
@@ -441,7 +440,7 @@ __device__ __forceinline__ void ta_join(const TreeAttention &P, const TreePlanLa
 {
     constexpr int D4 = D / 4;
     const int tid = threadIdx.x;
-    unsigned *counter = reinterpret_cast<unsigned *>(plan + L.counters) + (size_t)it.counter * H + head;
+    unsigned *counter = reinterpret_cast<unsigned *>(plan + L.counters) + (size_t)it.slot * H + head;
     xwg_wait_stores();
     __syncthreads();
     if (tid == 0) *last_one = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (unsigned)it.pieces - 1;

@@ -45,11 +45,11 @@ hipError_t launch_tree_accept(const AcceptParams &P, int n_layers, hipStream_t s
 
 // ---- the attention and its plan --------------------------------------------------------------
 // Query rows (a node's heads that share a key head, nodes one after the other) go to workgroups in tiles of 16, 32, 64 or 128, positions in pieces.
-// A plan: the work list of a key head (TreeItem), an arrival counter for each tile and key head, and the sums of the pieces.
+// A plan: the work list of a key head (TreeItem), arrival counters and the sums of the tiles that are cut into pieces.
 struct TreeItem {
     int request, first, nodes, len;    // rows first .. first + nodes - 1 behind len cached positions
     int tile, piece, pieces, slot;     // slot: the tile's first place among the sums, one for each piece; -1 with a single piece
-    int t0, t1, counter, pad;          // positions; the tile's number
+    int t0, t1, pad[2];                // positions
 };
 struct TreePlanHead { int items, key, cuts, pad[13]; };       // cuts: tiles that have several pieces, listed behind the items
 struct TreePlanLayout {

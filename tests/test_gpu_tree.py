@@ -236,6 +236,21 @@ def test_requests_that_the_plan_leaves_out():
     s.check(got, requests=[0])
 
 
+def test_a_plan_without_slots_counts_every_request_and_one_of_other_sizes_writes_nothing():
+    rng = np.random.default_rng(18)
+    s = Step([30, 7], trees_of(rng, [5, 40]), (4, 2, 64)).to_gpu()
+    s.g["slots"].fill_(-1)
+    s.batch.slots = 0
+    s.run_plan()
+    s.check(s.attention())
+    s.g_out.fill_(7.0)
+    cf.cfpp_tree_attention(s.pages, s.g_pool[0], s.batch, s.g_q, s.H // 2 * 1, s.g_out, s.q_stride, s.out_stride, stream())   # (2 query heads)
+    s.batch.max_nodes -= 1
+    cf.cfpp_tree_attention(s.pages, s.g_pool[0], s.batch, s.g_q, s.H, s.g_out, s.q_stride, s.out_stride, stream())
+    torch.cuda.synchronize()
+    assert (s.g_out == 7.0).all()
+
+
 # ---- append ---------------------------------------------------------------------------------------------
 @pytest.mark.parametrize("heads,d,page,rows,pad", [(1, 64, 16, 1, 0), (3, 80, 48, 37, 8), (8, 128, 64, 300, 0), (32, 80, 16, 5, 5120)])
 def test_page_append(heads, d, page, rows, pad):
@@ -278,6 +293,20 @@ def test_tree_attention_behind_long_contexts(heads, lens, sizes, page):
     first = s.attention()
     s.check(first)
     assert np.array_equal(first.view(np.uint16), s.attention().view(np.uint16)), "the bits change from call to call"
+
+
+def test_a_page_outside_the_pool_that_only_some_nodes_see():
+    """A drafted node in a page outside the pool: its descendants and itself are NaN, the others as ever."""
+    s = Step([16], [[-1] + [0] * 30 + [30, 31]], (4, 2, 64), page=16)       # nodes 16 .. 31 stand in the third page
+    good = s.table.copy()
+    s.table[0, 2] = -1
+    s.to_gpu().run_plan()
+    got = s.attention()
+    s.table = good
+    assert np.isnan(got[16:33, :256]).all() and np.isfinite(got[:16]).all()
+    e, off = s.plain(0, s.up[0])
+    g = got[:16, :256].astype(np.float64).reshape(16, 4, 64)
+    assert (np.abs(g - e[:16]) <= np.abs(e[:16]) * 2.0 ** -11 + 2.0 ** -25 + off[:16] * (1 + 2.0 ** -11)).all()
 
 
 def test_tree_attention_many_requests():
@@ -359,9 +388,10 @@ def test_light_positions_behind_a_heavy_one_without_value():
     s.check(s.attention())
 
 
-def test_pages_outside_the_pool_make_their_readers_nan():
+@pytest.mark.parametrize("sizes", [[10, 6, 4], [3, 40, 33]])
+def test_pages_outside_the_pool_make_their_readers_nan(sizes):
     rng = np.random.default_rng(11)
-    s = Step([40, 70, 20], trees_of(rng, [10, 6, 4]), (4, 2, 80))
+    s = Step([40, 70, 20], trees_of(rng, sizes), (4, 2, 80))
     good = s.table.copy()
     s.table[1, 2] = s.n_pages
     s.table[2, 0] = -5

@@ -54,7 +54,7 @@ def test_plan_bytes():
 
 
 @pytest.mark.parametrize("change", [dict(n_requests=0), dict(n_requests=4097), dict(max_rows=0), dict(max_rows=(1 << 20) + 1), dict(max_nodes=0),
-                                    dict(max_nodes=257), dict(table_stride=0), dict(table_stride=1 << 26), dict(lens=0), dict(lens=4098),
+                                    dict(max_nodes=257), dict(table_stride=0), dict(table_stride=1 << 26), dict(table_stride=(1 << 24) + 1), dict(lens=0), dict(lens=4098),
                                     dict(row_start=0)])
 def test_batches_that_no_call_takes(change):
     p, b, x = cf.Pages(*PAGES), a_batch(**change), 65536
