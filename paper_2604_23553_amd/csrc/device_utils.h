@@ -162,11 +162,6 @@ __device__ __forceinline__ float2 xwg_load2(const float *p)      // p 8-byte ali
     f.y = __uint_as_float((unsigned)(v >> 32));
     return f;
 }
-__device__ __forceinline__ void xwg_store2(float *p, float a, float b)    // p 8-byte aligned
-{
-    const unsigned long long w = ((unsigned long long)__float_as_uint(b) << 32) | (unsigned long long)__float_as_uint(a);
-    __hip_atomic_store(as_global(reinterpret_cast<unsigned long long *>(p)), w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
 __device__ __forceinline__ void xwg_store_half(__half *p, float v)
 {
     const __half hv = __float2half_rn(v);

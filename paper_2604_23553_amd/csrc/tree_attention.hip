@@ -418,6 +418,12 @@ constexpr int kTaDevice = 16;                              // sc1
 __device__ __forceinline__ f32x4 ta_load(__amdgpu_buffer_rsrc_t b, unsigned off) { return __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(b, (int)off, 0, kTaDevice)); }
 __device__ __forceinline__ void ta_store(__amdgpu_buffer_rsrc_t b, unsigned off, f32x4 v) { __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), b, (int)off, 0, kTaDevice); }
 
+__device__ __forceinline__ void xwg_store2(float *p, float a, float b)                  // p 8-byte aligned
+{
+    const unsigned long long w = ((unsigned long long)__float_as_uint(b) << 32) | (unsigned long long)__float_as_uint(a);
+    __hip_atomic_store(as_global(reinterpret_cast<unsigned long long *>(p)), w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
 // Where a tile's pieces leave their sums: [piece][key head], each [row][D] and then (maximum, weight) of each row
 template <int D>
 struct TaSlot {
