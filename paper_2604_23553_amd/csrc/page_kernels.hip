@@ -11,8 +11,11 @@ namespace cfpp {
 // target_r = ceil((len_r + count_r) / page); a request takes target - held pages from the end of the free list or gives back
 // held - target.  Three running sums over the requests (pages taken, pages given back, rows) say which entry of the free list and
 // which rows are whose.  One workgroup has all requests: every sum needs all of the ones before it, and 4096 requests are four to a thread.
+// A chain of dependent reads, not bytes, bounds it: lengths, sums, list, table (one request 3.7 us, 4096 10.0 and 4.0 for the launch of their slots;
+// the reads alone are 80 KB).
 constexpr int kTablesEach = 4;           // requests of a thread
-constexpr int kTablesRows = 4096;        // rows whose slots it writes itself
+// Rows whose slots it writes itself, in a launch less (a launch is about 4 us): 4096 are four to a thread of 1024 or sixteen to one of 256
+constexpr int kTablesRows = 4096;
 constexpr int kSumMost = 1 << 28;      // sums stop here: more than any pool's pages or batch's rows, and two of them still fit 32 bits
 
 __device__ __forceinline__ int add_most(int a, int b) { return min(a + b, kSumMost); }
@@ -194,7 +197,7 @@ hipError_t launch_page_tables(const TablesParams &P, hipStream_t s)
 
 // ---- append ------------------------------------------------------------------------------------
 // A wavefront has 8 rows and 128 bytes of each, 16 to a lane: whole lines are read, and where the rows' slots follow one another 256 bytes in a
-// run are written.  `from`: where the pieces of K and V rows lie.
+// run are written.  Bound by the bytes: 4096 rows of hidden 4096, 134 MB read and written, 27.7 us, 4.85 TB/s, what a large copy reaches.  `from`: where the pieces of K and V rows lie.
 struct AppendFrom {
     const __half *k, *v;
     long long row, head;       // halves from row to row, from head to head
@@ -266,7 +269,9 @@ hipError_t launch_tree_out(const int *slots, int n_rows, const __half *from, __h
 // ---- the accepted path ---------------------------------------------------------------------------
 // A workgroup has one request and one of the K and V arrays of the layers; each walks the tree by itself (a step: every thread
 // looks whether its node is a child that agrees, the lowest one goes on).  Node path[j] >= j moves to index j: rows are moved in
-// ascending order, a block of pieces at a time, read before written.
+// ascending order, a block of pieces at a time, read before written: 8 loads to a thread are in flight, and the walk is done again by each workgroup
+// because a launch in between would cost more than its few steps in LDS.  48 requests of up to 63 nodes, 16 layers of hidden 4096,
+// are bound by the bytes of the nodes that move (155 MB, 35 - 39 us, 4.0 - 4.4 TB/s); 26 nodes of one request by the walk's steps (6.2 us).
 __global__ void __launch_bounds__(256) k_tree_accept(AcceptParams P, int n_layers)
 {
     __shared__ int parent[kTreeMaxNodes], token[kTreeMaxNodes], pick[kTreeMaxNodes], slot[kTreeMaxNodes], path[kTreeMaxNodes], child[2];

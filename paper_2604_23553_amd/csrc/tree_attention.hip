@@ -7,11 +7,19 @@
 //   O^T += V^T P^T (16 dimensions x 16 query rows): a lane's 8 K values are the positions of its own scores in two granules of 16, so
 //                  that P needs no exchange.  V goes through LDS as it lies in the pool; ds_read_b64_tr_b16 gives a lane four positions of its
 //                  dimension, 512 contiguous bytes to a wavefront.
-// One pass over the positions with the running maximum and sum of the softmax; a workgroup has a piece of a request's positions for one
-// key head, its four wavefronts every fourth row of 32 of them, each with sums of its own that are joined in LDS in order.  Requests of
-// few rows are cut into pieces until the CUs are full (k_tree_plan); the last workgroup of a tile adds the pieces in order.
+// One pass over the positions with the running maximum and sum of the softmax.  A workgroup has a piece of a request's positions for one key
+// head: up to 32 query rows, its four wavefronts take every fourth row of 32 positions, each with sums of its own that are joined in LDS in
+// order (ta_narrow); more query rows, the wavefronts share the query rows and every position goes through LDS once (ta_wide).  Requests are
+// cut into pieces until the CUs are full (k_tree_plan), and the pieces' sums are added in order, so a result does not depend on who comes first.
 // Weights enter the matrix instruction as two fp16 values, head and remainder, 2^9 times their size: 2^-21 of each and 2^-33 of the largest, as near
 // as the sums in 32 bits are.  Queries and keys are fp16 as they come.
+//
+// Bound and measured (repeated launches, the join included): few query rows by the K and V that are read - one token of 8 requests behind 8000
+// positions of hidden 4096 103 us, 5.7 TB/s; 64 requests of up to 9 nodes behind up to 3000, four query heads to a key head, 86 us, 4.3 TB/s; 16 of 30
+// behind 2500 of hidden 2560 71 us, 5.3 TB/s - by the launches and one piece's way through them where a single request is short (one token
+// behind 128 positions 9.5 us, 26 behind 4096 18 us).  Many query rows are bound by issue: 8 requests of 200 to 256 nodes behind 6000 to 8200 of
+// hidden 4096 take 415 us, 555 TFLOP/s of the formula's own and half as much again for the remainders, the matrix instructions busy 44 % of the time beside
+// the exponentials and splits of the weights.  Without the remainders it is 388 us of then 462, an error of 2^-11 to each weight: not taken.
 #include <hip/hip_runtime.h>
 #include <hip/hip_fp16.h>
 #include "tree_params.h"
@@ -26,11 +34,19 @@ typedef _Float16 ta_f16x8 __attribute__((ext_vector_type(8)));
 typedef unsigned ta_u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kTaThreads = 256, kTaWaves = kTaThreads / 64, kTaRow = 32, kTaStep = kTaRow * kTaWaves;
-constexpr int kTaWhole = 256;                              // positions that are not cut
-constexpr int kTaWgsWide = 512;
-constexpr int kTaWgs = 512;                                // workgroups that the pieces aim at
-constexpr int kTaShort = 1024;                             // positions of a piece
-constexpr int kTaLastJoins = 16;                           // up to so many query rows to a tile its last workgroup adds the pieces
+// Positions that are not cut.  Of hidden 2560 and one token, whole / cut: behind 500 10.3 / 8.4 us, behind 900 15.5 / 9.3; a piece of 128 is one row to a
+// wavefront, and joining pieces costs about what a second row does.
+constexpr int kTaWhole = 256;
+// Workgroups that the pieces aim at, two to a CU.  With 256 / 512 / 768 / 1024: one token of 8 requests behind 8000 120 / 104 / 107 / 104 us, 26 nodes
+// behind 4096 18 / 22 / 28 / 30 (see kTaShort); with 256 / 512 / 1024 / 1536, 64 nodes behind 8000 of hidden 4096 38.0 / 37.6 / 49.5 / 54.9, 4 requests of 60 nodes
+// with four query heads to a key head 54 / 48.5 / 60 / 74.  Two wavefronts more to each SIMD in workgroups of eight instead: 112 of 104, 20.5 of 18.4.
+constexpr int kTaWgs = 512;
+// Up to 32 query rows whose pieces would have half as many positions or fewer are given half the workgroups: 26 nodes behind 4096 22.2 / 18.1 us, one token
+// there 16.0 / 14.6; tiles of 128 rows are left at kTaWgs, where half of them costs 54 us instead of 48.5 (the 4 requests above).
+constexpr int kTaShort = 1024;
+// Up to so many query rows to a tile its last workgroup adds the pieces, above it a launch does, which has all CUs for the up to 128 rows of sums: 64 nodes
+// behind 8000 49 / 38 us, 200 behind 300 25.5 / 16.9, 26 behind 500 14.1 / 12.6.  With 16 rows the launch costs more: one token behind 4096 15.9 / 17.8.
+constexpr int kTaLastJoins = 16;
 constexpr float kTaLowest = -3.402823466e38f;
 
 // ---- the plan --------------------------------------------------------------------------------------
@@ -41,7 +57,7 @@ TreePlanLayout tree_plan_layout(const PageDims &pg, int n_heads, int requests, i
     L.tile_rows = tree_tile_rows((int)(group * max_nodes));
     const long long each = (group * max_nodes + L.tile_rows - 1) / L.tile_rows * requests, all = group * max_rows / L.tile_rows + requests;
     L.tiles = (int)(each < all ? each : all);
-    L.want = ((L.tile_rows <= kTaLastJoins ? kTaWgs : kTaWgsWide) + pg.heads - 1) / pg.heads;
+    L.want = (kTaWgs + pg.heads - 1) / pg.heads;
     L.work = L.want + L.tiles;                             // (pieces of a tile: its share of `want`, to the nearest whole number, and one at least)
     L.piece_step = L.tile_rows <= 32 ? kTaStep : kTaRow;
     size_t o = align_up(sizeof(TreePlanHead), 256);
@@ -128,7 +144,6 @@ __device__ __forceinline__ void tree_work(const PageDims &pg, const TreeBatch &b
     __syncthreads();
     total = 0;
     for (int w = 0; w < kTaWaves; ++w) total += wave_total[w];
-    // Few rows behind a short way: one workgroup to a CU (26 nodes behind 4096 positions of hidden 2560, pieces of 384 / 640: 22.2 / 18.1 us)
     const int want = L.tile_rows <= 32 && total * 2 <= (long long)kTaShort * L.want ? (L.want + 1) / 2 : L.want;
     const long long C = max((total + want - 1) / want, (long long)kTaStep);
     // the nearest number of pieces: they come to 4 / 3 of `want` at most beside those of the tiles that stay whole
@@ -635,7 +650,8 @@ __device__ __forceinline__ void ta_narrow(const TreeAttention &P, const TreePlan
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 15, kg = lane >> 4;
     const TreeItem &it = w.it;
     const int words = tree_words(P.b.max_nodes);
-    // rows on their way: as many as registers hold beside the sums
+    // rows on their way in registers: as many as fit beside the sums (two of head_dim 128 with 32 query rows go to memory).  Bypassing the caches pays: no
+    // row is read again but by the tiles of its own request (loads kept there: the 64 requests 100 of 94 us, one token of 8 behind 8000 117 of 107).
     constexpr int AHEAD = QT == 1 || D <= 80 ? 2 : 1;
     TaRow<D> r[AHEAD];
     const int row0 = it.t0 / kTaRow + wave;
@@ -762,6 +778,9 @@ __device__ __forceinline__ void ta_narrow(const TreeAttention &P, const TreePlan
 // A row of 32 positions goes through LDS for all four wavefronts, K and V as they lie in the pool, straight from memory: a ring of kTwRing
 // rows, one granule of K or V of each to a wavefront, waited for by count, and one barrier a row.  A wavefront has 16 QT query rows and all positions
 // of the piece, so nothing is joined but the pieces.  Positions past the piece's end read its last one again: their weights are zero.
+// A workgroup's rows come through LDS, not registers, because four wavefronts read each of them: 607 -> 576 us (8 requests of 256 nodes).  A K value is
+// then used by 32 query rows and a V value by as many, so the LDS reads stay below the matrix instructions' time; scores a row ahead took 495 to 475,
+// sums side by side 444 to 420.  (With every load of one row that the L2 holds: 446 to 404, so waiting for memory is a tenth at most.)
 constexpr int kTwRing = 4;
 template <int D>
 struct TwLds {
