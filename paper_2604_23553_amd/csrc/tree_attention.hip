@@ -864,10 +864,21 @@ __device__ __forceinline__ void ta_wide(const TreeAttention &P, const TreePlanLa
                 for (int j = 0; j < QT; ++j) S[j][t] = Q[j].score(x, s, S[j][t]);
             }
     };
+    int at = 0;
     tw_arrive<(kTwRing - 2) * Lds::loads>();
+    // A wavefront without a query row of its own only loads and waits with the others (64 requests of 36 query rows: 103 -> 98 us).
+    if (wave * RW >= w.rows) {
+        for (int row = first; row * kTaRow < it.t1; ++row) {
+            tw_arrive<(kTwRing - 3) * Lds::loads>();
+            request(row + kTwRing - 1, (at + kTwRing - 1) % kTwRing, next);
+            next = w.pages.pick(2 * (row + kTwRing) + mine);
+            at = (at + 1) % kTwRing;
+        }
+        tw_arrive<0>();
+        return;
+    }
     keys(0);
     scores(S);
-    int at = 0;
     for (int row = first; row * kTaRow < it.t1; ++row) {
         const int ahead = (at + 1) % kTwRing;
         tw_arrive<(kTwRing - 3) * Lds::loads>();           // (the next row is here)
