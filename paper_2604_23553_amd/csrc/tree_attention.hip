@@ -121,13 +121,16 @@ __device__ __forceinline__ void tree_masks(const PageDims &pg, const TreeBatch &
 }
 
 // The work list, by one workgroup: with tiles_r tiles of query rows, a request's positions are cut into equal pieces of about C, multiples of what the
-// wavefronts take at a time, so that all pieces come to about `want`.
+// wavefronts take at a time, so that all pieces come to about `want`.  The requests of the longest pieces come first, in classes of an eighth of C, so that
+// short ones fill the end: 64 requests of up to 9 nodes, lengths from 33 to 3000, 86 us in the requests' order and 77 so, of 16 nodes each 106 and 95.
 __device__ __forceinline__ void tree_work(const PageDims &pg, const TreeBatch &b, int group, const TreePlanLayout &L, char *plan)
 {
-    extern __shared__ int tp_sums[];                       // running sums, [3][requests]
-    int *items = tp_sums, *multi = tp_sums + b.requests, *tiles = tp_sums + 2 * b.requests;
-    __shared__ int wave_part[3][kTaWaves], cuts;
+    extern __shared__ int tp_sums[];                       // [3][requests]: running sums of the items and of those of cut tiles; tiles, class, first place
+    int *items = tp_sums, *multi = tp_sums + b.requests, *place = tp_sums + 2 * b.requests;
+    constexpr int CLASSES = 16;
+    __shared__ int wave_part[2][kTaWaves], cuts, classes[CLASSES];
     if (threadIdx.x == 0) cuts = 0;
+    if (threadIdx.x < CLASSES) classes[threadIdx.x] = 0;
     __shared__ long long wave_total[kTaWaves];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, R = b.requests, each = (R + kTaThreads - 1) / kTaThreads;
     const int lo = min(tid * each, R), hi = min(lo + each, R);
@@ -135,7 +138,7 @@ __device__ __forceinline__ void tree_work(const PageDims &pg, const TreeBatch &b
     long long total = 0;
     for (int r = lo; r < hi; ++r) {
         const int n = tree_rows(pg, b, r, first), t = (n * group + L.tile_rows - 1) / L.tile_rows;
-        tiles[r] = t;
+        place[r] = t;
         items[r] = n > 0 ? b.lens[r] + n : 0;              // (positions, for the moment)
         total += (long long)t * items[r];
     }
@@ -149,17 +152,19 @@ __device__ __forceinline__ void tree_work(const PageDims &pg, const TreeBatch &b
     // the nearest number of pieces: they come to 4 / 3 of `want` at most beside those of the tiles that stay whole
     auto piece_size = [&](int x, int pieces) { return ((x + pieces - 1) / pieces + L.piece_step - 1) / L.piece_step * L.piece_step; };
     auto pieces_of = [&](int x) { return x <= kTaWhole ? 1 : max(1, (int)((2 * (long long)x + C) / (2 * C))); };
-    int sum[3] = {0, 0, 0};
+    int sum[2] = {0, 0};
     for (int r = lo; r < hi; ++r) {
-        const int t = tiles[r], x = items[r], n = pieces_of(x), size = piece_size(x, n), pieces = t <= 0 ? 0 : (x + size - 1) / size;
+        const int t = place[r], x = items[r], n = pieces_of(x), size = piece_size(x, n), pieces = t <= 0 ? 0 : (x + size - 1) / size;
         sum[0] += t * pieces;
         sum[1] += pieces > 1 ? t * pieces : 0;
-        sum[2] += t;
-        items[r] = sum[0]; multi[r] = sum[1]; tiles[r] = sum[2];
+        items[r] = sum[0]; multi[r] = sum[1];
+        const int c = CLASSES - 1 - (int)min(CLASSES - 1LL, 8LL * size / C);
+        place[r] = c;
+        if (t > 0) atomicAdd(&classes[c], t * pieces);
     }
-    int before[3];
+    int before[2];
 #pragma unroll
-    for (int k = 0; k < 3; ++k) {
+    for (int k = 0; k < 2; ++k) {
         int s = sum[k];
         for (int m = 1; m < 64; m <<= 1) {
             const int o = __shfl_up(s, m, 64);
@@ -169,9 +174,25 @@ __device__ __forceinline__ void tree_work(const PageDims &pg, const TreeBatch &b
         before[k] = s - sum[k];
     }
     __syncthreads();
-    for (int k = 0; k < 3; ++k)
+    for (int k = 0; k < 2; ++k)
         for (int w = 0; w < wave; ++w) before[k] += wave_part[k][w];
-    for (int r = lo; r < hi; ++r) { items[r] += before[0]; multi[r] += before[1]; tiles[r] += before[2]; }
+    if (wave == 0) {                                       // where the classes begin
+        int s = lane < CLASSES ? classes[lane] : 0;
+        const int own = s;
+        for (int m = 1; m < CLASSES; m <<= 1) {
+            const int o = __shfl_up(s, m, 64);
+            if (lane >= m) s += o;
+        }
+        if (lane < CLASSES) classes[lane] = s - own;
+    }
+    __syncthreads();
+    int last = 0;
+    for (int r = lo; r < hi; ++r) {
+        const int sums = items[r];
+        if (sums > last) place[r] = atomicAdd(&classes[place[r]], sums - last);
+        last = sums;
+        items[r] = sums + before[0]; multi[r] += before[1];
+    }
     __syncthreads();
     const int n_items = R > 0 ? items[R - 1] : 0;
     if (tid == 0) {
@@ -187,22 +208,23 @@ __device__ __forceinline__ void tree_work(const PageDims &pg, const TreeBatch &b
             if (items[mid] > i) z = mid;
             else a = mid + 1;
         }
-        const int r = a, t0 = r > 0 ? tiles[r - 1] : 0, n_tiles = tiles[r] - t0, at = i - (r > 0 ? items[r - 1] : 0);
+        const int r = a, before = r > 0 ? items[r - 1] : 0, at = i - before;
         TreeItem it;
         it.request = r;                                    // (one that takes part: it has items)
         it.first = b.row_start[r];
         it.nodes = b.row_start[r + 1] - it.first;
         it.len = b.lens[r];
-        it.pieces = (items[r] - (r > 0 ? items[r - 1] : 0)) / n_tiles;
+        const int n_tiles = (it.nodes * group + L.tile_rows - 1) / L.tile_rows, to = place[r] + at;
+        it.pieces = (items[r] - before) / n_tiles;
         it.piece = at / n_tiles;                           // (the tiles of a piece follow one another: they read the same rows)
         it.tile = at - it.piece * n_tiles;
         it.slot = it.pieces > 1 ? (r > 0 ? multi[r - 1] : 0) + it.tile * it.pieces : -1;
         const int x = it.len + it.nodes, size = piece_size(x, pieces_of(x));
         it.t0 = it.piece * size;
         it.t1 = min(x, it.t0 + size);
-        if (it.pieces > 1 && it.piece == 0) cut[atomicAdd(&cuts, 1)] = i;              // (at most want / 1.5; in any order)
+        if (it.pieces > 1 && it.piece == 0) cut[atomicAdd(&cuts, 1)] = to;             // (at most want / 1.5; in any order)
         it.pad[0] = it.pad[1] = 0;
-        list[i] = it;
+        list[to] = it;
     }
     __syncthreads();
     if (tid == 0) reinterpret_cast<TreePlanHead *>(plan)->cuts = cuts;
