@@ -15,11 +15,12 @@
 // as the sums in 32 bits are.  Queries and keys are fp16 as they come.
 //
 // Bound and measured (repeated launches, the join included): few query rows by the K and V that are read - one token of 8 requests behind 8000
-// positions of hidden 4096 103 us, 5.7 TB/s; 64 requests of up to 9 nodes behind up to 3000, four query heads to a key head, 86 us, 4.3 TB/s; 16 of 30
+// positions of hidden 4096 103 us, 5.7 TB/s; 64 requests of up to 9 nodes behind up to 3000, four query heads to a key head, 77 us, 4.8 TB/s; 16 of 30
 // behind 2500 of hidden 2560 71 us, 5.3 TB/s - by the launches and one piece's way through them where a single request is short (one token
 // behind 128 positions 9.5 us, 26 behind 4096 18 us).  Many query rows are bound by issue: 8 requests of 200 to 256 nodes behind 6000 to 8200 of
-// hidden 4096 take 415 us, 555 TFLOP/s of the formula's own and half as much again for the remainders, the matrix instructions busy 44 % of the time beside
-// the exponentials and splits of the weights.  Without the remainders it is 388 us of then 462, an error of 2^-11 to each weight: not taken.
+// hidden 4096 take 401 - 430 us by the card, 230 GFLOP of the formula's own, 413 issued with the remainders, the sums of the weights and the rows that
+// fill tiles: 0.96 - 1.03 PFLOP/s, where a library product of 8192^3 reached 1.07.  Without the remainders it is 388 us of then 462, an error of 2^-11 to
+// each weight: not taken.
 #include <hip/hip_runtime.h>
 #include <hip/hip_fp16.h>
 #include "tree_params.h"
