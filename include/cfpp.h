@@ -423,7 +423,8 @@ cfpp_status cfpp_validate_pages(const cfpp_pages *pages);
 size_t cfpp_page_pool_bytes(const cfpp_pages *pages);
 /* Bytes of a batch's plan: the attention's launch plan, its counters and the sums that
  * workgroups hand over.  0 for invalid arguments.  n_heads: query heads, a multiple of
- * n_kv_heads, at most 256 to each of them. */
+ * n_kv_heads, at most 256 to each of them; less than 2^24 tiles (128 query rows of a
+ * request and key head) in all. */
 size_t cfpp_tree_plan_bytes(const cfpp_pages *pages, int32_t n_heads, int32_t n_requests,
                             int32_t max_rows, int32_t max_nodes);
 
@@ -459,7 +460,7 @@ cfpp_status cfpp_tree_plan(const cfpp_pages *pages, const cfpp_tree_batch *batch
 
 /* Row i of k_rows and v_rows (DEVICE fp16 [n_rows][row_stride], head n's values at
  * n * head_dim; row_stride in elements, a multiple of 8) into slots[i] of a layer's
- * pool.  Slots outside the pool are skipped; of equal slots one row wins, piece by piece. */
+ * pool; less than 2^33 values to K.  Slots outside the pool are skipped; of equal slots one row wins, piece by piece. */
 cfpp_status cfpp_page_append(const cfpp_pages *pages, void *kv_pool, const void *k_rows,
                              const void *v_rows, int64_t row_stride, const int32_t *slots,
                              int32_t n_rows, cfpp_stream stream);

@@ -1092,10 +1092,19 @@ static cfpp_status check_tree_sizes(int32_t requests, int32_t max_rows, int32_t 
     return CFPP_OK;
 }
 
+// a launch has less than 2^32 threads
+static cfpp_status check_tree_grid(const cfpp_pages *p, const TreePlanLayout &L)
+{
+    if ((long long)L.work * p->n_kv_heads >= 1 << 24)
+        return fail(CFPP_EUNSUPPORTED, "up to %d tiles of query rows for each of %d key heads: less than 2^24 in all", L.work, p->n_kv_heads);
+    return CFPP_OK;
+}
+
 extern "C" size_t cfpp_tree_plan_bytes(const cfpp_pages *p, int32_t n_heads, int32_t n_requests, int32_t max_rows, int32_t max_nodes)
 {
     if (cfpp_validate_pages(p) != CFPP_OK || check_tree_heads(p, n_heads) != CFPP_OK || check_tree_sizes(n_requests, max_rows, max_nodes) != CFPP_OK) return 0;
-    return tree_plan_layout(page_dims(*p), n_heads, n_requests, max_rows, max_nodes, 1).total;
+    const TreePlanLayout L = tree_plan_layout(page_dims(*p), n_heads, n_requests, max_rows, max_nodes, 1);
+    return check_tree_grid(p, L) == CFPP_OK ? L.total : 0;
 }
 
 // what every call needs of a batch; its arrays are checked by the calls that use them
@@ -1119,8 +1128,9 @@ static cfpp_status check_tree_plan(const cfpp_pages *p, const cfpp_tree_batch *b
     cfpp_status st = check_tree_heads(p, n_heads);
     if (st != CFPP_OK) return st;
     if (!b->plan || (reinterpret_cast<uintptr_t>(b->plan) & 255u)) return fail(CFPP_EINVAL, "plan is NULL or not 256-byte aligned");
-    const size_t need = tree_plan_layout(page_dims(*p), n_heads, b->n_requests, b->max_rows, b->max_nodes, b->table_stride).total;
-    if (b->plan_bytes < need) return fail(CFPP_ENOMEM, "plan of %zu bytes, %zu needed", b->plan_bytes, need);
+    const TreePlanLayout L = tree_plan_layout(page_dims(*p), n_heads, b->n_requests, b->max_rows, b->max_nodes, b->table_stride);
+    if ((st = check_tree_grid(p, L)) != CFPP_OK) return st;
+    if (b->plan_bytes < L.total) return fail(CFPP_ENOMEM, "plan of %zu bytes, %zu needed", b->plan_bytes, L.total);
     if (!aligned4(b->masks)) return fail(CFPP_EINVAL, "masks is NULL or misaligned");
     return CFPP_OK;
 }
@@ -1162,6 +1172,8 @@ extern "C" cfpp_status cfpp_page_append(const cfpp_pages *pages, void *kv_pool, 
     if (n_rows < 0 || n_rows > kTreeMaxRows) return fail(CFPP_EINVAL, "n_rows %d outside [0, %d]", n_rows, kTreeMaxRows);
     if (row_stride % 8 || row_stride < (int64_t)pages->n_kv_heads * pages->head_dim || row_stride > (1ll << 32))
         return fail(CFPP_EINVAL, "row_stride %lld: a multiple of 8, at least n_kv_heads * head_dim and at most 2^32", (long long)row_stride);
+    if ((long long)n_rows * pages->n_kv_heads * pages->head_dim >= 1ll << 33)           // (a launch has less than 2^32 threads)
+        return fail(CFPP_EUNSUPPORTED, "%d rows of %d heads of %d: less than 2^33 values", n_rows, pages->n_kv_heads, pages->head_dim);
     if (n_rows == 0) return CFPP_OK;
     HIP_OK(launch_page_append(page_dims(*pages), static_cast<__half *>(kv_pool), static_cast<const __half *>(k_rows),
                               static_cast<const __half *>(v_rows), row_stride, slots, n_rows, static_cast<hipStream_t>(stream)));

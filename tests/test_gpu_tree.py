@@ -316,6 +316,26 @@ def test_tree_attention_many_requests():
     s.check(s.attention())
 
 
+def test_tree_attention_of_4096_requests():
+    """All that a step may have, most of them short or without rows: the plan's classes by length, several requests to a thread."""
+    rng = np.random.default_rng(8)
+    sizes, lens = [int(v) for v in rng.integers(0, 3, 4096)], [int(v) for v in rng.integers(0, 20, 4096)]
+    for r, n in ((0, 700), (17, 1500), (2048, 333), (4095, 900)):
+        sizes[r], lens[r] = 2, n
+    s = Step(lens, trees_of(rng, sizes), (2, 1, 64), 16).to_gpu().run_plan()
+    s.check(s.attention())
+
+
+@pytest.mark.parametrize("heads", [(4, 1, 64), (8, 2, 80), (4, 1, 128)])
+def test_tiles_that_some_wavefronts_have_no_rows_of(heads):
+    rng = np.random.default_rng(sum(heads))
+    sizes = [9, 16, 24, 13, 17, 1]                         # query rows: 36, 64, 96, 52, 68, 4
+    s = Step([900, 40, 2000, 5, 33, 4000], trees_of(rng, sizes), heads, 48).to_gpu().run_plan()
+    first = s.attention()
+    s.check(first)
+    assert np.array_equal(first.view(np.uint16), s.run_plan().attention().view(np.uint16)), "the bits change from plan to plan"
+
+
 @pytest.mark.parametrize("lens,sizes", [([0, 40], [9, 40]), ([70], [33])])
 def test_masks_of_the_callers_own(lens, sizes):
     """Any set of nodes; rows that see nothing (zeros where nothing is cached), all, a later node, and bits behind the last node."""

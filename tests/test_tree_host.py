@@ -146,3 +146,16 @@ def test_plain_allocator_by_hand():
     assert slots[16] == 12 * 16 and slots[17] == 11 * 16 and list(slots[20:]) == [-1] * 4
     granted, starts, slots = a.step([0, 20], [0, 30], 24)            # 50 positions are four pages: the table is too short
     assert granted == [1, 0] and a.tables == [[], [11]] and a.free == [10, 13, 12]
+
+
+def test_launches_of_2_32_threads_are_refused():
+    p, x = cf.Pages(64, 16, 256, 64), 65536
+    b = a_batch(n_requests=4096, max_rows=1 << 20, max_nodes=256)
+    assert cf.cfpp_tree_plan_bytes(p, 256, 4096, 1 << 20, 256) > 0                     # 16384 tiles, 256 key heads
+    for heads, rows in ((256 * 16, 1 << 20), (256 * 256, 1 << 20), (256 * 256, 1 << 16)):
+        assert cf.cfpp_tree_plan_bytes(p, heads, 4096, rows, 256) == 0
+        b.max_rows = rows
+        assert refused(cf.cfpp_tree_plan, p, b, heads) == -2
+        assert refused(cf.cfpp_tree_attention, p, x, b, x, heads, 1 << 50) == -2
+    wide = cf.Pages(64, 16, 64, 128)
+    assert refused(cf.cfpp_page_append, wide, x, x, x, x, 1 << 20) == -2
