@@ -1015,7 +1015,7 @@ __global__ void __launch_bounds__(kTaThreads, 2) k_tree_attention(TreeAttention 
 }
 
 // The pieces of many query rows are added by a launch of its own, 1024 sums to a workgroup at a time: for one workgroup they are up to 16384.
-constexpr int kTaJoinWgs = 1024;
+constexpr int kTaJoinWgs = 1024;                          // (256 / 512 / 1024: 4 requests of 60 nodes 49 / 45 / 45 us, 64 of 9 81 / 79.5 / 78)
 template <int D, int TQ, bool STACK>
 __global__ void __launch_bounds__(kTaThreads) k_tree_join(TreeAttention P, TreePlanLayout L, const char *plan)
 {
