@@ -406,7 +406,8 @@ typedef struct cfpp_tree_batch {
     int32_t max_nodes;          /* most nodes of a request, 1 .. 256                       */
     int32_t table_stride;       /* entries of a request's block table; times page_len at most 2^30 */
     const int32_t *lens;        /* [n_requests]                                            */
-    int32_t *row_start;         /* [n_requests + 1]         written by cfpp_page_tables    */
+    int32_t *row_start;         /* [n_requests + 1]         written by cfpp_page_tables; must not fall:
+                                   where it does, the plan holds no request                */
     int32_t *block_table;       /* [n_requests][table_stride]  pages, by position / page_len */
     int32_t *slots;             /* [max_rows]               written by cfpp_page_tables    */
     const int32_t *parents;     /* [max_rows]                                              */

@@ -124,6 +124,8 @@ __device__ __forceinline__ void tree_masks(const PageDims &pg, const TreeBatch &
 // The work list, by one workgroup: with tiles_r tiles of query rows, a request's positions are cut into equal pieces of about C, multiples of what the
 // wavefronts take at a time, so that all pieces come to about `want`.  The requests of the longest pieces come first, in classes of an eighth of C, so that
 // short ones fill the end: 64 requests of up to 9 nodes, lengths from 33 to 3000, 86 us in the requests' order and 77 so, of 16 nodes each 106 and 95.
+// L.tiles bounds the tiles of rows that are one request's each.  Where row_start falls, rows can be several requests', whose tiles may be more than the list
+// holds: such a batch has no items.
 __device__ __forceinline__ void tree_work(const PageDims &pg, const TreeBatch &b, int group, const TreePlanLayout &L, char *plan)
 {
     extern __shared__ int tp_sums[];                       // [3][requests]: running sums of the items and of those of cut tiles; tiles, class, first place
@@ -133,21 +135,25 @@ __device__ __forceinline__ void tree_work(const PageDims &pg, const TreeBatch &b
     if (threadIdx.x == 0) cuts = 0;
     if (threadIdx.x < CLASSES) classes[threadIdx.x] = 0;
     __shared__ long long wave_total[kTaWaves];
+    __shared__ bool wave_falls[kTaWaves];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, R = b.requests, each = (R + kTaThreads - 1) / kTaThreads;
     const int lo = min(tid * each, R), hi = min(lo + each, R);
     int first;
     long long total = 0;
+    bool falls = false;
     for (int r = lo; r < hi; ++r) {
+        falls = falls || b.row_start[r + 1] < b.row_start[r];
         const int n = tree_rows(pg, b, r, first), t = (n * group + L.tile_rows - 1) / L.tile_rows;
         place[r] = t;
         items[r] = n > 0 ? b.lens[r] + n : 0;              // (positions, for the moment)
         total += (long long)t * items[r];
     }
     for (int m = 1; m < 64; m <<= 1) total += __shfl_xor(total, m, 64);
-    if (lane == 0) wave_total[wave] = total;
+    falls = __any(falls);
+    if (lane == 0) { wave_total[wave] = total; wave_falls[wave] = falls; }
     __syncthreads();
     total = 0;
-    for (int w = 0; w < kTaWaves; ++w) total += wave_total[w];
+    for (int w = 0; w < kTaWaves; ++w) { total += wave_total[w]; falls = falls || wave_falls[w]; }
     const int want = L.tile_rows <= 32 && total * 2 <= (long long)kTaShort * L.want ? (L.want + 1) / 2 : L.want;
     const long long C = max((total + want - 1) / want, (long long)kTaStep);
     // the nearest number of pieces: they come to 4 / 3 of `want` at most beside those of the tiles that stay whole
@@ -155,7 +161,7 @@ __device__ __forceinline__ void tree_work(const PageDims &pg, const TreeBatch &b
     auto pieces_of = [&](int x) { return x <= kTaWhole ? 1 : max(1, (int)((2 * (long long)x + C) / (2 * C))); };
     int sum[2] = {0, 0};
     for (int r = lo; r < hi; ++r) {
-        const int t = place[r], x = items[r], n = pieces_of(x), size = piece_size(x, n), pieces = t <= 0 ? 0 : (x + size - 1) / size;
+        const int t = falls ? 0 : place[r], x = items[r], n = pieces_of(x), size = piece_size(x, n), pieces = t <= 0 ? 0 : (x + size - 1) / size;
         sum[0] += t * pieces;
         sum[1] += pieces > 1 ? t * pieces : 0;
         items[r] = sum[0]; multi[r] = sum[1];

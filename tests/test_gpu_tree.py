@@ -251,6 +251,28 @@ def test_a_plan_without_slots_counts_every_request_and_one_of_other_sizes_writes
     assert (s.g_out == 7.0).all()
 
 
+def test_a_row_start_that_falls_leaves_every_request_out():
+    """Rows that are several requests', of which the work list's room knows nothing: no output is written, nor anything behind the plan.  2048 tiles of
+    query rows where the plan's sizes are made for 272."""
+    R, rows = 256, 256
+    s = Step([1], [[-1] + [0] * (rows - 1)], (8, 1, 64), max_nodes=rows, max_rows=rows)
+    s.R = R                                                # (sizes of R requests; the arrays below take the place of the one request's)
+    s.to_gpu()
+    n = s.plan.numel()
+    guarded = torch.full((n + (1 << 20),), 0x5A, dtype=torch.uint8, device="cuda")
+    starts, lens = i32([0, rows] * (R // 2) + [0]), i32([1] * R)
+    table, slots = i32(np.repeat(s.table, R, 0)), i32(s.slots)
+    s.batch = cf.TreeBatch.of(rows, lens, starts, table, slots, s.g["parents"], s.g_masks, s.g_positions, guarded[:n])
+    s.run_plan()
+    got = s.attention()
+    assert (got == 7.0).all()
+    assert bool((guarded[n:] == 0x5A).all())
+    starts.copy_(i32([0] + [rows] * R))                    # (one request has them all)
+    s.run_plan()
+    s.R, s.starts = 1, [0]
+    s.check(s.attention())
+
+
 # ---- append ---------------------------------------------------------------------------------------------
 @pytest.mark.parametrize("heads,d,page,rows,pad", [(1, 64, 16, 1, 0), (3, 80, 48, 37, 8), (8, 128, 64, 300, 0), (32, 80, 16, 5, 5120)])
 def test_page_append(heads, d, page, rows, pad):
