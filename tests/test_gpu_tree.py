@@ -504,6 +504,49 @@ def test_offsets_past_32_bits():
     assert (np.abs(g - e) <= np.abs(e) * 2.0 ** -11 + 2.0 ** -25 + off * (1 + 2.0 ** -11)).all()
 
 
+# (query rows of 16, 32, 64 and 128 to a tile; more than 256 positions are cut into pieces)
+@pytest.mark.parametrize("heads,sizes", [((4, 4, 64), [7, 2]), ((5, 5, 80), [26, 3]), ((4, 2, 128), [30, 20]), ((4, 1, 64), [33, 9])])
+def test_values_that_are_not_finite_in_pieces(heads, sizes):
+    """Infinite and NaN K and V in the middle of a request that is cut into pieces, cached (everybody's) and drafted (its descendants')."""
+    rng = np.random.default_rng(sum(sizes))
+    s = Step([1500, 700, 400], trees_of(rng, sizes + [5]), heads, 16)
+    H = heads[1]
+    for r, at, which, head, value in ((0, 620, 1, 0, np.inf), (0, 700, 1, 1 % H, -np.inf), (0, 1001, 0, H - 1, np.inf), (1, 333, 1, 0, np.nan), (1, 420, 0, H - 1, -np.inf),
+                                      (2, 402, 1, 0, np.nan), (2, 403, 0, 0, np.inf)):
+        s.pool[0, which, s.table[r, at // 16], head, 1, at % 16, 5] = value
+    s.to_gpu().run_plan()
+    first = s.attention()
+    # (the 2-norm of all roundings needs many finite values: each by itself here)
+    for r in range(3):
+        e, off = s.plain(r, s.up[r])
+        g = first[s.starts[r]:s.starts[r] + s.counts[r], :s.H * s.d].astype(np.float64).reshape(e.shape)
+        fine = np.isfinite(e)
+        assert np.array_equal(np.isnan(g), np.isnan(e)), f"request {r}: NaN in other places"
+        assert np.array_equal(g[~fine & ~np.isnan(e)], e[~fine & ~np.isnan(e)])
+        assert (np.abs(g - e)[fine] <= (np.abs(e) * 2.0 ** -11 + 2.0 ** -25 + off * (1 + 2.0 ** -11))[fine]).all(), f"request {r}"
+    assert np.isfinite(first[:s.rows]).any() and np.isnan(first[:s.rows, :s.H * s.d]).any()
+    assert np.array_equal(first.view(np.uint16), s.attention().view(np.uint16)), "the bits change from call to call"
+
+
+@pytest.mark.parametrize("heads", [(2, 2, 64), (4, 2, 80), (8, 2, 64)])
+def test_pages_outside_the_pool_in_pieces(heads):
+    """A cached page outside the pool in a middle piece makes all of its request NaN; one that only some nodes see, in the last piece, makes these NaN."""
+    rng = np.random.default_rng(sum(heads))
+    s = Step([1500, 1500, 600], [tree_ref.random_tree(rng, 6), [-1] + [0] * 12 + [12, 13], tree_ref.random_tree(rng, 11)], heads, 16)
+    good = s.table.copy()
+    s.table[0, 40] = s.n_pages + 7
+    s.table[1, 94] = -1                                    # (positions 1504 on: the second request's nodes 4 .. 14)
+    s.to_gpu().run_plan()
+    got = s.attention()
+    width = s.H * s.d
+    assert np.isnan(got[:6, :width]).all() and np.isnan(got[10:21, :width]).all()
+    s.table = good
+    e, off = s.plain(1, s.up[1])
+    g = got[6:10, :width].astype(np.float64).reshape(4, s.H, s.d)
+    assert (np.abs(g - e[:4]) <= np.abs(e[:4]) * 2.0 ** -11 + 2.0 ** -25 + off[:4] * (1 + 2.0 ** -11)).all()
+    s.check(got, requests=[2])
+
+
 # ---- the accepted path -------------------------------------------------------------------------------------
 def check_accept(s, tokens, picks, layers, inplace=False, limit=None):
     s.to_gpu()
