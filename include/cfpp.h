@@ -442,7 +442,8 @@ size_t cfpp_tree_plan_bytes(const cfpp_pages *pages, int32_t n_heads, int32_t n_
  *                the block table is too short, lens or counts negative, or the rows pass
  *                max_rows: such a request neither takes nor gives, and its slots are -1
  * Uses lens; writes block_table (taken pages; -1 in place of those given back),
- * row_start (the sums of counts, up to max_rows; a negative one counts as 0) and slots.
+ * row_start (the sums of counts, up to max_rows; a negative one counts as 0) and slots
+ * (-1 too for a position whose page, held or from the list, is none of the pool's).
  * The batch's other pointers may be NULL.  Asynchronous on `stream`, as the calls below. */
 cfpp_status cfpp_page_tables(const cfpp_pages *pages, const cfpp_tree_batch *batch,
                              const int32_t *counts, int32_t *held, int32_t *free_pages,

@@ -59,9 +59,11 @@ __device__ __forceinline__ int find_above(const int *sum, int n, int v)
     return lo;
 }
 
+// -1 where the block table's entry lies outside the pool (its product with the page's length could come back to a slot of another page)
 __device__ __forceinline__ int slot_of(const TablesParams &P, int r, int at)
 {
-    return P.b.table[(size_t)r * P.b.stride + at / P.pg.page] * P.pg.page + at % P.pg.page;
+    const int page = P.b.table[(size_t)r * P.b.stride + at / P.pg.page];
+    return (unsigned)page < (unsigned)P.pg.n_pages ? page * P.pg.page + at % P.pg.page : -1;
 }
 
 template <int THREADS, bool SLOTS>

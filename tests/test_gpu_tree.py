@@ -195,6 +195,27 @@ def test_page_tables_refuse_single_requests():
     assert sorted(alloc.free) == list(range(40))
 
 
+@pytest.mark.parametrize("max_rows", [80, 5000])
+def test_slots_of_block_table_entries_outside_the_pool(max_rows):
+    """Held pages that are none: their positions have a slot of -1, also where page * page_len comes back to a slot of the pool in 32 bits."""
+    page, n_pages, stride = 16, 9, 4
+    odd = [2 ** 28 + 3, -3, n_pages, -2 ** 31, 2]          # (the first: slot 48 of 2^32 + 48)
+    lens, counts = [5] * 5, [14] * 5
+    table = np.full((5, stride), -1, dtype=np.int32)
+    table[:, 0] = odd
+    g = dict(lens=i32(lens), row_start=i32([0] * 6), table=i32(table), slots=i32([-5] * max_rows), counts=i32(counts), held=i32([1] * 5),
+             free=i32([0, 1, 3, 4, 5, 6, 7, 8, -1]), free_count=i32([8]), granted=i32([-5] * 5))
+    cf.cfpp_page_tables(cf.Pages(n_pages, page, 1, 64), cf.TreeBatch.of(14, g["lens"], g["row_start"], g["table"], g["slots"]), g["counts"], g["held"],
+                        g["free"], g["free_count"], g["granted"], stream())
+    torch.cuda.synchronize()
+    slots, table = g["slots"].cpu().numpy(), g["table"].cpu().numpy()
+    assert list(g["granted"].cpu().numpy()) == [1] * 5 and list(table[:, 0]) == odd and list(table[:, 1]) == [8, 7, 6, 5, 4]
+    for r in range(5):
+        first = [2 * page + 5 + i if r == 4 else -1 for i in range(11)]
+        assert list(slots[14 * r:14 * r + 14]) == first + [(8 - r) * page + i for i in range(3)], f"request {r}"
+    assert (slots[70:] == -1).all()
+
+
 # ---- masks and positions ---------------------------------------------------------------------------
 @pytest.mark.parametrize("sizes", [[1], [26], [33, 1, 0, 32, 64, 31], [256, 255, 129], [0, 0, 3]])
 def test_tree_plan(sizes):
