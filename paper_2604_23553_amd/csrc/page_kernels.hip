@@ -239,19 +239,18 @@ hipError_t launch_page_append_slabs(const PageDims &pg, __half *pool, const __ha
 // ---- either side of a stack's step ---------------------------------------------------------------
 __global__ void __launch_bounds__(256) k_tree_rope(TreeBatch b, const float2 *rope, int half, int max_seq, float2 *rope_rows, unsigned *err)
 {
-    const int i = blockIdx.x * 256 + threadIdx.x, row = i / half, j = i - row * half;
+    const int i = blockIdx.x * 256 + threadIdx.x, per = max(half, 1), row = i / per, j = i - row * per;
     if (row >= b.max_rows) return;
     int pos = b.slots[row] >= 0 ? b.positions[row] : 0;
     if (pos < 0 || pos >= max_seq) {
         *err = kErrBadPos;
         pos = 0;
     }
-    rope_rows[i] = rope[(size_t)pos * half + j];
+    if (half > 0) rope_rows[i] = rope[(size_t)pos * half + j];             // (positions count where nothing is rotated too)
 }
 hipError_t launch_tree_rope(const TreeBatch &b, const float2 *rope, int half, int max_seq, float2 *rope_rows, unsigned *err, hipStream_t s)
 {
-    if (half == 0) return hipSuccess;
-    hipLaunchKernelGGL(k_tree_rope, dim3((unsigned)(((long long)b.max_rows * half + 255) / 256)), dim3(256), 0, s, b, rope, half, max_seq, rope_rows, err);
+    hipLaunchKernelGGL(k_tree_rope, dim3((unsigned)(((long long)b.max_rows * (half > 0 ? half : 1) + 255) / 256)), dim3(256), 0, s, b, rope, half, max_seq, rope_rows, err);
     return hipGetLastError();
 }
 

@@ -121,3 +121,31 @@ def test_stack_tree_of_values_that_are_not_finite(orc, lens, sizes):
         assert 1 < kinds[1] < sizes[0] - 1
     finally:
         m.close()
+
+
+@pytest.mark.parametrize("max_rows", [8, 300])
+def test_far_positions_without_rotary_dimensions(orc, max_rows):
+    """A position outside [0, max_seq) raises the flag whatever the rotation."""
+    shape = synth.ModelShape(512, 8, 64, 0, 2048, n_layers=2, name="neox-h512-r0")
+    m = Model(shape, 1, 16, 5, max_rows, 4, 3, max_seq=64)
+    try:
+        kvs = m.fill_cache([30], 6)
+        m.set_trees([[-1, 0, 0, 2]])
+        X = synth.x_input(shape, 13, batch=4)
+        m.x[:4] = dev(X)
+        m.enqueue_tables()
+        m.enqueue_stack()
+        torch.cuda.synchronize()
+        cf.cfpp_device_error(m.ctx)
+        check_step(orc, m, kvs, [30], X, m.out.cpu().numpy())
+        for position in (64, -1):
+            m.positions[3] = position
+            m.enqueue_stack()
+            with pytest.raises(cf.CfppError) as e:
+                cf.cfpp_device_error(m.ctx)
+            assert e.value.status == -6
+        m.positions[3] = 63
+        m.enqueue_stack()
+        cf.cfpp_device_error(m.ctx)
+    finally:
+        m.close()
