@@ -375,7 +375,9 @@ cfpp_status cfpp_generate_capture(cfpp_ctx *ctx, const void *const *packed_layer
  * Everything that varies from step to step is device memory, read by the kernels:
  * a captured graph follows it.  Nothing here raises the device error flag
  * (cfpp_stack_tree's positions apart): a request that cannot be served has
- * granted[r] = 0 and slots of -1, and its rows are left out by the calls behind.
+ * granted[r] = 0 and slots of -1, and its rows are left out by the calls behind.  One of more
+ * than max_nodes rows has pages and slots, but cfpp_tree_plan leaves it out, and with it the
+ * attention, cfpp_stack_tree and cfpp_tree_accept; cfpp_page_append goes by slots alone.
  * No call may overlap in time with another one that writes what it uses.
  *
  * One layer's pool (DEVICE, cfpp_page_pool_bytes(pages) bytes):
@@ -508,12 +510,13 @@ cfpp_status cfpp_tree_accept(const cfpp_pages *pages, void *const *kv_pools, int
  *              the configuration's
  *   batch    : after cfpp_page_tables and cfpp_tree_plan (n_heads: the
  *              configuration's); at most 4096 max_rows, all of which the products run over
- *   x, out   : DEVICE fp16 [max_rows][hidden]; rows without a slot are not
- *              written; out must not overlap x
+ *   x, out   : DEVICE fp16 [max_rows][hidden]; rows without a slot, and those of requests that
+ *              the plan leaves out, are not written and put nothing into the pools; out must
+ *              not overlap x
  *   scratch  : DEVICE, 256-byte aligned, at least cfpp_tree_scratch_bytes(cfg, max_rows)
  *              bytes; contents undefined afterwards
- * A position outside [0, cfg.max_seq) raises the context's device error flag, and its row
- * is of no use.  Any launch mode.  CFPP_EUNSUPPORTED for shapes that cfpp_stack_prefill_gemm refuses.
+ * A position outside [0, cfg.max_seq) of a row that takes part raises the context's device error
+ * flag, and the row is of no use.  Any launch mode.  CFPP_EUNSUPPORTED for shapes that cfpp_stack_prefill_gemm refuses.
  * Rows of cfpp_lm_next's logits and cfpp_tree_accept follow.  Asynchronous on `stream`;
  * may be captured. */
 size_t cfpp_tree_scratch_bytes(const cfpp_config *cfg, int32_t max_rows);

@@ -1228,8 +1228,8 @@ extern "C" cfpp_status cfpp_tree_accept(const cfpp_pages *pages, void *const *kv
 }
 
 // Scratch of a stack's step over the rows of trees, byte offsets: that of a prompt's pass, then the layer's new K and V rows in
-// slabs, a rotary line for each row, and the output of all rows.
-struct TreeScratch { size_t kv, rope, out, total; int rows; };
+// slabs, a rotary line and a slot for each row, and the output of all rows.
+struct TreeScratch { size_t kv, rope, slots, out, total; int rows; };
 static TreeScratch tree_scratch(const Dims &dm, int max_rows)
 {
     TreeScratch S;
@@ -1238,6 +1238,7 @@ static TreeScratch tree_scratch(const Dims &dm, int max_rows)
     auto take = [&](size_t bytes) { const size_t at = o; o = align_up(o + bytes, 256); return at; };
     S.kv = take((size_t)2 * S.rows * dm.h * sizeof(__half));
     S.rope = take((size_t)S.rows * (dm.r / 2) * sizeof(float2));
+    S.slots = take((size_t)S.rows * sizeof(int));
     S.out = take((size_t)S.rows * dm.h * sizeof(__half));
     S.total = o;
     return S;
@@ -1295,8 +1296,15 @@ extern "C" cfpp_status cfpp_stack_tree(cfpp_ctx *ctx, const void *const *packed_
     float2 *rope_rows = reinterpret_cast<float2 *>(sc + S.rope);
     P.rope = rope_rows;
     P.tree = &T;
-    HIP_OK(launch_tree_rope(T.b, reinterpret_cast<const float2 *>(ctx->ws + ctx->wl.rope), dm.r / 2, dm.max_seq, rope_rows,
-                            reinterpret_cast<unsigned *>(ctx->ws + ctx->wl.sync) + kSyncErr, s));
+    TreeRows R;
+    R.plan = T.plan; R.key = tree_plan_layout(T.pg, dm.H, batch->n_requests, n, batch->max_nodes, batch->table_stride).key;
+    R.rope = reinterpret_cast<const float2 *>(ctx->ws + ctx->wl.rope);
+    R.half = dm.r / 2; R.max_seq = dm.max_seq;
+    R.rope_rows = rope_rows;
+    R.slots = reinterpret_cast<int *>(sc + S.slots);
+    R.err = reinterpret_cast<unsigned *>(ctx->ws + ctx->wl.sync) + kSyncErr;
+    HIP_OK(launch_tree_rope(T.pg, T.b, R, s));
+    T.b.slots = R.slots;                                   // (rows of requests that the plan leaves out have none from here on)
     pf_plan_pass(P);
     if (!pf_plan_narrow(P, ctx->n_cu)) { pf_plan_middle(P); pf_plan_long(P); }
     float *xa = reinterpret_cast<float *>(sc + pl.xres), *xb = reinterpret_cast<float *>(sc + pl.xnext);
@@ -1309,7 +1317,7 @@ extern "C" cfpp_status cfpp_stack_tree(cfpp_ctx *ctx, const void *const *packed_
         P.xnext = (l & 1) ? xa : xb;
         HIP_OK(launch_pf_layer(P, s));
     }
-    HIP_OK(launch_tree_out(batch->slots, n, P.out, static_cast<__half *>(out), dm.h, s));
+    HIP_OK(launch_tree_out(R.slots, n, P.out, static_cast<__half *>(out), dm.h, s));
     return CFPP_OK;
 }
 

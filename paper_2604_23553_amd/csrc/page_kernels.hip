@@ -237,20 +237,32 @@ hipError_t launch_page_append_slabs(const PageDims &pg, __half *pool, const __ha
 }
 
 // ---- either side of a stack's step ---------------------------------------------------------------
-__global__ void __launch_bounds__(256) k_tree_rope(TreeBatch b, const float2 *rope, int half, int max_seq, float2 *rope_rows, unsigned *err)
+__global__ void __launch_bounds__(256) k_tree_rope(PageDims pg, TreeBatch b, TreeRows R)
 {
-    const int i = blockIdx.x * 256 + threadIdx.x, per = max(half, 1), row = i / per, j = i - row * per;
+    const int i = blockIdx.x * 256 + threadIdx.x, per = max(R.half, 1), row = i / per, j = i - row * per;
     if (row >= b.max_rows) return;
-    int pos = b.slots[row] >= 0 ? b.positions[row] : 0;
-    if (pos < 0 || pos >= max_seq) {
-        *err = kErrBadPos;
+    int lo = 0, hi = b.requests - 1;                       // the last request that begins at this row or before it
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (b.row_start[mid] <= row) lo = mid;
+        else hi = mid - 1;
+    }
+    int first;
+    const int n = tree_rows(pg, b, lo, first);
+    const TreePlanHead &plan = *reinterpret_cast<const TreePlanHead *>(R.plan);
+    const bool served = plan.key == R.key && plan.items > 0 && row >= first && row < first + n;
+    const int slot = served ? b.slots[row] : -1;
+    if (j == 0) R.slots[row] = slot;
+    int pos = slot >= 0 ? b.positions[row] : 0;
+    if (pos < 0 || pos >= R.max_seq) {
+        *R.err = kErrBadPos;
         pos = 0;
     }
-    if (half > 0) rope_rows[i] = rope[(size_t)pos * half + j];             // (positions count where nothing is rotated too)
+    if (R.half > 0) R.rope_rows[i] = R.rope[(size_t)pos * R.half + j];     // (positions count where nothing is rotated too)
 }
-hipError_t launch_tree_rope(const TreeBatch &b, const float2 *rope, int half, int max_seq, float2 *rope_rows, unsigned *err, hipStream_t s)
+hipError_t launch_tree_rope(const PageDims &pg, const TreeBatch &b, const TreeRows &R, hipStream_t s)
 {
-    hipLaunchKernelGGL(k_tree_rope, dim3((unsigned)(((long long)b.max_rows * (half > 0 ? half : 1) + 255) / 256)), dim3(256), 0, s, b, rope, half, max_seq, rope_rows, err);
+    hipLaunchKernelGGL(k_tree_rope, dim3((unsigned)(((long long)b.max_rows * (R.half > 0 ? R.half : 1) + 255) / 256)), dim3(256), 0, s, pg, b, R);
     return hipGetLastError();
 }
 

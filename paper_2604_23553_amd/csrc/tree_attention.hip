@@ -75,15 +75,6 @@ TreePlanLayout tree_plan_layout(const PageDims &pg, int n_heads, int requests, i
     return L;
 }
 
-// Rows of a request that take part: all or none
-__device__ __forceinline__ int tree_rows(const PageDims &pg, const TreeBatch &b, int r, int &first)
-{
-    first = b.row_start[r];
-    const int n = b.row_start[r + 1] - first, len = b.lens[r];
-    if (n <= 0 || n > b.max_nodes || first < 0 || first + n > b.max_rows || len < 0 || (long long)len + n > (long long)b.stride * pg.page) return 0;
-    return b.slots && b.slots[first] < 0 ? 0 : n;
-}
-
 // A request's masks by pointer doubling: after round k a node's words hold its 2^k nearest ancestors and itself, and the node that stands
 // 2^k above it is known.  One workgroup has a request, one thread a node.
 __device__ __forceinline__ void tree_masks(const PageDims &pg, const TreeBatch &b, int r)

@@ -43,6 +43,15 @@ struct AcceptParams {
 };
 hipError_t launch_tree_accept(const AcceptParams &P, int n_layers, hipStream_t s);
 
+// Rows of a request that take part, in the plan and so in all that follows it: all or none
+__device__ __forceinline__ int tree_rows(const PageDims &pg, const TreeBatch &b, int r, int &first)
+{
+    first = b.row_start[r];
+    const int n = b.row_start[r + 1] - first, len = b.lens[r];
+    if (n <= 0 || n > b.max_nodes || first < 0 || first + n > b.max_rows || len < 0 || (long long)len + n > (long long)b.stride * pg.page) return 0;
+    return b.slots && b.slots[first] < 0 ? 0 : n;
+}
+
 // ---- the attention and its plan --------------------------------------------------------------
 // Query rows (a node's heads that share a key head, nodes one after the other) go to workgroups in tiles of 16, 32, 64 or 128, positions in pieces.
 // A plan: the work list of a key head (TreeItem), arrival counters and the sums of the tiles that are cut into pieces.
@@ -90,8 +99,18 @@ struct TreePass {
     char *plan;
 };
 hipError_t launch_page_append_slabs(const PageDims &pg, __half *pool, const __half *kv, int rows, const int *slots, int n_rows, hipStream_t s);
-// rotary table by row: rope_rows[row] = rope[positions[row]]; rows without a slot take position 0, positions outside the table raise the error flag
-hipError_t launch_tree_rope(const TreeBatch &b, const float2 *rope, int half, int max_seq, float2 *rope_rows, unsigned *err, hipStream_t s);
+// What a step needs of each row: its slot, -1 where its request takes no part in the plan, and its line of the rotary table, rope[positions[row]]; rows
+// without a slot take position 0, positions outside the table raise the error flag
+struct TreeRows {
+    const char *plan;
+    int key;                           // of the plan that belongs to the batch
+    const float2 *rope;
+    int half, max_seq;
+    float2 *rope_rows;
+    int *slots;
+    unsigned *err;
+};
+hipError_t launch_tree_rope(const PageDims &pg, const TreeBatch &b, const TreeRows &R, hipStream_t s);
 // rows that have a slot
 hipError_t launch_tree_out(const int *slots, int n_rows, const __half *from, __half *to, int h, hipStream_t s);
 struct PfParams;

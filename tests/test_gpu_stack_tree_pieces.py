@@ -149,3 +149,39 @@ def test_far_positions_without_rotary_dimensions(orc, max_rows):
         cf.cfpp_device_error(m.ctx)
     finally:
         m.close()
+
+
+@pytest.mark.parametrize("max_rows", [40, 300])
+def test_requests_that_the_plan_leaves_out(orc, max_rows):
+    """A request of more than max_nodes nodes has pages and slots, but no masks and positions: its outputs and its slots stay as they were, its positions, of
+    whatever step, raise no flag, and the others are served.  A plan of other sizes serves nobody."""
+    shape, lens = H512, [20, 5, 10]
+    m = Model(shape, 3, 16, 6, max_rows, 12, 3, max_seq=64)
+    try:
+        kvs = m.fill_cache(lens, 6)
+        rng = np.random.default_rng(9)
+        m.set_trees([tree_ref.random_tree(rng, n) for n in (12, 14, 5)])
+        X = synth.x_input(shape, 13, batch=31)
+        m.x[:31] = dev(X)
+        m.positions.fill_(10 ** 6)
+        m.enqueue_tables()
+        m.enqueue_stack()
+        torch.cuda.synchronize()
+        assert (m.granted == 1).all() and (m.slots[:31] >= 0).all()
+        cf.cfpp_device_error(m.ctx)
+        got, slots = m.out.cpu().numpy(), m.slots.cpu().numpy()
+        assert (got[12:26] == 7.0).all()
+        for l in range(shape.n_layers):
+            assert all(np.isnan(m.row(l, int(slot))).all() for slot in slots[12:26])
+        m.trees[1] = []
+        check_step(orc, m, kvs, lens, X, got)
+        before = [p.clone() for p in m.pools]
+        m.batch.max_nodes = 11
+        m.out.fill_(7.0)
+        m.enqueue_stack()
+        torch.cuda.synchronize()
+        cf.cfpp_device_error(m.ctx)
+        assert (m.out == 7.0).all()
+        assert all(torch.equal(a.view(torch.int16), b.view(torch.int16)) for a, b in zip(before, m.pools))
+    finally:
+        m.close()
