@@ -126,25 +126,26 @@ __device__ __forceinline__ void tree_work(const PageDims &pg, const TreeBatch &b
     if (threadIdx.x == 0) cuts = 0;
     if (threadIdx.x < CLASSES) classes[threadIdx.x] = 0;
     __shared__ long long wave_total[kTaWaves];
-    __shared__ bool wave_falls[kTaWaves];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, R = b.requests, each = (R + kTaThreads - 1) / kTaThreads;
     const int lo = min(tid * each, R), hi = min(lo + each, R);
     int first;
     long long total = 0;
+    constexpr long long FALLS = 1ll << 53;                 // (512 tiles of 2^30 positions for 4096 requests are less than half of it, it times 256 threads fits)
     bool falls = false;
     for (int r = lo; r < hi; ++r) {
-        falls = falls || b.row_start[r + 1] < b.row_start[r];
         const int n = tree_rows(pg, b, r, first), t = (n * group + L.tile_rows - 1) / L.tile_rows;
+        falls = falls || b.row_start[r + 1] < first;
         place[r] = t;
         items[r] = n > 0 ? b.lens[r] + n : 0;              // (positions, for the moment)
         total += (long long)t * items[r];
     }
+    if (falls) total += FALLS;
     for (int m = 1; m < 64; m <<= 1) total += __shfl_xor(total, m, 64);
-    falls = __any(falls);
-    if (lane == 0) { wave_total[wave] = total; wave_falls[wave] = falls; }
+    if (lane == 0) wave_total[wave] = total;
     __syncthreads();
     total = 0;
-    for (int w = 0; w < kTaWaves; ++w) { total += wave_total[w]; falls = falls || wave_falls[w]; }
+    for (int w = 0; w < kTaWaves; ++w) total += wave_total[w];
+    falls = total >= FALLS;
     const int want = L.tile_rows <= 32 && total * 2 <= (long long)kTaShort * L.want ? (L.want + 1) / 2 : L.want;
     const long long C = max((total + want - 1) / want, (long long)kTaStep);
     // the nearest number of pieces: they come to 4 / 3 of `want` at most beside those of the tiles that stay whole

@@ -544,7 +544,7 @@ def test_values_that_are_not_finite_in_pieces(heads, sizes):
         fine = np.isfinite(e)
         assert np.array_equal(np.isnan(g), np.isnan(e)), f"request {r}: NaN in other places"
         assert np.array_equal(g[~fine & ~np.isnan(e)], e[~fine & ~np.isnan(e)])
-        assert (np.abs(g - e)[fine] <= (np.abs(e) * 2.0 ** -11 + 2.0 ** -25 + off * (1 + 2.0 ** -11))[fine]).all(), f"request {r}"
+        assert (np.abs(g[fine] - e[fine]) <= np.abs(e[fine]) * 2.0 ** -11 + 2.0 ** -25 + off[fine] * (1 + 2.0 ** -11)).all(), f"request {r}"
     assert np.isfinite(first[:s.rows]).any() and np.isnan(first[:s.rows, :s.H * s.d]).any()
     assert np.array_equal(first.view(np.uint16), s.attention().view(np.uint16)), "the bits change from call to call"
 
