@@ -434,15 +434,17 @@ size_t cfpp_tree_plan_bytes(const cfpp_pages *pages, int32_t n_heads, int32_t n_
 /* Pages for counts[r] new rows behind the lens[r] cached positions of every request.
  * With target_r = ceil((lens[r] + counts[r]) / page_len) and held[r] pages at entries
  * 0 .. held[r] - 1 of its block table, a request takes target_r - held[r] pages or
- * gives back the last held[r] - target_r: lens = counts = 0 gives back all.
+ * gives back the last held[r] - target_r: lens = counts = 0 gives back all, if granted.
  *   held       : DEVICE int32 [n_requests], updated
  *   free_pages : DEVICE int32 [n_pages], *free_count of them free.  Pages are taken from the end of the list, for requests in
  *                order; those given back follow what is left, in order, and can be
  *                taken from the next call on
  *   granted    : DEVICE int32 [n_requests]: 1, or 0 where the pages that this request
  *                and those before it need are more than the free ones (and it needs any),
- *                the block table is too short, lens or counts negative, or the rows pass
- *                max_rows: such a request neither takes nor gives, and its slots are -1
+ *                the block table is too short, lens or counts negative, or the counts of the
+ *                requests up to this one come to more than max_rows (whatever its own: a count
+ *                too large for the batch leaves out every request behind it, those of no rows
+ *                among them): such a request neither takes nor gives, and its slots are -1
  * Uses lens; writes block_table (taken pages; -1 in place of those given back),
  * row_start (the sums of counts, up to max_rows; a negative one counts as 0) and slots
  * (-1 too for a position whose page, held or from the list, is none of the pool's).
@@ -517,8 +519,8 @@ cfpp_status cfpp_tree_accept(const cfpp_pages *pages, void *const *kv_pools, int
  *              bytes; contents undefined afterwards
  * A position outside [0, cfg.max_seq) of a row that takes part raises the context's device error
  * flag, and the row is of no use.  Any launch mode.  CFPP_EUNSUPPORTED for shapes that cfpp_stack_prefill_gemm refuses.
- * Rows of cfpp_lm_next's logits and cfpp_tree_accept follow.  Asynchronous on `stream`;
- * may be captured. */
+ * The picks and cfpp_tree_accept follow; cfpp_lm_next gives one row's pick to a call (with a
+ * *pos_dev of its own, which it advances).  Asynchronous on `stream`; may be captured. */
 size_t cfpp_tree_scratch_bytes(const cfpp_config *cfg, int32_t max_rows);
 cfpp_status cfpp_stack_tree(cfpp_ctx *ctx, const void *const *packed_layers, void *const *kv_pools,
                             const cfpp_pages *pages, const cfpp_tree_batch *batch, const void *x,

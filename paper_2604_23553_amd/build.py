@@ -22,7 +22,7 @@ HEADERS = ["layout.h", "device_utils.h", "decode_params.h", "attention_common.h"
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
-    # packed-fp32 VALU forms are kept out of the generated code on the test machines
+    # packed-fp32 VALU forms are kept out of the generated code on this hardware
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
     "-Wall", "-Wno-unused-function",
 ]

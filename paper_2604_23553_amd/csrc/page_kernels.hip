@@ -11,8 +11,9 @@ namespace cfpp {
 // target_r = ceil((len_r + count_r) / page); a request takes target - held pages from the end of the free list or gives back
 // held - target.  Three running sums over the requests (pages taken, pages given back, rows) say which entry of the free list and
 // which rows are whose.  One workgroup has all requests: every sum needs all of the ones before it, and 4096 requests are four to a thread.
-// A chain of dependent reads, not bytes, bounds it: lengths, sums, list, table (one request 3.7 us, 4096 10.0 and 4.0 for the launch of their slots;
-// the reads alone are 80 KB).
+// A chain of dependent reads, not bytes, bounds it: lengths, sums, and for the pages that move a search of their request, the list, the table.  One request
+// 3.7 us, 4.0 where it takes a page; 4096 requests 9.8 us where no page moves, 18.1 where 8428 are taken, 20.4 where they are given back (160 KB of lists
+// and tables); the launch of their slots 4.1, and 15.3 where all of 131 thousand rows are nobody's, which one workgroup writes.
 constexpr int kTablesEach = 4;           // requests of a thread
 // Rows whose slots it writes itself, in a launch less (a launch is about 4 us): 4096 are four to a thread of 1024 or sixteen to one of 256
 constexpr int kTablesRows = 4096;
@@ -199,7 +200,8 @@ hipError_t launch_page_tables(const TablesParams &P, hipStream_t s)
 
 // ---- append ------------------------------------------------------------------------------------
 // A wavefront has 8 rows and 128 bytes of each, 16 to a lane: whole lines are read, and where the rows' slots follow one another 256 bytes in a
-// run are written.  Bound by the bytes: 4096 rows of hidden 4096, 134 MB read and written, 27.7 us, 4.85 TB/s, what a large copy reaches.  `from`: where the pieces of K and V rows lie.
+// run are written.  Bound by the bytes: 4096 rows of hidden 4096, 134 MB read and written, 27.4 us, 4.9 TB/s, where a large copy reaches 5.14.  `from`: where the
+// pieces of K and V rows lie.
 struct AppendFrom {
     const __half *k, *v;
     long long row, head;       // halves from row to row, from head to head
@@ -283,8 +285,9 @@ hipError_t launch_tree_out(const int *slots, int n_rows, const __half *from, __h
 // A workgroup has one request and one of the K and V arrays of the layers; each walks the tree by itself (a step: every thread
 // looks whether its node is a child that agrees, the lowest one goes on).  Node path[j] >= j moves to index j: rows are moved in
 // ascending order, a block of pieces at a time, read before written: 8 loads to a thread are in flight, and the walk is done again by each workgroup
-// because a launch in between would cost more than its few steps in LDS.  48 requests of up to 63 nodes, 16 layers of hidden 4096,
-// are bound by the bytes of the nodes that move (155 MB, 35 - 39 us, 4.0 - 4.4 TB/s); 26 nodes of one request by the walk's steps (6.2 us).
+// because a launch in between would cost more than its few steps in LDS.  48 requests of up to 63 nodes, 16 layers of hidden 4096, of which
+// some 100 nodes move, take 35 - 40 us for 27 MB read and as many written: a row lies in runs of 32 bytes, and the lines of 128 that hold them are 99 MB
+// (counted; 30 MB written), so that 3.3 - 3.7 TB/s flow.  26 nodes of one request are bound by the walk's steps (6.1 us).
 __global__ void __launch_bounds__(256) k_tree_accept(AcceptParams P, int n_layers)
 {
     __shared__ int parent[kTreeMaxNodes], token[kTreeMaxNodes], pick[kTreeMaxNodes], slot[kTreeMaxNodes], path[kTreeMaxNodes], child[2];

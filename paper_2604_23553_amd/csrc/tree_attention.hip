@@ -14,13 +14,13 @@
 // Weights enter the matrix instruction as two fp16 values, head and remainder, 2^9 times their size: 2^-21 of each and 2^-33 of the largest, as near
 // as the sums in 32 bits are.  Queries and keys are fp16 as they come.
 //
-// Bound and measured (repeated launches, the join included): few query rows by the K and V that are read - one token of 8 requests behind 8000
-// positions of hidden 4096 103 us, 5.7 TB/s; 64 requests of up to 9 nodes behind up to 3000, four query heads to a key head, 77 us, 4.8 TB/s; 16 of 30
-// behind 2500 of hidden 2560 71 us, 5.3 TB/s - by the launches and one piece's way through them where a single request is short (one token
-// behind 128 positions 9.5 us, 26 behind 4096 18 us).  Many query rows are bound by issue: 8 requests of 200 to 256 nodes behind 6000 to 8200 of
-// hidden 4096 take 401 - 430 us by the card, 230 GFLOP of the formula's own, 413 issued with the remainders, the sums of the weights and the rows that
-// fill tiles: 0.96 - 1.03 PFLOP/s, where a library product of 8192^3 reached 1.07.  Without the remainders it is 388 us of then 462, an error of 2^-11 to
-// each weight: not taken.
+// Bound and measured (calls in a captured graph, the join included; so are both sides of the rules below, each pair on one card): few query rows by the
+// K and V that are read - one token of 8 requests behind 1000 to 8000 positions of hidden 4096 107 us, 5.5 TB/s; 64 requests of up to 9 nodes behind up to
+// 3000, four query heads to a key head, 77 us, 4.8 TB/s; 16 of 30 behind 2500 of hidden 2560 70 us, 5.4 TB/s - by the launches and one piece's way through
+// them where a single request is short (one token behind 128 positions 6.8 us, 26 behind 4096 18.7 us).  Many query rows are bound by issue: 8 requests
+// of 200 to 256 nodes behind 6000 to 8200 of hidden 4096 take 403 - 410 us, 230 GFLOP of the formula's own, 413 issued with the remainders, the sums of the
+// weights and the rows that fill tiles: 1.0 PFLOP/s, where a library product of 8192^3 reached 1.1.  Without the remainders an earlier build took 388 of
+// 462 us, an error of 2^-11 to each weight: not taken.
 #include <hip/hip_runtime.h>
 #include <hip/hip_fp16.h>
 #include "tree_params.h"
@@ -35,18 +35,19 @@ typedef _Float16 ta_f16x8 __attribute__((ext_vector_type(8)));
 typedef unsigned ta_u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kTaThreads = 256, kTaWaves = kTaThreads / 64, kTaRow = 32, kTaStep = kTaRow * kTaWaves;
-// Positions that are not cut.  Of hidden 2560 and one token, whole / cut: behind 500 10.3 / 8.4 us, behind 900 15.5 / 9.3; a piece of 128 is one row to a
+// Positions that are not cut.  Of hidden 2560 and one token, whole / cut: behind 500 10.5 / 10.0 us, behind 900 12.0 / 9.7; a piece of 128 is one row to a
 // wavefront, and joining pieces costs about what a second row does.
 constexpr int kTaWhole = 256;
-// Workgroups that the pieces aim at, two to a CU.  With 256 / 512 / 768 / 1024: one token of 8 requests behind 8000 120 / 104 / 107 / 104 us, 26 nodes
-// behind 4096 18 / 22 / 28 / 30 (see kTaShort); with 256 / 512 / 1024 / 1536, 64 nodes behind 8000 of hidden 4096 38.0 / 37.6 / 49.5 / 54.9, 4 requests of 60 nodes
-// with four query heads to a key head 54 / 48.5 / 60 / 74.  Two wavefronts more to each SIMD in workgroups of eight instead: 112 of 104, 20.5 of 18.4.
+// Workgroups that the pieces aim at, two to a CU.  With 256 / 512 / 768 / 1024 / 1536: one token of 8 requests behind 8000 117 / 107 / 107 / 104 / 103 us, 64 requests of
+// up to 9 nodes 84 / 77 / 85 / 83 / 91, 8 of 256 406 / 405 / 435 / 428 / 439, 64 nodes behind 8000 of hidden 4096 34.6 / 37.7 / 43.7 / 46.9 / 54, 4 requests of 60 nodes
+// with four query heads to a key head 48.5 / 44.5 / 55 / 58 / 72.  Two wavefronts more to each SIMD in workgroups of eight instead, in an earlier build: 112 of 104, 20.5 of 18.4.
 constexpr int kTaWgs = 512;
-// Up to 32 query rows whose pieces would have half as many positions or fewer are given half the workgroups: 26 nodes behind 4096 22.2 / 18.1 us, one token
-// there 16.0 / 14.6; tiles of 128 rows are left at kTaWgs, where half of them costs 54 us instead of 48.5 (the 4 requests above).
+// Up to 32 query rows whose pieces would have half as many positions or fewer are given half the workgroups: 26 nodes behind 4096 22.6 / 18.5 us, one token
+// there 15.9 / 14.5; tiles of 128 rows are left at kTaWgs, where half of them costs 48.5 us instead of 44.5 (the 4 requests above).
 constexpr int kTaShort = 1024;
 // Up to so many query rows to a tile its last workgroup adds the pieces, above it a launch does, which has all CUs for the up to 128 rows of sums: 64 nodes
-// behind 8000 49 / 38 us, 200 behind 300 25.5 / 16.9, 26 behind 500 14.1 / 12.6.  With 16 rows the launch costs more: one token behind 4096 15.9 / 17.8.
+// behind 8000 49 / 38 us, 200 behind 300 25.3 / 16.5, 26 behind 500 14.2 / 13.1, 26 behind 4096 19.3 / 18.6.  With 16 rows the launch costs more: one token behind
+// 4096 14.4 / 15.7.
 constexpr int kTaLastJoins = 16;
 constexpr float kTaLowest = -3.402823466e38f;
 
@@ -114,7 +115,8 @@ __device__ __forceinline__ void tree_masks(const PageDims &pg, const TreeBatch &
 
 // The work list, by one workgroup: with tiles_r tiles of query rows, a request's positions are cut into equal pieces of about C, multiples of what the
 // wavefronts take at a time, so that all pieces come to about `want`.  The requests of the longest pieces come first, in classes of an eighth of C, so that
-// short ones fill the end: 64 requests of up to 9 nodes, lengths from 33 to 3000, 86 us in the requests' order and 77 so, of 16 nodes each 106 and 95.
+// short ones fill the end: 64 requests of up to 9 nodes, lengths from 33 to 3000, 87 us in the requests' order and 78 so, of 16 nodes each 109 and 96 (but one
+// token of 8 requests 104 and 107).
 // L.tiles bounds the tiles of rows that are one request's each.  Where row_start falls, rows can be several requests', whose tiles may be more than the list
 // holds: such a batch has no items.
 __device__ __forceinline__ void tree_work(const PageDims &pg, const TreeBatch &b, int group, const TreePlanLayout &L, char *plan)
@@ -672,7 +674,7 @@ __device__ __forceinline__ void ta_narrow(const TreeAttention &P, const TreePlan
     const TreeItem &it = w.it;
     const int words = tree_words(P.b.max_nodes);
     // rows on their way in registers: as many as fit beside the sums (two of head_dim 128 with 32 query rows go to memory).  Bypassing the caches pays: no
-    // row is read again but by the tiles of its own request (loads kept there: the 64 requests 100 of 94 us, one token of 8 behind 8000 117 of 107).
+    // row is read again but by the tiles of its own request (loads kept there: the 64 requests 86 of 77 us, one token of 8 behind 8000 117 of 107).
     constexpr int AHEAD = QT == 1 || D <= 80 ? 2 : 1;
     TaRow<D> r[AHEAD];
     const int row0 = it.t0 / kTaRow + wave;
@@ -799,7 +801,7 @@ __device__ __forceinline__ void ta_narrow(const TreeAttention &P, const TreePlan
 // A row of 32 positions goes through LDS for all four wavefronts, K and V as they lie in the pool, straight from memory: a ring of kTwRing
 // rows, one granule of K or V of each to a wavefront, waited for by count, and one barrier a row.  A wavefront has 16 QT query rows and all positions
 // of the piece, so nothing is joined but the pieces.  Positions past the piece's end read its last one again: their weights are zero.
-// A workgroup's rows come through LDS, not registers, because four wavefronts read each of them: 607 -> 576 us (8 requests of 256 nodes).  A K value is
+// A workgroup's rows come through LDS, not registers, because four wavefronts read each of them: 607 -> 576 us (8 requests of 256 nodes; builds of then).  A K value is
 // then used by 32 query rows and a V value by as many, so the LDS reads stay below the matrix instructions' time; scores a row ahead took 495 to 475,
 // sums side by side 444 to 420.  (With every load of one row that the L2 holds: 446 to 404, so waiting for memory is a tenth at most.)
 constexpr int kTwRing = 4;
@@ -887,7 +889,7 @@ __device__ __forceinline__ void ta_wide(const TreeAttention &P, const TreePlanLa
     };
     int at = 0;
     tw_arrive<(kTwRing - 2) * Lds::loads>();
-    // A wavefront without a query row of its own only loads and waits with the others (64 requests of 36 query rows: 103 -> 98 us).
+    // A wavefront without a query row of its own only loads and waits with the others (64 requests of 36 query rows: 91.6 -> 88.8 us).
     if (wave * RW >= w.rows) {
         for (int row = first; row * kTaRow < it.t1; ++row) {
             tw_arrive<(kTwRing - 3) * Lds::loads>();
@@ -1013,7 +1015,7 @@ __global__ void __launch_bounds__(kTaThreads, 2) k_tree_attention(TreeAttention 
 }
 
 // The pieces of many query rows are added by a launch of its own, 1024 sums to a workgroup at a time: for one workgroup they are up to 16384.
-constexpr int kTaJoinWgs = 1024;                          // (256 / 512 / 1024: 4 requests of 60 nodes 49 / 45 / 45 us, 64 of 9 81 / 79.5 / 78)
+constexpr int kTaJoinWgs = 1024;                          // (256 / 512 / 1024: 4 requests of 60 nodes 50 / 47 / 46 us, 64 of 9 81 / 79 / 78)
 template <int D, int TQ, bool STACK>
 __global__ void __launch_bounds__(kTaThreads) k_tree_join(TreeAttention P, TreePlanLayout L, const char *plan)
 {

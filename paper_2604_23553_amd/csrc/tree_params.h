@@ -68,9 +68,9 @@ struct TreePlanLayout {
     size_t items, cut, counters, sums, total;   // byte offsets
 };
 // The smallest tile that has a request's query rows, or 128.  Tiles of 64 and 128 rows read K and V once where tiles of 32 read them twice or more: 64
-// requests of 16 nodes, four query heads to a key head, 108 us with tiles of 64 and 132 with 32, 36 rows to a request 101 and 125, 256 rows 607 with 128
-// and 885 with 32 (both then).  Requests of fewer rows than the tile run as if it were smaller, so a ragged batch loses little: up to 36 rows, of which most
-// have fewer, 86 and 82.
+// requests of 16 nodes, four query heads to a key head, 98 us with tiles of 64 and 118 with 32, 36 rows to a request 88 and 107, 8 requests of up to 256 rows 405
+// with 128, 480 with 64 and 758 with 32.  Requests of fewer rows than the tile run as if it were smaller, so a ragged batch loses nothing: up to 36 rows, of
+// which most have fewer, 78 and 79.
 CFPP_HD int tree_tile_rows(int max_rows_of_request) { return max_rows_of_request <= 16 ? 16 : max_rows_of_request <= 32 ? 32 : max_rows_of_request <= 64 ? 64 : 128; }
 TreePlanLayout tree_plan_layout(const PageDims &pg, int n_heads, int requests, int max_rows, int max_nodes, int stride);
 
