@@ -287,11 +287,11 @@ def _plain_sample(s):
     keep &= ws >= s.min_p.double()[:, None]
     keep = (keep & (tau > 0)) | (rank == 0)
     s.kept.copy_(keep.sum(-1))
-    wk = torch.zeros_like(w).scatter_(1, order, ws * keep)
-    sums = wk.cumsum(-1)
-    token = (sums <= s.uniform.double()[:, None] * sums[:, -1:]).sum(-1).clamp(max=V - 1)
-    s.tokens.copy_(token)
-    s.probs.copy_(wk.gather(1, token[:, None])[:, 0] / sums[:, -1])
+    ws = ws * keep
+    sums = ws.cumsum(-1)
+    at = (sums <= s.uniform.double()[:, None] * sums[:, -1:]).sum(-1, keepdim=True).clamp(max=V - 1)
+    s.tokens.copy_(order.gather(1, at)[:, 0])
+    s.probs.copy_((ws.gather(1, at) / sums[:, -1:])[:, 0])
 
 
 def run(s):
@@ -365,7 +365,7 @@ def exact(case, seed):
             first = first[:int(k)] if k > 0 else first
             if p < 1:
                 first = first[:1 + np.searchsorted(np.cumsum(w[first]), p * w[first].sum())]
-            first = np.sort(first[w[first] >= m])
+            first = first[w[first] >= m]
             sums = np.cumsum(w[first])
             probs[r] = w[first[np.searchsorted(sums, u * sums[-1], side="right")]] / sums[-1]
         return {"tokens": None, "probs": torch.from_numpy(probs), "kept": None}
