@@ -188,6 +188,7 @@ def prepare(case, seed):
         s.tokens, s.kept, s.probs = i32(np.zeros(R)), i32(np.zeros(R)), f32(np.zeros(R))
         if own:
             import paper_2604_23553_amd as cf
+            s.type = {"f32": cf.TYPE_F32, "f16": cf.TYPE_F16}[case["type"]]
             s.how = cf.Sampling.of(temperature=s.temperature, top_k=s.top_k, top_p=s.top_p, min_p=s.min_p, uniform=s.uniform)
         return s
     q, kv, d = HEADS[case["heads"]]
@@ -306,7 +307,7 @@ def run(s):
         elif op == "attention":
             cf.cfpp_page8_attention(s.pages, s.type, s.pool, s.batch, s.q, HEADS[s.case["heads"]][0], s.out, stream=stream)
         else:
-            cf.cfpp_sample(s.logits, s.case["rows"], s.case["vocab"], s.how, s.tokens, s.probs, s.kept, stream=stream)
+            cf.cfpp_sample(s.logits, s.type, s.case["rows"], s.case["vocab"], s.how, s.tokens, s.probs, s.kept, stream=stream)
     elif op == "append":
         _plain_append(s)
     elif op == "read":
