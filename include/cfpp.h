@@ -526,6 +526,92 @@ cfpp_status cfpp_stack_tree(cfpp_ctx *ctx, const void *const *packed_layers, voi
                             const cfpp_pages *pages, const cfpp_tree_batch *batch, const void *x,
                             void *out, void *scratch, size_t scratch_bytes, cfpp_stream stream);
 
+/* ---- a paged cache in 8 bits ----------------------------------------------------
+ * The same pages with half the bytes: a row of K or V of one head is head_dim codes
+ * of 8 bits and its largest absolute value a, an fp16 number that is kept as it is.
+ * A code c stands for c * a / 127 (CFPP_TYPE_INT8, whole numbers) or c * a / 448
+ * (CFPP_TYPE_E4M3, floating point with three fraction bits).  Pages, block tables,
+ * slots and plans are those of the drafted trees: cfpp_page_tables and
+ * cfpp_tree_plan serve both kinds of pools, and a decode step of many requests is
+ *   cfpp_page_tables (counts 1) -> cfpp_tree_plan (max_nodes 1, parents -1)
+ *   -> per layer cfpp_page8_append -> cfpp_page8_attention -> logits -> cfpp_sample
+ * Sequences with shorter pages lose nothing; no call raises the device error flag. */
+#define CFPP_TYPE_F16  1
+#define CFPP_TYPE_F32  2
+#define CFPP_TYPE_INT8 3
+#define CFPP_TYPE_E4M3 4
+
+/* One layer's pool (DEVICE, cfpp_page8_pool_bytes(pages) bytes, 16-byte aligned):
+ *     bytes [n_pages][n_kv_heads][page_len/16][32 * head_dim + 64]
+ * The last axis is 16 positions t = 4 T + i of a head:
+ *     K codes [T][head_dim/16][i][16]    V codes [head_dim][16 positions]
+ *     a of the K rows, fp16 [16]         a of the V rows, fp16 [16]
+ * It needs no initialisation.  Returns 0 if `pages` is invalid. */
+size_t cfpp_page8_pool_bytes(const cfpp_pages *pages);
+
+/* cfpp_page_append for a pool of 8-bit codes of `type` (INT8 or E4M3): code = 127 x / a
+ * or 448 x / a, rounded to the nearest, ties to even.  A row with a value that is infinite or
+ * NaN is NaN as a whole (a NaN, codes 0).  Slots outside the pool are skipped; the
+ * others must differ from each other: what a slot that is named twice holds afterwards is
+ * undefined.  Rows that follow one another in slots of one granule of 16 are written
+ * together. */
+cfpp_status cfpp_page8_append(const cfpp_pages *pages, int32_t type, void *kv_pool, const void *k_rows,
+                              const void *v_rows, int64_t row_stride, const int32_t *slots,
+                              int32_t n_rows, cfpp_stream stream);
+
+/* The values that slots[i] holds, rounded to fp16, into row i of k_rows and v_rows (DEVICE
+ * fp16 [n_rows][row_stride], as cfpp_page_append reads them; k_rows and v_rows may
+ * interleave but must not overlap).  Rows of slots outside the pool are left as they were.
+ * A slot may be named twice. */
+cfpp_status cfpp_page8_read(const cfpp_pages *pages, int32_t type, const void *kv_pool, const int32_t *slots,
+                            int32_t n_rows, void *k_rows, void *v_rows, int64_t row_stride, cfpp_stream stream);
+
+/* cfpp_tree_attention over a pool of 8-bit codes: the same batch, plan, masks, arguments
+ * and rules, with the codes' values, unrounded, for K and V.  Fastest where a request's nodes
+ * times the query heads of a key head are at most 16, above all one new token to a
+ * request: more are taken 16 at a time, each time with the cache read again.  Positions
+ * that a row sees have to have been written by cfpp_page8_append. */
+cfpp_status cfpp_page8_attention(const cfpp_pages *pages, int32_t type, const void *kv_pool,
+                                 const cfpp_tree_batch *batch, const void *q, int64_t q_stride,
+                                 int32_t n_heads, void *out, int64_t out_stride, cfpp_stream stream);
+
+/* ---- sampling --------------------------------------------------------------------
+ * Filters of each row (HOST struct of DEVICE pointers, 4-byte aligned, each [n_rows] or NULL).
+ * A row's order is larger logit first, lower index among equals; its weights are
+ * w = exp((logit - largest logit) / temperature).  In turn:
+ *   temperature : NULL: 1.  Not above 0: the first of the order, whatever the rest
+ *   top_k       : the first k of the order are kept; NULL, 0 or less, or as many as there are: all
+ *   top_p       : of these as many, from the first on, as it takes for their sum to reach
+ *                 top_p times the sum of all of these; one at least; NULL, 1 or more, NaN: all
+ *   min_p       : of these, those whose weight is at least min_p (at most 1) times the largest;
+ *                 NULL, 0 or less, NaN: all
+ *   uniform     : random numbers in [0, 1), the caller's; never NULL.  The first of the order
+ *                 whose running sum is above uniform times the sum of what is kept is
+ *                 drawn (below 0 or NaN count as 0; from 1 on: the last that has a weight)
+ * Logits that are minus infinity or NaN are no part of the order.  Where the largest is plus
+ * infinity, those that are weigh 1 and all others 0.  Weights are rounded to multiples of 2^-45 of
+ * the largest and added exactly: the token does not depend on how the sum is split. */
+typedef struct cfpp_sampling {
+    const float *temperature;
+    const int32_t *top_k;
+    const float *top_p, *min_p;
+    const float *uniform;
+} cfpp_sampling;
+
+/* One token for each row of logits.
+ *   logits : DEVICE, `type` CFPP_TYPE_F32 or CFPP_TYPE_F16, [n_rows][row_stride], aligned to a
+ *            value; row_stride in values, at least vocab, any number.  cfpp_lm_next's
+ *            logits_dev is one row of them
+ *   vocab  : 1 .. 2^18 logits of each row
+ *   tokens : DEVICE int32 [n_rows]: the token; -1 where the order has none
+ *   probs  : DEVICE float [n_rows] or NULL: its weight over the sum of what is kept
+ *   kept   : DEVICE int32 [n_rows] or NULL: how many tokens the filters keep
+ * Reads how's pointers when called, what they point to on the device.  Asynchronous on `stream`; may be
+ * captured. */
+cfpp_status cfpp_sample(const void *logits, int32_t type, int64_t row_stride, int32_t n_rows, int32_t vocab,
+                        const cfpp_sampling *how, int32_t *tokens, float *probs, int32_t *kept,
+                        cfpp_stream stream);
+
 /* The whole-stack kernel marks the words its workgroups exchange with a 32-bit
  * epoch that every launch advances by n_layers + 1; the library counts the
  * epochs on the host and, before they could wrap (after about 2^32 / (n_layers + 1)

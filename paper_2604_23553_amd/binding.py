@@ -68,7 +68,7 @@ def _load(kind: str) -> C.CDLL:
         for n in ("cfpp_packed_layer_bytes", "cfpp_kv_layer_bytes", "cfpp_workspace_bytes"):
             getattr(L, n).restype = C.c_size_t
             getattr(L, n).argtypes = [C.POINTER(Config)]
-        L.cfpp_page_pool_bytes.restype = L.cfpp_tree_plan_bytes.restype = L.cfpp_tree_scratch_bytes.restype = C.c_size_t
+        L.cfpp_page_pool_bytes.restype = L.cfpp_tree_plan_bytes.restype = L.cfpp_tree_scratch_bytes.restype = L.cfpp_page8_pool_bytes.restype = C.c_size_t
         L.cfpp_prefill_scratch_bytes.restype = C.c_size_t
         L.cfpp_prefill_scratch_bytes.argtypes = [C.POINTER(Config), C.c_int32]
         for n, types in _TREE_CALLS.items():
@@ -293,6 +293,19 @@ class TreeBatch(C.Structure):
                    0 if plan is None else plan.numel())
 
 
+TYPE_F16, TYPE_F32, TYPE_INT8, TYPE_E4M3 = 1, 2, 3, 4
+
+
+class Sampling(C.Structure):
+    """Mirror of `cfpp_sampling`: filters and random numbers of each row (device pointers; keep the tensors alive)."""
+    _fields_ = [(n, C.c_void_p) for n in ("temperature", "top_k", "top_p", "min_p", "uniform")]
+
+    @classmethod
+    def of(cls, uniform, temperature=None, top_k=None, top_p=None, min_p=None):
+        """From float32 tensors (top_k: int32), each [rows] or None."""
+        return cls(*[_ptr(t).value for t in (temperature, top_k, top_p, min_p, uniform)])
+
+
 def cfpp_validate_pages(pages: Pages) -> int:
     """Returns the status code (0 = supported); does not raise."""
     return int(lib().cfpp_validate_pages(C.byref(pages)))
@@ -315,6 +328,10 @@ _TREE_CALLS = {
     "cfpp_page_append": (_PAGES, _P, _P, _P, _L, _P, _I, _P),
     "cfpp_tree_attention": (_PAGES, _P, _BATCH, _P, _L, _I, _P, _L, _P),
     "cfpp_tree_accept": (_PAGES, C.POINTER(_P), _I, _BATCH, _P, _P, _P, _P, _P, _P, _P),
+    "cfpp_page8_append": (_PAGES, _I, _P, _P, _P, _L, _P, _I, _P),
+    "cfpp_page8_read": (_PAGES, _I, _P, _P, _I, _P, _P, _L, _P),
+    "cfpp_page8_attention": (_PAGES, _I, _P, _BATCH, _P, _L, _I, _P, _L, _P),
+    "cfpp_sample": (_P, _I, _L, _I, _I, C.POINTER(Sampling), _P, _P, _P, _P),
 }
 
 
@@ -354,6 +371,47 @@ def cfpp_tree_accept(pages: Pages, kv_pools, batch: TreeBatch, tokens, picks, ac
                                 _addr(next_tokens), _addr(lens_out), _addr(stream))
     if st:
         _check(st, "cfpp_tree_accept")
+
+
+# ---- a paged cache in 8 bits, sampling -------------------------------------------
+def cfpp_page8_pool_bytes(pages: Pages) -> int:
+    return int(lib().cfpp_page8_pool_bytes(C.byref(pages)))
+
+
+def cfpp_page8_append(pages: Pages, type: int, kv_pool, k_rows, v_rows, slots, n_rows: int, row_stride: int | None = None, stream=None):
+    """type: TYPE_INT8 or TYPE_E4M3; row_stride: elements between rows, n_kv_heads * head_dim by default."""
+    if row_stride is None:
+        row_stride = pages.n_kv_heads * pages.head_dim
+    st = lib().cfpp_page8_append(pages, type, _addr(kv_pool), _addr(k_rows), _addr(v_rows), row_stride, _addr(slots), n_rows, _addr(stream))
+    if st:
+        _check(st, "cfpp_page8_append")
+
+
+def cfpp_page8_read(pages: Pages, type: int, kv_pool, slots, n_rows: int, k_rows, v_rows, row_stride: int | None = None, stream=None):
+    """type: TYPE_INT8 or TYPE_E4M3; row_stride: elements between rows, n_kv_heads * head_dim by default."""
+    if row_stride is None:
+        row_stride = pages.n_kv_heads * pages.head_dim
+    st = lib().cfpp_page8_read(pages, type, _addr(kv_pool), _addr(slots), n_rows, _addr(k_rows), _addr(v_rows), row_stride, _addr(stream))
+    if st:
+        _check(st, "cfpp_page8_read")
+
+
+def cfpp_page8_attention(pages: Pages, type: int, kv_pool, batch: TreeBatch, q, n_heads: int, out, q_stride: int | None = None,
+                         out_stride: int | None = None, stream=None):
+    """type: TYPE_INT8 or TYPE_E4M3; q_stride, out_stride: elements between rows, n_heads * head_dim by default."""
+    width = n_heads * pages.head_dim
+    st = lib().cfpp_page8_attention(pages, type, _addr(kv_pool), batch, _addr(q), width if q_stride is None else q_stride, n_heads, _addr(out),
+                                    width if out_stride is None else out_stride, _addr(stream))
+    if st:
+        _check(st, "cfpp_page8_attention")
+
+
+def cfpp_sample(logits, type: int, n_rows: int, vocab: int, how: Sampling, tokens, probs=None, kept=None, row_stride: int | None = None, stream=None):
+    """type: TYPE_F32 or TYPE_F16; row_stride: logits between rows, vocab by default."""
+    st = lib().cfpp_sample(_addr(logits), type, vocab if row_stride is None else row_stride, n_rows, vocab, how, _addr(tokens), _addr(probs),
+                           _addr(kept), _addr(stream))
+    if st:
+        _check(st, "cfpp_sample")
 
 
 def cfpp_tree_scratch_bytes(cfg: Config, max_rows: int) -> int:

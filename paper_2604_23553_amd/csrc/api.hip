@@ -20,6 +20,7 @@
 #include "prefill_params.h"
 #include "decode_params.h"
 #include "tree_params.h"
+#include "sample_params.h"
 
 using namespace cfpp;
 
@@ -1162,11 +1163,9 @@ extern "C" cfpp_status cfpp_tree_plan(const cfpp_pages *pages, const cfpp_tree_b
     return CFPP_OK;
 }
 
-extern "C" cfpp_status cfpp_page_append(const cfpp_pages *pages, void *kv_pool, const void *k_rows, const void *v_rows, int64_t row_stride,
-                                        const int32_t *slots, int32_t n_rows, cfpp_stream stream)
+static cfpp_status check_page_rows(const cfpp_pages *pages, const void *kv_pool, const void *k_rows, const void *v_rows, int64_t row_stride,
+                                   const int32_t *slots, int32_t n_rows)
 {
-    cfpp_status st = cfpp_validate_pages(pages);
-    if (st != CFPP_OK) return st;
     if (!aligned16(kv_pool) || !aligned16(k_rows) || !aligned16(v_rows)) return fail(CFPP_EINVAL, "kv_pool, k_rows or v_rows is NULL or not 16-byte aligned");
     if (!aligned4(slots)) return fail(CFPP_EINVAL, "slots is NULL or misaligned");
     if (n_rows < 0 || n_rows > kTreeMaxRows) return fail(CFPP_EINVAL, "n_rows %d outside [0, %d]", n_rows, kTreeMaxRows);
@@ -1174,17 +1173,27 @@ extern "C" cfpp_status cfpp_page_append(const cfpp_pages *pages, void *kv_pool, 
         return fail(CFPP_EINVAL, "row_stride %lld: a multiple of 8, at least n_kv_heads * head_dim and at most 2^32", (long long)row_stride);
     if ((long long)n_rows * pages->n_kv_heads * pages->head_dim >= 1ll << 33)           // (a launch has less than 2^32 threads)
         return fail(CFPP_EUNSUPPORTED, "%d rows of %d heads of %d: less than 2^33 values", n_rows, pages->n_kv_heads, pages->head_dim);
+    return CFPP_OK;
+}
+
+extern "C" cfpp_status cfpp_page_append(const cfpp_pages *pages, void *kv_pool, const void *k_rows, const void *v_rows, int64_t row_stride,
+                                        const int32_t *slots, int32_t n_rows, cfpp_stream stream)
+{
+    cfpp_status st = cfpp_validate_pages(pages);
+    if (st != CFPP_OK) return st;
+    if ((st = check_page_rows(pages, kv_pool, k_rows, v_rows, row_stride, slots, n_rows)) != CFPP_OK) return st;
     if (n_rows == 0) return CFPP_OK;
     HIP_OK(launch_page_append(page_dims(*pages), static_cast<__half *>(kv_pool), static_cast<const __half *>(k_rows),
                               static_cast<const __half *>(v_rows), row_stride, slots, n_rows, static_cast<hipStream_t>(stream)));
     return CFPP_OK;
 }
 
-extern "C" cfpp_status cfpp_tree_attention(const cfpp_pages *pages, const void *kv_pool, const cfpp_tree_batch *batch, const void *q,
-                                           int64_t q_stride, int32_t n_heads, void *out, int64_t out_stride, cfpp_stream stream)
+// arguments of an attention over pages, but for its pool's
+static cfpp_status tree_attention_of(const cfpp_pages *pages, const void *kv_pool, const cfpp_tree_batch *batch, const void *q, int64_t q_stride,
+                                     int32_t n_heads, void *out, int64_t out_stride, TreeAttention *P)
 {
-    TreeAttention P;
-    cfpp_status st = tree_batch(pages, batch, &P.b);
+    std::memset(P, 0, sizeof *P);
+    cfpp_status st = tree_batch(pages, batch, &P->b);
     if (st != CFPP_OK) return st;
     if ((st = check_tree_plan(pages, batch, n_heads)) != CFPP_OK) return st;
     if (!aligned4(batch->block_table)) return fail(CFPP_EINVAL, "block_table is NULL or misaligned");
@@ -1194,11 +1203,20 @@ extern "C" cfpp_status cfpp_tree_attention(const cfpp_pages *pages, const void *
         return fail(CFPP_EINVAL, "strides %lld, %lld: multiples of 8, at least n_heads * head_dim and at most 2^32", (long long)q_stride, (long long)out_stride);
     const size_t rows = (size_t)batch->max_rows - 1;
     if (overlap(q, (rows * q_stride + width) * 2, out, (rows * out_stride + width) * 2)) return fail(CFPP_EINVAL, "out overlaps q");
-    P.pg = page_dims(*pages);
-    P.n_heads = n_heads; P.group = n_heads / pages->n_kv_heads;
+    P->pg = page_dims(*pages);
+    P->n_heads = n_heads; P->group = n_heads / pages->n_kv_heads;
+    P->q = static_cast<const __half *>(q); P->out = static_cast<__half *>(out);
+    P->q_stride = q_stride; P->out_stride = out_stride;
+    return CFPP_OK;
+}
+
+extern "C" cfpp_status cfpp_tree_attention(const cfpp_pages *pages, const void *kv_pool, const cfpp_tree_batch *batch, const void *q,
+                                           int64_t q_stride, int32_t n_heads, void *out, int64_t out_stride, cfpp_stream stream)
+{
+    TreeAttention P;
+    const cfpp_status st = tree_attention_of(pages, kv_pool, batch, q, q_stride, n_heads, out, out_stride, &P);
+    if (st != CFPP_OK) return st;
     P.pool = static_cast<const __half *>(kv_pool);
-    P.q = static_cast<const __half *>(q); P.out = static_cast<__half *>(out);
-    P.q_stride = q_stride; P.out_stride = out_stride;
     HIP_OK(launch_tree_attention(P, static_cast<char *>(batch->plan), static_cast<hipStream_t>(stream)));
     return CFPP_OK;
 }
@@ -1224,6 +1242,96 @@ extern "C" cfpp_status cfpp_tree_accept(const cfpp_pages *pages, void *const *kv
     P.tokens = tokens; P.picks = picks;
     P.accepted = accepted; P.path = path; P.next = next_tokens; P.lens_out = lens_out;
     HIP_OK(launch_tree_accept(P, n_layers, static_cast<hipStream_t>(stream)));
+    return CFPP_OK;
+}
+
+// ---- a paged cache in 8 bits ---------------------------------------------------------------
+static_assert(CFPP_TYPE_INT8 == kPage8Int8 && CFPP_TYPE_E4M3 == kPage8E4m3 && CFPP_TYPE_F16 == kLogitsF16 && CFPP_TYPE_F32 == kLogitsF32, "types");
+static cfpp_status check_page8_type(int32_t type)
+{
+    if (type != CFPP_TYPE_INT8 && type != CFPP_TYPE_E4M3) return fail(CFPP_EINVAL, "type %d: CFPP_TYPE_INT8 or CFPP_TYPE_E4M3", type);
+    return CFPP_OK;
+}
+
+extern "C" size_t cfpp_page8_pool_bytes(const cfpp_pages *p)
+{
+    if (cfpp_validate_pages(p) != CFPP_OK) return 0;
+    return page8_pool_bytes(page_dims(*p));
+}
+
+static cfpp_status page8_rows(const cfpp_pages *pages, int32_t type, const void *kv_pool, const void *k_rows, const void *v_rows, int64_t row_stride,
+                              const int32_t *slots, int32_t n_rows, Page8Rows *P)
+{
+    cfpp_status st = cfpp_validate_pages(pages);
+    if (st != CFPP_OK) return st;
+    if ((st = check_page8_type(type)) != CFPP_OK) return st;
+    if ((st = check_page_rows(pages, kv_pool, k_rows, v_rows, row_stride, slots, n_rows)) != CFPP_OK) return st;
+    P->pg = page_dims(*pages);
+    P->pool = static_cast<unsigned char *>(const_cast<void *>(kv_pool));
+    P->k = static_cast<__half *>(const_cast<void *>(k_rows));
+    P->v = static_cast<__half *>(const_cast<void *>(v_rows));
+    P->stride = row_stride; P->slots = slots; P->n_rows = n_rows;
+    return CFPP_OK;
+}
+
+extern "C" cfpp_status cfpp_page8_append(const cfpp_pages *pages, int32_t type, void *kv_pool, const void *k_rows, const void *v_rows, int64_t row_stride,
+                                         const int32_t *slots, int32_t n_rows, cfpp_stream stream)
+{
+    Page8Rows P;
+    const cfpp_status st = page8_rows(pages, type, kv_pool, k_rows, v_rows, row_stride, slots, n_rows, &P);
+    if (st != CFPP_OK) return st;
+    if (n_rows == 0) return CFPP_OK;
+    HIP_OK(launch_page8_append(P, type, static_cast<hipStream_t>(stream)));
+    return CFPP_OK;
+}
+
+extern "C" cfpp_status cfpp_page8_read(const cfpp_pages *pages, int32_t type, const void *kv_pool, const int32_t *slots, int32_t n_rows, void *k_rows,
+                                       void *v_rows, int64_t row_stride, cfpp_stream stream)
+{
+    Page8Rows P;
+    const cfpp_status st = page8_rows(pages, type, kv_pool, k_rows, v_rows, row_stride, slots, n_rows, &P);
+    if (st != CFPP_OK) return st;
+    if (n_rows == 0) return CFPP_OK;
+    HIP_OK(launch_page8_read(P, type, static_cast<hipStream_t>(stream)));
+    return CFPP_OK;
+}
+
+extern "C" cfpp_status cfpp_page8_attention(const cfpp_pages *pages, int32_t type, const void *kv_pool, const cfpp_tree_batch *batch, const void *q,
+                                            int64_t q_stride, int32_t n_heads, void *out, int64_t out_stride, cfpp_stream stream)
+{
+    TreeAttention P;
+    cfpp_status st = tree_attention_of(pages, kv_pool, batch, q, q_stride, n_heads, out, out_stride, &P);
+    if (st != CFPP_OK) return st;
+    if ((st = check_page8_type(type)) != CFPP_OK) return st;
+    const TreePlanLayout L = tree_plan_layout(P.pg, n_heads, batch->n_requests, batch->max_rows, batch->max_nodes, batch->table_stride);
+    if ((long long)L.work * P.pg.heads * page8_subtiles(L) >= 1 << 24)     // (a launch has less than 2^32 threads)
+        return fail(CFPP_EUNSUPPORTED, "up to %d tiles of %d query rows for each of %d key heads: less than 2^24 sets of 16 rows in all", L.work, L.tile_rows, P.pg.heads);
+    P.pool = nullptr;
+    HIP_OK(launch_page8_attention(P, static_cast<const unsigned char *>(kv_pool), type, static_cast<char *>(batch->plan), static_cast<hipStream_t>(stream)));
+    return CFPP_OK;
+}
+
+// ---- sampling ----------------------------------------------------------------------------------
+extern "C" cfpp_status cfpp_sample(const void *logits, int32_t type, int64_t row_stride, int32_t n_rows, int32_t vocab, const cfpp_sampling *how,
+                                   int32_t *tokens, float *probs, int32_t *kept, cfpp_stream stream)
+{
+    if (type != CFPP_TYPE_F32 && type != CFPP_TYPE_F16) return fail(CFPP_EINVAL, "type %d: CFPP_TYPE_F32 or CFPP_TYPE_F16", type);
+    if (!logits || (reinterpret_cast<uintptr_t>(logits) & (type == CFPP_TYPE_F32 ? 3u : 1u))) return fail(CFPP_EINVAL, "logits is NULL or misaligned");
+    if (!how) return fail(CFPP_EINVAL, "how is NULL");
+    if (n_rows < 0 || n_rows > kTreeMaxRows) return fail(CFPP_EINVAL, "n_rows %d outside [0, %d]", n_rows, kTreeMaxRows);
+    if (vocab < 1) return fail(CFPP_EINVAL, "vocab %d < 1", vocab);
+    if (vocab > kSampleMaxVocab) return fail(CFPP_EUNSUPPORTED, "vocab %d > %d", vocab, kSampleMaxVocab);
+    if (row_stride < vocab || row_stride > (1ll << 32)) return fail(CFPP_EINVAL, "row_stride %lld: at least vocab and at most 2^32", (long long)row_stride);
+    if (!aligned4(how->uniform) || !aligned4(tokens)) return fail(CFPP_EINVAL, "uniform or tokens is NULL or misaligned");
+    for (const void *p : {static_cast<const void *>(how->temperature), static_cast<const void *>(how->top_k), static_cast<const void *>(how->top_p),
+                          static_cast<const void *>(how->min_p), static_cast<const void *>(probs), static_cast<const void *>(kept)})
+        if (p && !aligned4(p)) return fail(CFPP_EINVAL, "temperature, top_k, top_p, min_p, probs or kept is misaligned");
+    if (n_rows == 0) return CFPP_OK;
+    SampleParams P;
+    P.logits = logits; P.stride = row_stride; P.vocab = vocab;
+    P.temperature = how->temperature; P.top_k = how->top_k; P.top_p = how->top_p; P.min_p = how->min_p; P.uniform = how->uniform;
+    P.tokens = tokens; P.probs = probs; P.kept = kept;
+    HIP_OK(launch_sample(P, type, n_rows, static_cast<hipStream_t>(stream)));
     return CFPP_OK;
 }
 

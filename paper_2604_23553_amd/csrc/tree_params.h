@@ -90,6 +90,29 @@ struct TreeAttention {
 };
 hipError_t launch_tree_plan(const PageDims &pg, const TreeBatch &b, int n_heads, char *plan, hipStream_t s);
 hipError_t launch_tree_attention(const TreeAttention &P, char *plan, hipStream_t s);
+// adds the pieces of tiles of more than kTaLastJoins query rows
+hipError_t launch_tree_join(const TreeAttention &P, const TreePlanLayout &L, const char *plan, hipStream_t s);
+
+// ---- a cache in 8 bits (page8_kernels.hip, page8_attention.hip) -------------------------------
+// A pool: bytes [n_pages][heads][page / 16][page8_granule(d)].  A granule, 16 positions t = 4 T + i of a head: K codes [T][d / 16][i][16], V codes
+// [d][16 positions], then the largest absolute values of its K rows and of its V rows, fp16 [16] each.
+enum { kPage8Int8 = 3, kPage8E4m3 = 4 };
+CFPP_HD int page8_granule(int d) { return 32 * d + 64; }
+CFPP_HD size_t page8_pool_bytes(const PageDims &p) { return (size_t)p.n_pages * p.heads * (p.page / 16) * page8_granule(p.d); }
+struct Page8Rows {
+    PageDims pg;
+    unsigned char *pool;
+    __half *k, *v;                     // [n_rows][stride]: read by the append, written by the other one
+    long long stride;
+    const int *slots;
+    int n_rows;
+};
+hipError_t launch_page8_append(const Page8Rows &P, int type, hipStream_t s);
+hipError_t launch_page8_read(const Page8Rows &P, int type, hipStream_t s);
+// P: as for launch_tree_attention, without its pool
+hipError_t launch_page8_attention(const TreeAttention &P, const unsigned char *pool, int type, char *plan, hipStream_t s);
+// workgroups that the attention launches for each item of the plan's list and key head
+CFPP_HD int page8_subtiles(const TreePlanLayout &L) { return L.tile_rows / 16; }
 
 // ---- the rows of a stack's step (PfParams::tree) ---------------------------------------------
 struct TreePass {

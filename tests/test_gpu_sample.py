@@ -1,0 +1,196 @@
+"""Sampling on the GPU against its plain form in 64 bits, and a server's step on a cache in 8 bits."""
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+
+import paper_2604_23553_amd as cf
+from tests import page8_ref
+from tests.test_gpu_tree import dev, i32, stream
+
+pytestmark = pytest.mark.gpu
+
+
+def f32(a):
+    return dev(np.asarray(a, dtype=np.float32))
+
+
+def draw(logits, temperature=None, top_k=None, top_p=None, min_p=None, uniform=None, stride=None, offset=0):
+    """[(token, prob, kept)] of each row; offset: logits in front of the first row"""
+    n, vocab = logits.shape
+    stride = vocab if stride is None else stride
+    flat = np.full(offset + n * stride, np.nan, dtype=logits.dtype)
+    for r in range(n):
+        flat[offset + r * stride:offset + r * stride + vocab] = logits[r]
+    x = dev(flat)
+    how = {k: v for k, v in dict(temperature=temperature, top_p=top_p, min_p=min_p, uniform=uniform).items() if v is not None}
+    g = {k: f32(np.broadcast_to(v, n)) for k, v in how.items()}
+    if top_k is not None:
+        g["top_k"] = i32(np.broadcast_to(top_k, n))
+    tokens, kept, probs = i32([-7] * n), i32([-7] * n), f32([-7] * n)
+    type = cf.TYPE_F16 if logits.dtype == np.float16 else cf.TYPE_F32
+    cf.cfpp_sample(x.data_ptr() + offset * logits.itemsize, type, n, vocab, cf.Sampling.of(**g), tokens, probs, kept, stride, stream())
+    torch.cuda.synchronize()
+    return list(zip(tokens.cpu().numpy().tolist(), probs.cpu().numpy().tolist(), kept.cpu().numpy().tolist()))
+
+
+def check(logits, **how):
+    got = draw(logits, **how)
+    for n in ("stride", "offset"):
+        how.pop(n, None)
+    for r in range(len(logits)):
+        one = {k: (int if k == "top_k" else float)(np.broadcast_to(v, len(logits))[r]) for k, v in how.items()}
+        page8_ref.check_sample(logits[r], got[r], **one)
+    return got
+
+
+def model_logits(rng, n, vocab, dtype=np.float32):
+    x = 2.5 * rng.standard_normal((n, vocab))
+    for r in range(n):
+        x[r, rng.integers(0, vocab, 12)] += 9.0
+    return x.astype(dtype)
+
+
+@pytest.mark.parametrize("dtype", [np.float32, np.float16])
+@pytest.mark.parametrize("vocab", [1, 2, 3, 5, 63, 64, 65, 255, 1023, 4095, 4096, 4097, 12289, 50304, 131071])
+def test_sizes(vocab, dtype):
+    rng = np.random.default_rng(vocab)
+    n = 24
+    x = model_logits(rng, n, vocab, dtype)
+    check(x, temperature=rng.choice([0.0, 0.3, 0.8, 1.0, 2.0], n), top_k=rng.choice([0, 1, 2, 5, 50, 400, vocab - 1, vocab, vocab + 1], n),
+          top_p=rng.choice([0.1, 0.5, 0.9, 0.99, 1.0], n), min_p=rng.choice([0.0, 0.01, 0.1, 0.5], n), uniform=rng.random(n, dtype=np.float32),
+          stride=vocab + 3, offset=1)
+
+
+@pytest.mark.parametrize("how", [dict(), dict(temperature=0.7), dict(top_k=40), dict(top_p=0.9), dict(min_p=0.05), dict(top_k=1000, top_p=0.95), dict(top_k=7, min_p=0.2),
+                                 dict(top_p=0.8, min_p=0.02), dict(top_k=300, top_p=0.7, min_p=0.001, temperature=1.5), dict(top_k=30000), dict(top_p=0.999, temperature=3.0)])
+def test_filters(how):
+    rng = np.random.default_rng(17)
+    u = np.concatenate([[0.0, 2.0 ** -24, 0.5, 1 - 2.0 ** -24], rng.random(36, dtype=np.float32)])
+    check(model_logits(rng, 40, 50304), uniform=u, **how)
+
+
+def test_filters_that_are_not_given_or_keep_all():
+    rng = np.random.default_rng(3)
+    x, u = model_logits(rng, 30, 3000), rng.random(30, dtype=np.float32)
+    plain = draw(x, uniform=u)
+    for how in (dict(temperature=1.0), dict(top_k=0), dict(top_k=-5), dict(top_k=3000), dict(top_k=2 ** 31 - 1), dict(top_p=1.0), dict(top_p=7.0), dict(top_p=np.nan),
+                dict(min_p=0.0), dict(min_p=-1.0), dict(min_p=np.nan)):
+        assert draw(x, uniform=u, **how) == plain, how
+
+
+def test_filters_that_leave_the_first():
+    rng = np.random.default_rng(4)
+    x, u = model_logits(rng, 30, 3000), rng.random(30, dtype=np.float32)
+    first = [(int(i), 1.0, 1) for i in x.argmax(-1)]
+    for how in (dict(temperature=0.0), dict(temperature=-1.0), dict(temperature=np.nan), dict(top_k=1), dict(top_p=0.0), dict(top_p=-2.0), dict(min_p=1.0),
+                dict(min_p=5.0), dict(top_p=1e-30), dict(temperature=1e-30)):
+        got = draw(x, uniform=u, **how)
+        if "temperature" in how and how["temperature"] > 0:
+            got = [(t, p, 1) for t, p, _ in got]
+        assert got == first, how
+
+
+@pytest.mark.parametrize("dtype", [np.float32, np.float16])
+def test_equal_logits(dtype):
+    """Ties go by the index: whole rows of one value, a few values, and ties in the place where a filter ends"""
+    rng = np.random.default_rng(5)
+    n, vocab = 20, 9000
+    u = rng.random(n, dtype=np.float32)
+    x = np.full((n, vocab), -1.25, dtype=dtype)
+    got = check(x, uniform=u)
+    assert [t for t, _, _ in got] == [int(np.floor(float(v) * vocab)) for v in u]
+    got = check(x, uniform=u, top_k=4321)
+    assert [t for t, _, _ in got] == [int(np.floor(float(v) * 4321)) for v in u]
+    check(x, uniform=u, top_p=0.37)
+    x = rng.choice(np.array([0.0, 1.0, 1.5, -0.0], dtype=dtype), (n, vocab))
+    check(x, uniform=u)
+    check(x, uniform=u, top_k=rng.integers(2, vocab, n))
+    check(x, uniform=u, top_p=rng.random(n, dtype=np.float32) * np.float32(0.98) + np.float32(0.01), top_k=rng.integers(2, vocab, n))
+
+
+def test_logits_of_all_sizes():
+    """Values that stand apart by more than the histogram reaches, so that most of a row falls into one bin"""
+    rng = np.random.default_rng(6)
+    n, vocab = 30, 20000
+    u = rng.random(n, dtype=np.float32)
+    x = rng.standard_normal((n, vocab)).astype(np.float32)
+    x[:10, 77] = 1e30
+    x[10:20] *= 1e4
+    x[20:] *= 1e-30
+    for how in (dict(), dict(top_k=3000), dict(top_k=15000, top_p=0.5), dict(top_p=0.9), dict(temperature=1e-6), dict(temperature=1e30), dict(temperature=np.inf),
+                dict(temperature=1e-40), dict(min_p=0.3), dict(top_k=5000, temperature=1e4)):
+        check(x, uniform=u, **how)
+
+
+@pytest.mark.parametrize("dtype", [np.float32, np.float16])
+def test_logits_that_are_no_numbers_or_infinite(dtype):
+    rng = np.random.default_rng(7)
+    n, vocab = 12, 5000
+    x = model_logits(rng, n, vocab, dtype)
+    x[0, ::2] = np.nan
+    x[1, 10:] = -np.inf
+    x[2] = -np.inf
+    x[3] = np.nan
+    x[4, [5, 4000, 4999]] = np.inf
+    x[5, 17] = np.inf
+    x[5, 3:9] = np.nan
+    x[6, :-1] = -np.inf
+    x[7] = np.finfo(dtype).min
+    x[8, 1:] = np.finfo(dtype).min
+    x[9, ::3] = np.finfo(dtype).max
+    u = rng.random(n, dtype=np.float32)
+    for how in (dict(), dict(top_k=3), dict(top_p=0.6), dict(temperature=0.0), dict(top_k=100, top_p=0.9, min_p=0.1), dict(temperature=0.5)):
+        got = check(x, uniform=u, **how)
+        assert got[2] == got[3] == (-1, 0.0, 0) and got[6][0] == vocab - 1
+
+
+def test_random_numbers_out_of_range():
+    rng = np.random.default_rng(8)
+    x = model_logits(rng, 6, 700)
+    zero, last = draw(x, uniform=0.0), draw(x, uniform=np.float32(1 - 2.0 ** -24))
+    assert [g[0] for g in zero] == list(x.argmax(-1))
+    for u in (-1.0, -np.inf, np.nan):
+        assert draw(x, uniform=u) == zero
+    for u in (1.0, 3.0, np.inf):
+        check(x, uniform=u)
+    assert draw(x, uniform=1.0) == draw(x, uniform=np.inf) and len(last) == 6
+
+
+def test_draws_follow_the_weights():
+    """Over random numbers that are evenly spaced a token comes up as often as its probability says, to one"""
+    rng = np.random.default_rng(9)
+    x = rng.standard_normal(40).astype(np.float32)
+    n = 1 << 14
+    got = draw(np.broadcast_to(x, (n, 40)), uniform=np.arange(n) / n, top_p=0.9, temperature=0.8)
+    r = page8_ref.sample(x, uniform=0.0, top_p=0.9, temperature=0.8)
+    times = np.bincount([t for t, _, _ in got], minlength=40)
+    want = np.zeros(40)
+    want[r["order"][:r["kept"]]] = r["w"][:r["kept"]] / r["sums"][r["kept"] - 1]
+    assert (np.abs(times - want * n) <= 1.0 + 1e-6).all()
+
+
+def test_outputs_that_are_not_wanted_and_replays():
+    rng = np.random.default_rng(10)
+    n, vocab = 300, 50304
+    x, u = model_logits(rng, n, vocab), rng.random(n, dtype=np.float32)
+    gx, gu, tokens = dev(x), f32(u), i32([-7] * n)
+    p = f32(rng.choice([0.5, 0.9, 1.0], n))
+    how = cf.Sampling.of(uniform=gu, top_p=p)
+    cf.cfpp_sample(gx, cf.TYPE_F32, n, vocab, how, tokens, stream=stream())
+    first = tokens.clone()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        cf.cfpp_sample(gx, cf.TYPE_F32, n, vocab, how, tokens, stream=stream())
+    for k in range(3):
+        tokens.fill_(-7)
+        graph.replay()
+        assert torch.equal(tokens, first)
+        gu.copy_(f32(rng.random(n, dtype=np.float32)))
+        graph.replay()
+        again = tokens.clone()
+        cf.cfpp_sample(gx, cf.TYPE_F32, n, vocab, how, tokens, stream=stream())
+        assert torch.equal(tokens, again) and not torch.equal(tokens, first)
+        gu.copy_(f32(u))
