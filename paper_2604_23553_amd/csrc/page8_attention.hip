@@ -95,6 +95,88 @@ __device__ __forceinline__ float p8_sum4(float v)
     return __uint_as_float(p[0]) + __uint_as_float(p[1]);
 }
 
+// The pieces of a tile of up to 16 query rows, added in order.  Up to kP8Join by the last workgroup that ends, more by the last ones of groups of about as many
+// as there are groups, whose sums the last of these adds: 128 pieces one after the other would be eleven trips to memory of a single workgroup
+// (one token of 8 query heads behind 131072 positions 24.6 -> 14.4 us).
+constexpr int kP8Join = 16;
+template <int D>
+__device__ __forceinline__ void p8_join(const TreeAttention &P, const TreePlanLayout &L, char *plan, const TreeItem &it, int H, int head, int rows, int *last_one)
+{
+    constexpr int D4 = D / 4, AT = 16, EACH = (16 * D4 + kTaThreads - 1) / kTaThreads;
+    const int tid = threadIdx.x;
+    const unsigned step = (unsigned)(H * L.tile_rows * (D + 2) * 4);       // from piece to piece
+    unsigned *counters = reinterpret_cast<unsigned *>(plan + L.counters);
+    auto last = [&](int number, int of) {                  // whether this workgroup is the last of so many; the counter is zero again then
+        unsigned *c = counters + (size_t)number * H + head;
+        xwg_wait_stores();
+        __syncthreads();
+        if (tid == 0) {
+            const bool is = __hip_atomic_fetch_add(c, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (unsigned)of - 1;
+            *last_one = is;
+            if (is) __hip_atomic_store(c, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+        __syncthreads();
+        return *last_one != 0;
+    };
+    // pieces first, first + apart, ..: `n` of them
+    f32x4 sum[EACH];
+    float m[EACH], l[EACH];
+    auto add = [&](int first, int apart, int n) {
+        const TaSlot<D> slot(L, plan, it, H, head, first);
+#pragma unroll
+        for (int k = 0; k < EACH; ++k) {
+            const int e = tid + k * kTaThreads, i = min(e / D4, rows - 1), dim = 4 * (e - e / D4 * D4);
+            const unsigned at = slot.at + (i * D + dim) * 4;
+            const float *ml_at = slot.p + slot.at / 4 + L.tile_rows * D + 2 * i;
+            m[k] = kTaLowest; l[k] = 0.f; sum[k] = f32x4{0.f, 0.f, 0.f, 0.f};
+            if (k > 0 && k * kTaThreads >= rows * D4) break;               // (uniform)
+            for (int z = 0; z < n; z += AT) {
+                float2 ml[AT];
+                f32x4 a[AT];
+#pragma unroll
+                for (int u = 0; u < AT; ++u) {             // (past the last: the last again)
+                    const int q = min(z + u, n - 1) * apart;
+                    ml[u] = xwg_load2(ml_at + (size_t)q * (step / 4));
+                    a[u] = ta_load(slot.sums, at + q * step);
+                }
+#pragma unroll
+                for (int u = 0; u < AT; ++u) {
+                    if (z + u >= n) continue;              // (uniform)
+                    const float mn = fmaxf(m[k], ml[u].x), c0 = __builtin_amdgcn_exp2f(m[k] - mn), c1 = __builtin_amdgcn_exp2f(ml[u].x - mn);
+                    l[k] = l[k] * c0 + ml[u].y * c1;
+                    sum[k] = sum[k] * c0 + a[u] * c1;
+                    m[k] = mn;
+                }
+            }
+        }
+    };
+    int apart = 1, groups = it.pieces;
+    if (it.pieces > kP8Join) {
+        while (apart * apart < it.pieces) ++apart;
+        groups = (it.pieces + apart - 1) / apart;
+        const int g = it.piece / apart, first = g * apart, n = min(apart, it.pieces - first);
+        if (!last(it.slot + first, n)) return;
+        add(first, 1, n);
+        __syncthreads();                                   // (the maxima have been read)
+        const TaSlot<D> slot(L, plan, it, H, head, first);
+#pragma unroll
+        for (int k = 0; k < EACH; ++k) {
+            const int e = tid + k * kTaThreads, i = e / D4, dim = 4 * (e - i * D4);
+            if (i >= rows) continue;
+            slot.put(i, dim, sum[k]);
+            if (dim == 0) slot.put_ml(i, m[k], l[k]);
+        }
+    }
+    // (the first group has the tile's own number, and its second piece's number is no group's)
+    if (!last(it.pieces > kP8Join ? it.slot + 1 : it.slot, groups)) return;
+    add(0, apart, groups);
+#pragma unroll
+    for (int k = 0; k < EACH; ++k) {
+        const int e = tid + k * kTaThreads, i = e / D4, dim = 4 * (e - i * D4);
+        if (i < rows) ta_deliver<D, false>(P, it, head, it.tile * L.tile_rows + i, dim, sum[k], l[k]);
+    }
+}
+
 // ONCE: every row is read by one workgroup only
 template <int D, bool INT8, bool ONCE>
 __global__ void __launch_bounds__(kTaThreads, 2) k_page8_attention(TreeAttention P, TreePlanLayout L, const unsigned char *pool, char *plan, int subs)
@@ -289,7 +371,7 @@ __global__ void __launch_bounds__(kTaThreads, 2) k_page8_attention(TreeAttention
             if (dim == 0) slot.put_ml(16 * sub + i, M, lt);
         }
     }
-    if (it.pieces > 1 && L.tile_rows <= kTaLastJoins) ta_join<D, false>(P, L, plan, it, H, head, rows, &last_one);
+    if (it.pieces > 1 && L.tile_rows <= kTaLastJoins) p8_join<D>(P, L, plan, it, H, head, rows, &last_one);
 }
 
 template <int D, bool INT8>

@@ -20,7 +20,7 @@ typedef unsigned p8_u32x2 __attribute__((ext_vector_type(2)));
 typedef unsigned short p8_u16x8 __attribute__((ext_vector_type(8)));
 typedef float p8_f32x2 __attribute__((ext_vector_type(2)));
 
-constexpr int kP8Window = 16, kP8Most = 2 * kP8Window - 1, kP8Heads = 4;
+constexpr int kP8Window = 16, kP8Most = 2 * kP8Window - 1;
 
 // The runs of a window, as bits of rows window .. window + 31; every lane of the wavefront has the same
 struct P8Runs {
@@ -41,6 +41,10 @@ struct P8Runs {
         row_bits = any & (end < 32 ? (1u << end) - 1u : ~0u) & ~((1u << first) - 1u);
         return true;
     }
+    __device__ __forceinline__ unsigned single() const     // runs of one row
+    {
+        return starts & ~((row_bits & ~starts) >> 1);
+    }
     __device__ __forceinline__ int length(int at) const    // of the run that begins with row `at` of the window
     {
         const unsigned rest = row_bits & ~starts, up = at < 31 ? rest >> (at + 1) : 0u;
@@ -56,6 +60,8 @@ __device__ __forceinline__ unsigned char *p8_granule_of(const Page8Rows &P, int 
 
 // the lanes that have a row of a head, 8 dimensions each: 8 or 16 (of which head_dim 80 uses ten)
 template <int D> constexpr int p8_lanes() { return D == 64 ? 8 : 16; }
+// heads of a workgroup: two dimensions of V to a thread, or as few as have 16 rows for 256 threads
+template <int D> constexpr int p8_heads(bool few) { return few ? (D == 64 ? 2 : 1) : 512 / D; }
 
 template <int LANES>
 __device__ __forceinline__ unsigned p8_most(unsigned v)
@@ -76,18 +82,19 @@ __device__ __forceinline__ float p8_quotient(float y, float a, float inv)
     return split_value(fmaf(fmaf(-q, a, y), inv, q));
 }
 
-template <int D, bool INT8>
+template <int D, bool INT8, bool FEW>
 __global__ void __launch_bounds__(256) k_page8_append(Page8Rows P)
 {
-    constexpr int LANES = p8_lanes<D>(), EACH = kP8Heads * kP8Window * LANES / 256, PIECES = D / 8, PITCH = kP8Heads * D;
+    constexpr int LANES = p8_lanes<D>(), HEADS = p8_heads<D>(FEW), EACH = HEADS * kP8Window * LANES / 256, PIECES = D / 8, PITCH = HEADS * D;
     constexpr float C = INT8 ? 127.f : 448.f;
     __shared__ __align__(16) unsigned char codes[kP8Most][PITCH];
     __shared__ int slot_of[32];
     P8Runs runs;
     if (!runs.of(P, blockIdx.x)) return;                   // (uniform)
-    const int tid = threadIdx.x, window = blockIdx.x * kP8Window, head0 = blockIdx.y * kP8Heads;
+    const int tid = threadIdx.x, window = blockIdx.x * kP8Window, head0 = blockIdx.y * HEADS;
     const bool v_rows = blockIdx.z != 0;
     if (tid < 32) slot_of[tid] = (runs.row_bits >> tid) & 1 ? P.slots[window + tid] : -1;
+    const unsigned single = runs.single();
     const __half *from = v_rows ? P.v : P.k;
     __syncthreads();
     for (int half = 0; half < runs.n; half += kP8Window) {
@@ -138,9 +145,18 @@ __global__ void __launch_bounds__(256) k_page8_append(Page8Rows P)
             if (piece == 0) *as_global(reinterpret_cast<unsigned short *>(g + 32 * D + (v_rows ? 32 : 0) + 2 * t)) = (unsigned short)(finite ? most : 0x7e00u);
         }
     }
-    if (!v_rows) return;
+    if (!v_rows) return;                                   // (uniform)
     __syncthreads();
-    for (unsigned left = runs.starts; left; left &= left - 1) {
+    // single rows together, a byte of a dimension to a thread: a wavefront's are in eight lines
+    if (single)
+#pragma unroll 4
+        for (int e = tid; e < runs.n * PITCH; e += 256) {
+            const int j = e / PITCH, x = e - j * PITCH, hb = x / D, dim = x - hb * D;
+            if (head0 + hb >= P.pg.heads || !((single >> (runs.first + j)) & 1)) continue;
+            const int slot = slot_of[runs.first + j];
+            *as_global(p8_granule_of(P, slot, head0 + hb) + 16 * D + dim * 16 + (slot & 15)) = codes[j][x];
+        }
+    for (unsigned left = runs.starts & ~single; left; left &= left - 1) {
         const int at = __builtin_ctz(left), len = runs.length(at), slot = slot_of[at], t0 = slot & 15;         // (uniform)
         for (int e = tid; e < PITCH; e += 256) {
             const int hb = e / D, dim = e - hb * D;
@@ -160,51 +176,73 @@ __global__ void __launch_bounds__(256) k_page8_append(Page8Rows P)
     }
 }
 
-template <int D, bool INT8>
+// fp16 of two codes, the low 16 bits of c, times their rows' largest values (the products have at most 18 significant bits)
+template <bool INT8>
+__device__ __forceinline__ unsigned p8_read(unsigned c, float a0, float a1)
+{
+    constexpr float C = INT8 ? 127.f : 448.f;
+    float f[2];
+    if constexpr (INT8) {
+        f[0] = (float)(int)(signed char)(c & 255u);
+        f[1] = (float)(int)(signed char)((c >> 8) & 255u);
+    } else {
+        const p8_f32x2 v = __builtin_amdgcn_cvt_pk_f32_fp8((int)c, false);
+        f[0] = v[0];
+        f[1] = v[1];
+    }
+    return (unsigned)__half_as_ushort(__float2half_rn(p8_quotient(f[0] * a0, C, 1.f / C))) |
+           (unsigned)__half_as_ushort(__float2half_rn(p8_quotient(f[1] * a1, C, 1.f / C))) << 16;
+}
+
+// V: a thread has two dimensions of a head and all positions of a run, which it writes one after the other, 256 bytes of a row to a wavefront; nothing
+// goes through LDS (16384 rows of 8 heads of 128 27.7 us through it, 23.1 so).
+template <int D, bool INT8, bool FEW>
 __global__ void __launch_bounds__(256) k_page8_read(Page8Rows P)
 {
-    constexpr int LANES = p8_lanes<D>(), EACH = kP8Heads * kP8Window * LANES / 256, PIECES = D / 8, PITCH = kP8Heads * D;
-    constexpr float C = INT8 ? 127.f : 448.f;
-    __shared__ __align__(16) unsigned char codes[kP8Most][PITCH];
+    constexpr int LANES = p8_lanes<D>(), HEADS = p8_heads<D>(FEW), EACH = HEADS * kP8Window * LANES / 256, PIECES = D / 8;
     __shared__ int slot_of[32];
     P8Runs runs;
     if (!runs.of(P, blockIdx.x)) return;                   // (uniform)
-    const int tid = threadIdx.x, window = blockIdx.x * kP8Window, head0 = blockIdx.y * kP8Heads;
-    const bool v_rows = blockIdx.z != 0;
+    const int tid = threadIdx.x, window = blockIdx.x * kP8Window, head0 = blockIdx.y * HEADS;
     if (tid < 32) slot_of[tid] = (runs.row_bits >> tid) & 1 ? P.slots[window + tid] : -1;
-    __half *to = v_rows ? P.v : P.k;
     __syncthreads();
-    if (v_rows) {
+    if (blockIdx.z != 0) {
+        const int hb = tid / (D / 2), dim = 2 * (tid - hb * (D / 2)), head = head0 + hb;
+        if (hb >= HEADS || head >= P.pg.heads) return;
         for (unsigned left = runs.starts; left; left &= left - 1) {
             const int at = __builtin_ctz(left), len = runs.length(at), slot = slot_of[at], t0 = slot & 15;     // (uniform)
-            for (int e = tid; e < PITCH; e += 256) {
-                const int hb = e / D, dim = e - hb * D;
-                if (head0 + hb >= P.pg.heads) break;
-                const u32x4 w = *as_global(reinterpret_cast<const u32x4 *>(p8_granule_of(P, slot, head0 + hb) + 16 * D + dim * 16));
-                unsigned char *c = &codes[at - runs.first][e];
+            const unsigned char *g = p8_granule_of(P, slot, head);
+            const u32x4 x = *as_global(reinterpret_cast<const u32x4 *>(g + 16 * D + dim * 16)), y = *as_global(reinterpret_cast<const u32x4 *>(g + 16 * D + dim * 16 + 16));
+            u32x4 most[2];
 #pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (i >= t0 && i < t0 + len) c[(i - t0) * PITCH] = (unsigned char)(w[i >> 2] >> 8 * (i & 3));
+            for (int u = 0; u < 2; ++u) most[u] = *as_global(reinterpret_cast<const u32x4 *>(g + 32 * D + 32 + 16 * u));
+            __half *to = P.v + (size_t)(window + at) * P.stride + (size_t)head * D + dim;
+#pragma unroll
+            for (int t = 0; t < 16; ++t) {
+                if (t < t0 || t >= t0 + len) continue;     // (uniform)
+                const float2 a2 = unpack_h2(most[t >> 3][(t >> 1) & 3]);
+                const float a = t & 1 ? a2.y : a2.x;
+                const unsigned c = ((x[t >> 2] >> 8 * (t & 3)) & 255u) | ((y[t >> 2] >> 8 * (t & 3)) & 255u) << 8;
+                *as_global(reinterpret_cast<unsigned *>(to + (size_t)(t - t0) * P.stride)) = p8_read<INT8>(c, a, a);
             }
         }
-        __syncthreads();
+        return;
     }
     for (int half = 0; half < runs.n; half += kP8Window) {
         p8_u32x2 x[EACH];
         unsigned short most[EACH];
         int slot[EACH];
 #pragma unroll
-        for (int u = 0; u < EACH; ++u) {
-            const int e = tid + 256 * u, piece = e % LANES, j = half + e / LANES % kP8Window, hb = e / (LANES * kP8Window), head = head0 + hb;
+        for (int u = 0; u < EACH; ++u) {                   // 16 rows of a head follow one another
+            const int e = tid + 256 * u, piece = e % LANES, j = half + e / LANES % kP8Window, head = head0 + e / (LANES * kP8Window);
             slot[u] = j < runs.n && piece < PIECES && head < P.pg.heads ? slot_of[runs.first + j] : -1;
             x[u] = p8_u32x2{0u, 0u};
             most[u] = 0;
             if (slot[u] < 0) continue;
             const unsigned char *g = p8_granule_of(P, slot[u], head);
             const int t = slot[u] & 15;
-            if (v_rows) x[u] = *reinterpret_cast<const p8_u32x2 *>(&codes[j][hb * D + piece * 8]);
-            else x[u] = *as_global(reinterpret_cast<const p8_u32x2 *>(g + (t >> 2) * 4 * D + (piece >> 1) * 64 + (t & 3) * 16 + (piece & 1) * 8));
-            most[u] = *as_global(reinterpret_cast<const unsigned short *>(g + 32 * D + (v_rows ? 32 : 0) + 2 * t));
+            x[u] = *as_global(reinterpret_cast<const p8_u32x2 *>(g + (t >> 2) * 4 * D + (piece >> 1) * 64 + (t & 3) * 16 + (piece & 1) * 8));
+            most[u] = *as_global(reinterpret_cast<const unsigned short *>(g + 32 * D + 2 * t));
         }
 #pragma unroll
         for (int u = 0; u < EACH; ++u) {
@@ -213,41 +251,37 @@ __global__ void __launch_bounds__(256) k_page8_read(Page8Rows P)
             const float a = __half2float(__ushort_as_half(most[u]));
             u32x4 out;
 #pragma unroll
-            for (int w = 0; w < 4; ++w) {
-                const unsigned c = x[u][w >> 1] >> 16 * (w & 1);
-                float f[2];
-                if constexpr (INT8) {
-                    f[0] = (float)(int)(signed char)(c & 255u);
-                    f[1] = (float)(int)(signed char)((c >> 8) & 255u);
-                } else {
-                    const p8_f32x2 v = __builtin_amdgcn_cvt_pk_f32_fp8((int)c, false);
-                    f[0] = v[0];
-                    f[1] = v[1];
-                }
-                // (the product has at most 18 significant bits)
-                out[w] = (unsigned)__half_as_ushort(__float2half_rn(p8_quotient(f[0] * a, C, 1.f / C))) |
-                         (unsigned)__half_as_ushort(__float2half_rn(p8_quotient(f[1] * a, C, 1.f / C))) << 16;
-            }
-            *as_global(reinterpret_cast<u32x4 *>(to + (size_t)(window + runs.first + j) * P.stride + (size_t)head * D + piece * 8)) = out;
+            for (int w = 0; w < 4; ++w) out[w] = p8_read<INT8>((x[u][w >> 1] >> 16 * (w & 1)) & 0xffffu, a, a);
+            *as_global(reinterpret_cast<u32x4 *>(P.k + (size_t)(window + runs.first + j) * P.stride + (size_t)head * D + piece * 8)) = out;
         }
     }
 }
 
-template <int D, bool INT8>
+// Up to so many workgroups of many heads there are some of few: 64 rows of 32 heads of 80, each in a page of its own, are 48 of six heads or 256 of one
+// (append 16.4 and 8.6 us, read of 77 rows 7.4 and 7.3); 4096 rows of hidden 4096 would take 24.0 and 27.4.
+constexpr int kP8Few = 256;
+template <int D, bool INT8, bool FEW>
 static hipError_t launch_of(const Page8Rows &P, bool append, hipStream_t s)
 {
-    const dim3 grid((P.n_rows + kP8Window - 1) / kP8Window, (P.pg.heads + kP8Heads - 1) / kP8Heads, 2);
-    if (append) hipLaunchKernelGGL((k_page8_append<D, INT8>), grid, dim3(256), 0, s, P);
-    else hipLaunchKernelGGL((k_page8_read<D, INT8>), grid, dim3(256), 0, s, P);
+    const dim3 grid((P.n_rows + kP8Window - 1) / kP8Window, (P.pg.heads + p8_heads<D>(FEW) - 1) / p8_heads<D>(FEW), 2);
+    if (append) hipLaunchKernelGGL((k_page8_append<D, INT8, FEW>), grid, dim3(256), 0, s, P);
+    else hipLaunchKernelGGL((k_page8_read<D, INT8, FEW>), grid, dim3(256), 0, s, P);
     return hipGetLastError();
+}
+template <int D>
+static hipError_t launch_type(const Page8Rows &P, int type, bool append, hipStream_t s)
+{
+    const int most = p8_heads<D>(false);
+    const bool few = (long long)((P.n_rows + kP8Window - 1) / kP8Window) * ((P.pg.heads + most - 1) / most) * 2 <= kP8Few;
+    if (type == kPage8Int8) return few ? launch_of<D, true, true>(P, append, s) : launch_of<D, true, false>(P, append, s);
+    return few ? launch_of<D, false, true>(P, append, s) : launch_of<D, false, false>(P, append, s);
 }
 static hipError_t launch(const Page8Rows &P, int type, bool append, hipStream_t s)
 {
-    const bool i8 = type == kPage8Int8;
     switch (P.pg.d) {
-    case 64: return i8 ? launch_of<64, true>(P, append, s) : launch_of<64, false>(P, append, s);
-    case 80: return i8 ? launch_of<80, true>(P, append, s) : launch_of<80, false>(P, append, s);
-    default: return i8 ? launch_of<128, true>(P, append, s) : launch_of<128, false>(P, append, s);
+    case 64: return launch_type<64>(P, type, append, s);
+    case 80: return launch_type<80>(P, type, append, s);
+    default: return launch_type<128>(P, type, append, s);
     }
 }
 hipError_t launch_page8_append(const Page8Rows &P, int type, hipStream_t s) { return launch(P, type, true, s); }
