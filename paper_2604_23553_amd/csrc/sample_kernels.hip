@@ -4,13 +4,17 @@
 // order - k tokens; as many as reach p of those k tokens' sum; those of at least min_p times the largest weight - and the token drawn is the first whose running sum
 // passes u times the sum of what is kept.  So all of it is the same question: where, in the order, does a running count or a running sum reach a target?
 //
-// Nothing is sorted.  A histogram over (l_max - l) in steps of 2^(1/32) of a weight, 2048 bins of counts and of sums in LDS, says in which bin that is; the bin's
-// tokens - tens of them for a usual row - are collected, and each finds its own place among them.  A bin of more than kList is cut again by the bits of its
-// logits, and equal logits by their index, until few are left.
+// Nothing is sorted.  A histogram over the logits in steps of 2^(1/32) of a weight, 2048 bins of counts or of sums in LDS, says in which bin that is; the
+// bin's tokens - some hundred of them for a usual row - are collected, and each finds its own place among them.  A bin of more than kList is cut again by the
+// bits of its logits, and equal logits by their index, until few are left.  Two or three passes over the row, the first from memory.
 //
-// Weights are whole multiples of 2^-45 of the largest, from a value with 2^-40 of relative error: their sums are exact in 64-bit integers whatever
-// the order, so that results do not depend on which of a workgroup's wavefronts comes first, and a border between two tokens is where 64-bit arithmetic
-// has it.  With weights in fp32 it would be up to 2^-24 off, which is another token once in some hundred thousand rows.
+// The histogram is laid from the largest of the row's first logits, which is known before the others have arrived; only where a later one stands more than
+// 2^16 above it, or where the first are all masked, is it laid again.
+//
+// Sums are exact: a bin's tokens add 2^(their place in the bin), which is near 1, as whole multiples of 2^-44 with a relative error of 2^-43, and the bin's sum, or
+// that of the first of its tokens, is scaled by 2^(-bin / 32) once, by a product of whole numbers that is cut off.  Whole numbers add up to the same
+// whichever wavefront comes first, and a border between two tokens is where 64-bit arithmetic has it but for 2^-40 of the sum.  With weights in fp32 it would
+// be up to 2^-24 off, which is another token once in some hundred thousand rows.
 #include <hip/hip_runtime.h>
 #include <hip/hip_fp16.h>
 #include "sample_params.h"
@@ -19,35 +23,18 @@
 // A token's weight is worked out in several places and has to be the same number in all of them: no product joins a sum but where fma() says so.
 #pragma clang fp contract(off)
 
+// A token's bin and its place in it are worked out in several places and have to be the same numbers in all of them: no product joins a sum but where
+// fma() says so.
+#pragma clang fp contract(off)
+
 namespace cfpp {
 
 typedef unsigned long long u64;
 
-constexpr int kBins = 2048, kList = 512;
+constexpr int kBins = 2048, kList = 512, kBinsToOctave = 32;
+constexpr float kAbove = 512.f;                            // bins above the reference
 // Rows up to which a row has a CU's 1024 threads; more, and two rows share it
 constexpr int kSampleOneEach = 256;
-constexpr float kBinsToOctave = 32.f, kWeightless = 47.f * kBinsToOctave;     // from there on weights are zero
-
-// 2^t for t <= 0 as a multiple of 2^-45; zero from 2^-46 down, and for NaN
-__device__ __forceinline__ u64 sample_weight(double t)
-{
-    t = fmax(t, -100.0);
-    const double whole = t + 6755399441055744.0;           // (1.5 2^52 more: the last bits are the whole number, rounded)
-    const double f = t - (whole - 6755399441055744.0);     // in [-1/2, 1/2]
-    // 2^f = 1 + f q(f), q fitted to the least relative error, 2^-40.1
-    double p = 1.317893346165606e-06;
-    p = fma(p, f, 1.5309156203092946e-05);
-    p = fma(p, f, 1.5403825462733238e-04);
-    p = fma(p, f, 1.3333454860442664e-03);
-    p = fma(p, f, 9.618128616123461e-03);
-    p = fma(p, f, 5.550410935266362e-02);
-    p = fma(p, f, 2.4022650698110598e-01);
-    p = fma(p, f, 6.931471805482123e-01);
-    p = fma(p, f, 1.0);
-    // times 2^(45 + the whole number), by the exponent; 2^52 more, and the last bits are the weight
-    const u64 scaled = (u64)__double_as_longlong(p) + ((u64)((unsigned)__double_as_longlong(whole) + 45u) << 52);
-    return (u64)__double_as_longlong(__longlong_as_double((long long)scaled) + 4503599627370496.0) - 0x4330000000000000ull;
-}
 
 // larger logits have larger keys (no NaN)
 __device__ __forceinline__ unsigned sample_key(float v)
@@ -58,6 +45,7 @@ __device__ __forceinline__ unsigned sample_key(float v)
 __device__ __forceinline__ float sample_of_key(unsigned k) { return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k); }
 // the order as one number, the first the smallest
 __device__ __forceinline__ u64 sample_place(unsigned key, int i) { return (u64)~key << 32 | (unsigned)i; }
+__device__ __forceinline__ float sample_of_place(u64 place) { return sample_of_key(~(unsigned)(place >> 32)); }
 
 template <int CTRL, int ROWS>
 __device__ __forceinline__ unsigned dpp_add(unsigned v)
@@ -93,15 +81,16 @@ __device__ __forceinline__ u64 lane_value(u64 v, int lane) { return (u64)lane_va
 template <int T>
 struct SampleShared {
     static constexpr int kWaves = T / 64;
-    u64 mass[kBins];
+    u64 mass[kBins];                                       // sums of the bins, then those of all bins before
     unsigned count[kBins];
-    u64 place[kList], sorted[kList], weight[kList];        // tokens as they were collected; in order, and their weights
+    u64 place[kList], weight[kList], ahead[kList];         // the list's tokens; their weights; the sum of those before, of the same bin
+    unsigned rank[kList];
     u64 wave_mass[2][kWaves];
     unsigned wave_count[2][kWaves];
-    float wave_max[kWaves];
-    int n_list, bin;
-    unsigned below, before_count, bin_n, lo, hi, kept, first;
-    u64 before_mass, value, found_place, found_mass, found_weight;
+    float wave_max[2][kWaves];
+    int n_list, bin, other;
+    unsigned below, before_count, lo, hi, kept, first;
+    u64 before_mass, value, found_place, found_weight;
 };
 
 // Sums of a value over the workgroup: those of the threads before this one, and of all.  `turn` alternates, so that a second call need not wait for the first one's readers.
@@ -120,11 +109,20 @@ __device__ __forceinline__ void block_scan(SampleShared<T> &s, int turn, unsigne
     count = c - own_count + (wave ? lane_value(wc, wave - 1) : 0u);
     mass = m - own_mass + (wave ? lane_value(wm, wave - 1) : 0ull);
 }
+template <int T>
+__device__ __forceinline__ float block_max(SampleShared<T> &s, int turn, float v)
+{
+    v = wave_max(v);
+    if ((threadIdx.x & 63) == 0) s.wave_max[turn][threadIdx.x >> 6] = v;
+    __syncthreads();
+    return wave_max(s.wave_max[turn][threadIdx.x & (T / 64 - 1)]);
+}
+__device__ __forceinline__ float max4(f32x4 v, float m) { return fmaxf(fmaxf(m, fmaxf(v[0], v[1])), fmaxf(v[2], v[3])); }
 
-// A row's logits, four to a thread that follow one another; NaN and what lies behind the row as minus infinity.  FEW: of less than four
+// A row's logits, four to a thread that follow one another; what lies behind the row as minus infinity, a NaN stays one.  FEW: of less than four
 template <int T, bool F16, bool FEW>
 struct SampleRow {
-    static constexpr int kThreads = T;
+    static constexpr int kThreads = T, STEP = 4 * T, AT = FEW ? 1 : 4;         // four vectors are on their way while four others are looked at
     const void *at;
     int vocab;
     // (the last ones of the row in place of those behind it; rows may begin at any logit)
@@ -140,17 +138,16 @@ struct SampleRow {
             return f32x4{(float)x[0], (float)x[1], (float)x[2], (float)x[3]};
         }
     }
-    // f(four logits, index of the first), all threads of the workgroup together; INFINITE: of a row whose largest logit is, 0 and minus infinity.  A NaN
-    // stays one.
-    template <bool INFINITE, class Fn>
-    __device__ __forceinline__ void each(Fn f) const
+    // first(the first vectors, which may hold logits twice or stand for ones behind the row), then f(four logits, index of the first) for all; all threads of the workgroup together
+    template <class First, class Fn>
+    __device__ __forceinline__ void each(First first, Fn f) const
     {
-        constexpr int STEP = 4 * T, AT = FEW ? 1 : 4;             // four vectors are on their way while four others are looked at
         int own = 4 * (int)threadIdx.x;
         asm volatile("" : "+v"(own));                      // (so that no pass keeps its addresses in registers for the next one)
         f32x4 next[AT];
 #pragma unroll
         for (int j = 0; j < AT; ++j) next[j] = raw(own + j * STEP);
+        first(next);
 #pragma unroll 1
         for (int base = 0; base < vocab; base += AT * STEP) {
             f32x4 x[AT];
@@ -174,34 +171,64 @@ struct SampleRow {
                         v[c] = i + c < vocab ? z : -INFINITY;
                     }
                 }
-                if constexpr (INFINITE)
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) v[c] = v[c] == INFINITY ? 0.f : -INFINITY;
                 f(v, i);
                 __builtin_amdgcn_sched_barrier(0);
             }
         }
     }
+    template <class Fn>
+    __device__ __forceinline__ void each(Fn f) const
+    {
+        each([](auto &) {}, f);
+    }
 };
 
 struct SampleHow { float tau, top_p, min_p, uniform; int top_k; };
 
-// The token of a row whose largest logit is `most`.  s.mass and s.count are zero.
-template <bool INFINITE, class Row, class Answer>
-__device__ __forceinline__ void sample_row(SampleShared<Row::kThreads> &s, const Row &R, const SampleHow &how, float most, Answer answer)
+// The token of a row.  LEVEL: the tokens that equal `most` weigh one and all others nothing; otherwise `most` is found here.  false: the weights are like
+// that, `most` is set and nothing is answered.  s.mass and s.count are zero.
+template <bool LEVEL, class Row, class Answer>
+__device__ __forceinline__ bool sample_row(SampleShared<Row::kThreads> &s, const Row &R, const SampleHow &how, float &most, Answer answer)
 {
     constexpr int T = Row::kThreads, EACH = kBins / T;
     const int tid = threadIdx.x;
-    const double octaves = 1.4426950408889634 / (double)how.tau;
-    const double least = how.min_p > 0.f ? log2((double)fminf(how.min_p, 1.f)) : -1.7976931348623157e308;
-    const float to_bin = fminf(fmaxf((float)octaves * kBinsToOctave, 1e-30f), 1e30f);          // (so that no product is none)
-    auto level = [&](float v) { return ((double)v - (double)most) * octaves; };
-    auto depth_of = [&](float v) { return (most - v) * to_bin; };              // (never rises with v)
-    auto bin_of = [&](float v) { return (int)fminf(depth_of(v), kBins - 1.f); };
+    // bins to a logit; at least so many that infinite differences stay infinite (the largest finite one is no thousandth of a bin then), at most so many that
+    // none becomes NaN
+    const double slope = fmin(fmax(LEVEL ? 1.0 : 1.4426950408889634 * kBinsToOctave / (double)how.tau, 1e-42), 1e37);
+    const float slope32 = (float)slope;
+    float ref = 0.f;                                       // its bin is kAbove
+    double shift = 0.0;
+    auto refer = [&](float to) {
+        ref = to;
+        shift = (double)ref * slope + ((double)kAbove - 0.5);
+    };
+    auto depth_of = [&](float v) { return fmaf(ref - v, slope32, kAbove); };   // (never rises with v; infinite for minus infinity)
+    auto bin_of = [&](float v) { return (int)fminf(fmaxf(depth_of(v), 0.f), kBins - 1.f); };
+    // 2^(-f / 32) in multiples of 2^-44, f the token's place in its bin from its middle: -1/2 to 1/2
+    auto weight_in = [&](float v, int bin) {
+        const double f = fma((double)v, -slope, shift) - (double)bin;
+        double p = 161364.9745385843;                      // (fitted to the least relative error, 2^-43.5)
+        p = fma(p, f, -29798760.585014474);
+        p = fma(p, f, 4127059964.301119);
+        p = fma(p, f, -381061692379.1814);
+        p = fma(p, f, 17592186044416.0);
+        return (u64)__double_as_longlong(p + 4503599627370496.0) - 0x4330000000000000ull;      // (2^52 more, and the last bits are the number)
+    };
+    int top_bin = 0;                                       // the largest logit's
+    auto scaled = [&](int bin, u64 sum) {                  // sum 2^((top_bin - bin) / 32), cut off
+        const u64 by = (u64)ldexp(exp2((double)(top_bin - bin) * (1.0 / kBinsToOctave)), 63);
+        return __umul64hi(sum << 1, by);
+    };
+    auto fit = [&](f32x4 v) {
+        if constexpr (LEVEL)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) v[c] = v[c] == most ? 0.f : -INFINITY;
+        return v;
+    };
     // f of the tokens that pick() is true of; a vector of four without any costs nothing more
-    auto each = [&](auto f) { R.template each<INFINITE>(f); };
     auto some = [&](auto pick, auto f) {
-        R.template each<INFINITE>([&](f32x4 v, int i) {
+        R.each([&](f32x4 x, int i) {
+            const f32x4 v = fit(x);
             bool on[4];
 #pragma unroll
             for (int c = 0; c < 4; ++c) on[c] = pick(v[c]);
@@ -212,287 +239,424 @@ __device__ __forceinline__ void sample_row(SampleShared<Row::kThreads> &s, const
         });
     };
     bool by_k = how.top_k > 0 && how.top_k < R.vocab;
-    const bool by_p = how.top_p < 1.f, small = R.vocab <= kList;
+    const bool by_p = how.top_p < 1.f, by_m = how.min_p > 0.f, small = R.vocab <= kList;
     int n_k = by_k ? how.top_k : R.vocab;                  // (at most so many: minus infinities are found later)
     u64 k_place = ~0ull;                                   // of the last token that top-k keeps
 
-    // kStageAll: the few tokens that top-k leaves, and some more, are in the list: all filters there.  Otherwise the places where top-k ends, where top-p does,
-    // and of the draw, one after the other
-    enum { kStageAll, kStageK, kStageP, kStageDraw };
-    int stage = small || (by_k && n_k <= kList / 2) ? kStageAll : by_k ? kStageK : by_p ? kStageP : kStageDraw;
+    // kStageAll: the few tokens that top-k leaves, and some more, are in the list: all filters there.  Otherwise the places where top-k ends, where top-p or min-p
+    // does, whichever comes first, and of the draw, one after the other
+    enum { kStageAll, kStageK, kStageCut, kStageDraw };
+    const int behind_k = by_p || by_m ? kStageCut : kStageDraw;
+    int stage = small || (by_k && n_k <= kList / 2) ? kStageAll : by_k ? kStageK : behind_k;
     enum { kNone, kCounts, kMasses };
-    int built = kNone;                                     // what the histogram holds
-    bool dirty = false, cut = false;                       // the histogram is to be cleared; top-p has cut
-    unsigned kept = 0, my_count = 0;                       // my_: running sums of the bins before this thread's
-    u64 mass = 0, my_mass = 0, all_k = 0;                  // mass: of what is kept; all_k: of what top-k keeps
-    const bool by_m = how.min_p > 0.f;
+    int built = kNone;                                     // what the histogram holds: running numbers or sums of the bins before
+    bool dirty = false, known = LEVEL, cut = false;        // the histogram is to be cleared; `most` is known; top-p or min-p has cut
+    unsigned kept = 0, all_count = 0;
+    u64 mass = 0, all_mass = 0;                            // mass: of what is kept; all_: of all bins
+    const double least = by_m ? log2((double)fminf(how.min_p, 1.f)) : 0.0;     // of a kept token's logarithm, by min-p
     int turn = 0;
     auto clear = [&]() {
         __syncthreads();
         for (int b = tid; b < kBins; b += T) { s.count[b] = 0u; s.mass[b] = 0ull; }
         __syncthreads();
     };
-    auto scan = [&](unsigned &all_count, u64 &all_mass) {
-        __syncthreads();
-        unsigned c = 0;
-        u64 m = 0;
-#pragma unroll
-        for (int b = 0; b < EACH; ++b) { c += s.count[EACH * tid + b]; m += s.mass[EACH * tid + b]; }
-        block_scan(s, turn ^= 1, c, m, my_count, my_mass, all_count, all_mass);
+    auto drawn = [&](u64 sum) {
+        const double u = how.uniform;
+        return min((u64)floor(fmin(u > 0.0 ? u : 0.0, 1.0) * (double)sum) + 1ull, sum);
     };
-    // the bin in which the running count or sum reaches the target
-    auto find = [&](bool counts, u64 target, unsigned c, u64 m) {
-#pragma unroll
-        for (int b = 0; b < EACH; ++b) {
-            const unsigned cb = s.count[EACH * tid + b];
-            const u64 mb = s.mass[EACH * tid + b];
-            if (counts ? c < target && target <= c + cb : m < target && target <= m + mb) {
-                s.bin = EACH * tid + b; s.bin_n = cb; s.before_count = c; s.before_mass = m;
-            }
-            c += cb; m += mb;
-        }
-    };
+    auto level = [&](float v) { return ((double)v - (LEVEL ? 0.0 : (double)most)) * slope * (1.0 / kBinsToOctave); };
+    if constexpr (LEVEL) {
+        refer(0.f);
+        top_bin = bin_of(0.f);
+    }
     for (;;) {
         const bool counts = stage <= kStageK;
-        if (built != (counts ? kCounts : kMasses) && !small) {
+        if (built != (counts ? kCounts : kMasses) && !(small && known)) {
             if (dirty) clear();
             dirty = true;
-            unsigned n;
-            u64 sum, total = 0;
-            if (counts) {
-                each([&](f32x4 v, int) {
+            float seen = -INFINITY;
+            unsigned n = 0;                                // tokens
+            const bool number = !by_k && stage == kStageDraw && !cut;
+            // a pass that lays the histogram; the first one from the largest of the first logits on
+            auto lay = [&](auto first) {
+                R.each([&](auto &x) {
+                    if constexpr (decltype(first)::value) {
+                        float m = -INFINITY;
 #pragma unroll
-                    for (int c = 0; c < 4; ++c)
-                        if (v[c] > -INFINITY) atomicAdd(&s.count[bin_of(v[c])], 1u);
-                });
-                scan(n, sum);
-                built = kCounts;
-                if (n <= (unsigned)n_k) {                  // (uniform) top-k keeps all that there is
-                    n_k = (int)n;
-                    by_k = false;
-                    if (n > (unsigned)kList) { stage = by_p ? kStageP : kStageDraw; continue; }
-                    stage = kStageAll;
-                }
-            } else {
-                // what min-p keeps is a beginning of the order too: its number and sum, beside the histogram of all that top-k keeps
-                const bool number = by_m || !(by_p || by_k);
-                unsigned reaches = 0;
-                each([&](f32x4 v, int i) {
+                        for (int j = 0; j < Row::AT; ++j)
+                            if (j * Row::STEP + 4 * tid < R.vocab) m = max4(x[j], m);
+                        m = block_max(s, 0, m);
+                        refer(fabsf(m) < INFINITY ? m : 0.f);
+                    }
+                }, [&](f32x4 x, int i) {
+                    f32x4 v = fit(x);
+                    if constexpr (decltype(first)::value) seen = max4(v, seen);
+                    if (small) return;                     // (uniform)
+                    if (counts) {                          // (uniform)
+#pragma unroll
+                        for (int c = 0; c < 4; ++c)
+                            if (v[c] > -INFINITY) atomicAdd(&s.count[bin_of(v[c])], 1u);
+                        return;
+                    }
                     if (by_k) {                            // (uniform)
 #pragma unroll
                         for (int c = 0; c < 4; ++c) v[c] = sample_place(sample_key(v[c]), i + c) > k_place ? -INFINITY : v[c];
                     }
+                    if (number)                            // (uniform)
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) n += v[c] > -INFINITY;
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
-                        const double t = level(v[c]);
-                        const u64 w = sample_weight(t);
                         const float y = depth_of(v[c]);
-                        if (y < kWeightless) atomicAdd(&s.mass[(int)y], w);
-                        if (number) {                      // (uniform)
-                            const bool on = t >= least;
-                            reaches += on;
-                            total += on ? w : 0ull;
-                        }
+                        const int b = (int)y;
+                        const u64 w = weight_in(v[c], b);
+                        if (y >= 0.f && y < (float)kBins) atomicAdd(&s.mass[b], w);
                     }
                 });
-                scan(n, all_k);
-                if (!cut) {
-                    kept = (unsigned)n_k;
-                    mass = all_k;
-                    if (number) {
-                        unsigned none;
-                        u64 before;
-                        block_scan(s, turn ^= 1, reaches, total, none, before, kept, sum);
-                        if (by_m) mass = sum;
+            };
+            if (!known) {
+                lay(std::true_type{});
+                most = block_max(s, 1, seen);
+                known = true;
+                if (most == -INFINITY) {
+                    if (tid == 0) answer(-1, 0.f, 0);
+                    return true;
+                }
+                // infinite, or so steep that only what equals it has a weight: one step of the largest number is more bins than there are
+                if (most == INFINITY || (double)fabsf(most) * slope > 0x1p40) return false;
+                if (depth_of(most) < 0.f) {                // (uniform) out of reach: the histogram from the largest on
+                    refer(most);
+                    if (!small) {
+                        n = 0;
+                        clear();
+                        lay(std::false_type{});
                     }
                 }
-                built = kMasses;
-            }
-        }
-        u64 target = (u64)n_k;
-        if (stage == kStageP) {
-            target = (u64)ceil((double)how.top_p * (double)all_k);
-            target = min(max(target, 1ull), all_k);
-        }
-        auto drawn = [&](u64 sum) {
-            const double u = how.uniform;
-            return min((u64)floor(fmin(u > 0.0 ? u : 0.0, 1.0) * (double)sum) + 1ull, sum);
-        };
-        if (stage == kStageDraw) target = drawn(mass);
-        if (!small) find(counts, target, my_count, my_mass);
-        else if (tid == 0) { s.bin = kBins; s.bin_n = 0u; s.before_count = 0u; s.before_mass = 0ull; }
-        if (tid == 0) { s.n_list = 0; s.below = 0u; s.lo = ~0u; s.hi = 0u; }
-        __syncthreads();
-        const int bin = s.bin;
-        unsigned before_count = s.before_count;
-        u64 before_mass = s.before_mass;
-        if (stage == kStageAll) {
-            if (before_count + s.bin_n > (unsigned)kList) { stage = kStageK; __syncthreads(); continue; }      // (uniform)
-            before_count = 0u;
-        }
-        const bool all = stage == kStageAll;
-        auto taken = [&](float v, int i) { return counts || !by_k || sample_place(sample_key(v), i) <= k_place; };
-        // what is looked at: the bin; keys k_lo .. k_hi of it; the indexes i_lo .. i_hi of the key k_lo
-        int depth = 0, i_lo = 0, i_hi = 0;
-        unsigned k_lo = 0, k_hi = 0;
-        const float from = all ? -1.f : (float)bin, to = bin >= kBins - 1 ? NAN : (float)(bin + 1);              // (the last bin has all that is left)
-        auto near = [&](float v) {
-            const float y = depth_of(v);
-            return y >= from && !(y >= to);
-        };
-        auto inside = [&](float v, int i) {
-            if (depth > 0) {
-                const unsigned key = sample_key(v);
-                if (key < k_lo || key > k_hi || (depth == 2 && (i < i_lo || i > i_hi))) return false;
-            }
-            return all || taken(v, i);
-        };
-        for (int round = 0;; ++round) {
-            auto collect = [&](float v, int i) {
-                if (!inside(v, i)) return;
-                const int at = atomicAdd(&s.n_list, 1);
-                if (at < kList) s.place[at] = sample_place(sample_key(v), i);
-            };
-            if (stage == kStageP && round == 0) {          // (what stands before a token that is kept is kept)
-                unsigned below = 0;
-                some([&](float v) { below += depth_of(v) < from; return near(v); }, collect);
-                below = wave_scan(below);
-                if ((tid & 63) == 63 && below) atomicAdd(&s.below, below);
+                top_bin = bin_of(most);
             } else {
-                some(near, collect);
+                lay(std::false_type{});
             }
             __syncthreads();
-            if (stage == kStageP && round == 0) before_count = s.below;
-            if (s.n_list <= kList || round == 4) break;    // (a cut by a logit's 32 bits takes three rounds at most, by the index one)
-            // too many for the list: a histogram of what is inside
-            if (depth == 0) {
+            if (!small) {
+                unsigned c[EACH], c0 = 0;
+                u64 m[EACH], m0 = 0;
+#pragma unroll
+                for (int b = 0; b < EACH; ++b) {
+                    c[b] = c0;
+                    m[b] = m0;
+                    if (counts) c0 += s.count[EACH * tid + b];
+                    else m0 += scaled(EACH * tid + b, s.mass[EACH * tid + b]);
+                }
+                unsigned c1;
+                u64 m1;
+                block_scan(s, turn ^= 1, c0, m0, c1, m1, all_count, all_mass);
+#pragma unroll
+                for (int b = 0; b < EACH; ++b) {
+                    if (counts) s.count[EACH * tid + b] = c1 + c[b];
+                    else s.mass[EACH * tid + b] = m1 + m[b];
+                }
+                if (!counts && !cut) {
+                    mass = all_mass;
+                    kept = (unsigned)n_k;
+                    if (number) {
+                        unsigned none;
+                        u64 none_of, no_sum;
+                        block_scan(s, turn ^= 1, n, 0ull, none, none_of, kept, no_sum);
+                    }
+                }
+                __syncthreads();
+                built = counts ? kCounts : kMasses;
+                if (counts && all_count <= (unsigned)n_k) {                    // (uniform) top-k keeps all that there is
+                    n_k = (int)all_count;
+                    by_k = false;
+                    if (all_count > (unsigned)kList) { stage = behind_k; continue; }
+                    stage = kStageAll;
+                }
+            }
+        }
+        // where the target is reached: the bin, and what stands before it
+        u64 target = (u64)n_k;
+        if (stage == kStageCut) target = by_p ? min(max((u64)ceil((double)how.top_p * (double)all_mass), 1ull), all_mass) : 1ull;
+        if (stage == kStageDraw) target = drawn(mass);
+        if (small) {
+            if (tid == 0) s.bin = kBins;
+        } else {
+#pragma unroll
+            for (int k = 0; k < EACH; ++k) {
+                const int b = EACH * tid + k;
+                const u64 from = counts ? s.count[b] : s.mass[b], to = b + 1 < kBins ? (counts ? s.count[b + 1] : s.mass[b + 1]) : counts ? all_count : all_mass;
+                if (from < target && target <= to) {
+                    s.bin = b; s.other = (int)min(to, (u64)kBins); s.before_count = (unsigned)from; s.before_mass = from;
+                }
+            }
+        }
+        if (tid == 0) { s.n_list = 0; s.lo = ~0u; s.hi = 0u; s.below = 0u; }
+        if (tid < kList) { s.rank[tid] = 0u; s.ahead[tid] = 0ull; }
+        __syncthreads();
+        int bin = s.bin;
+        unsigned before_count = s.before_count;
+        u64 before_mass = s.before_mass, before_in = 0;    // before_in: of the bin's own tokens, unscaled
+        const bool all = stage == kStageAll;
+        if (all && !small && s.other > kList) {            // (uniform) more tokens than the list has places for
+            stage = kStageK;
+            __syncthreads();
+            continue;
+        }
+        bool by_list = true;                               // whether the cut is to be found in a list
+        unsigned kept_m = ~0u;
+        u64 mass_m = ~0ull;
+        if (stage == kStageCut && by_m) {
+            // min-p ends in one of the bins m_lo .. m_hi (fp32 and fp64 may put a logit on either side of a border).  Where top-p ends in a bin before them, min-p
+            // keeps more; otherwise the tokens before and in them are numbered and added up.
+            const double at = ((double)ref - (LEVEL ? 0.0 : (double)most)) * slope + (double)kAbove - least * kBinsToOctave;
+            const int m_lo = (int)fmin(fmax(at - 0.01, 0.0), (double)kBins), m_hi = (int)fmin(fmax(at + 0.01, 0.0), (double)kBins);
+            by_list = by_p && bin <= m_hi;
+            if (!by_p || bin >= m_lo) {                    // (uniform)
+                const float from = m_lo < kBins ? (float)m_lo : (float)at, to = m_lo < kBins ? (float)(m_hi + 1) : from;
+                unsigned n = 0;
+                u64 in[2] = {0, 0};
+                some([&](float v) {
+                    const float y = depth_of(v);
+                    n += y < from;
+                    return y >= from && y < to;
+                }, [&](float v, int i) {
+                    if ((by_k && sample_place(sample_key(v), i) > k_place) || !(level(v) >= least)) return;
+                    const int b = (int)depth_of(v);
+                    ++n;
+                    if (b < kBins) in[b - m_lo] += weight_in(v, b);
+                });
+                unsigned none;
+                u64 none_of;
+                block_scan(s, turn ^= 1, n, in[0], none, none_of, kept_m, in[0]);
+                block_scan(s, turn ^= 1, 0u, in[1], none, none_of, n, in[1]);
+                mass_m = m_lo < kBins ? s.mass[m_lo] : all_mass;
+                if (m_lo < kBins && in[0]) mass_m = s.mass[m_lo] + scaled(m_lo, in[0]);
+                if (m_hi < kBins && m_hi > m_lo && in[1]) mass_m = s.mass[m_hi] + scaled(m_hi, in[1]);
+            }
+        }
+        if (by_list) {
+            // what is looked at: the bin; keys k_lo .. k_hi of it; the indexes i_lo .. i_hi of the key k_lo
+            int depth = 0, i_lo = 0, i_hi = 0;
+            unsigned k_lo = 0, k_hi = 0;
+            // (where numbers are asked for the first and last bins have all that lies outside of them)
+            const float from = all || (counts && bin == 0) ? -INFINITY : (float)bin, to = counts && bin >= kBins - 1 ? NAN : (float)(bin + 1);
+            auto near = [&](float v) {
+                const float y = depth_of(v);
+                return y >= from && !(y >= to);
+            };
+            auto inside = [&](float v, int i) {
+                if (depth > 0) {
+                    const unsigned key = sample_key(v);
+                    if (key < k_lo || key > k_hi || (depth == 2 && (i < i_lo || i > i_hi))) return false;
+                }
+                return counts || !by_k || sample_place(sample_key(v), i) <= k_place;
+            };
+            for (int round = 0;; ++round) {
+                auto collect = [&](float v, int i) {
+                    if (!inside(v, i)) return;
+                    const int at = atomicAdd(&s.n_list, 1);
+                    if (at >= kList) return;
+                    const int b = bin_of(v);
+                    u64 w = counts && !all ? 0ull : weight_in(v, b);
+                    if (all) w = depth_of(v) < (float)kBins ? scaled(b, w) : 0ull;
+                    s.place[at] = sample_place(sample_key(v), i);
+                    s.weight[at] = w;
+                };
+                if (stage == kStageCut && round == 0) {    // (what stands before a token that is kept is kept)
+                    unsigned below = 0;
+                    some([&](float v) { below += depth_of(v) < from; return near(v); }, collect);
+                    below = wave_scan(below);
+                    if ((tid & 63) == 63 && below) atomicAdd(&s.below, below);
+                } else {
+                    some(near, collect);
+                }
+                __syncthreads();
+                if (stage == kStageCut && round == 0) before_count = s.below;
+                if (s.n_list <= kList || round == 4) break;                    // (a cut by a logit's 32 bits takes three rounds at most, by the index one)
+                // too many for the list: a histogram of what is inside
+                if (depth == 0) {
+                    some(near, [&](float v, int i) {
+                        if (!inside(v, i)) return;
+                        const unsigned key = sample_key(v);
+                        atomicMin(&s.lo, key);
+                        atomicMax(&s.hi, key);
+                    });
+                    __syncthreads();
+                    k_lo = s.lo; k_hi = s.hi;
+                    depth = 1;
+                }
+                if (depth == 1 && k_lo == k_hi) { depth = 2; i_lo = 0; i_hi = R.vocab - 1; }
+                const unsigned span = depth == 1 ? k_hi - k_lo : (unsigned)(i_hi - i_lo);
+                int shift_by = 0;
+                while (span >> shift_by >= (unsigned)kBins) ++shift_by;
+                clear();
+                built = kNone;
                 some(near, [&](float v, int i) {
                     if (!inside(v, i)) return;
-                    const unsigned key = sample_key(v);
-                    atomicMin(&s.lo, key);
-                    atomicMax(&s.hi, key);
+                    const unsigned b = (depth == 1 ? k_hi - sample_key(v) : (unsigned)(i - i_lo)) >> shift_by;
+                    atomicAdd(&s.count[b], 1u);
+                    if (!counts) atomicAdd(&s.mass[b], weight_in(v, bin));
                 });
                 __syncthreads();
-                k_lo = s.lo; k_hi = s.hi;
-                depth = 1;
+                unsigned c = 0, none;
+                u64 m = 0, none_of;
+#pragma unroll
+                for (int k = 0; k < EACH; ++k) { c += s.count[EACH * tid + k]; m += s.mass[EACH * tid + k]; }
+                block_scan(s, turn ^= 1, c, m, c, m, none, none_of);
+                c += before_count;
+                m += before_in;
+#pragma unroll
+                for (int k = 0; k < EACH; ++k) {
+                    const unsigned cb = s.count[EACH * tid + k];
+                    const u64 mb = s.mass[EACH * tid + k];
+                    if (counts ? c < target && target <= c + cb : before_mass + scaled(bin, m) < target && target <= before_mass + scaled(bin, m + mb)) {
+                        s.other = EACH * tid + k; s.before_count = c; s.value = m;
+                    }
+                    c += cb; m += mb;
+                }
+                if (tid == 0) s.n_list = 0;
+                __syncthreads();
+                before_count = s.before_count;
+                before_in = s.value;
+                const unsigned b = (unsigned)s.other;
+                if (depth == 1) {
+                    k_hi -= b << shift_by;
+                    k_lo = max(k_lo, k_hi - min(k_hi, (1u << shift_by) - 1u));
+                } else {
+                    i_lo += (int)(b << shift_by);
+                    i_hi = min(i_hi, i_lo + (1 << shift_by) - 1);
+                }
             }
-            if (depth == 1 && k_lo == k_hi) { depth = 2; i_lo = 0; i_hi = R.vocab - 1; }
-            const unsigned span = depth == 1 ? k_hi - k_lo : (unsigned)(i_hi - i_lo);
-            int shift = 0;
-            while (span >> shift >= (unsigned)kBins) ++shift;
-            clear();
-            built = kNone;
-            some(near, [&](float v, int i) {
-                if (!inside(v, i)) return;
-                const unsigned b = (depth == 1 ? k_hi - sample_key(v) : (unsigned)(i - i_lo)) >> shift;
-                atomicAdd(&s.count[b], 1u);
-                if (!counts) atomicAdd(&s.mass[b], sample_weight(level(v)));
-            });
-            unsigned n;
-            u64 sum;
-            scan(n, sum);
-            find(counts, target, before_count + my_count, before_mass + my_mass);
-            if (tid == 0) s.n_list = 0;
-            __syncthreads();
-            before_count = s.before_count; before_mass = s.before_mass;
-            const unsigned b = (unsigned)s.bin;
-            if (depth == 1) {
-                k_hi -= b << shift;
-                k_lo = max(k_lo, k_hi - min(k_hi, (1u << shift) - 1u));
-            } else {
-                i_lo += (int)(b << shift);
-                i_hi = min(i_hi, i_lo + (1 << shift) - 1);
+            // every token counts those before it; where there are threads enough, several for a token
+            const int n = min(s.n_list, kList);
+            int wide = 64;
+            while (wide < n) wide <<= 1;                   // (a power of two up to kList, which divides the threads)
+            const int mine = tid & (wide - 1), share = (n + T / wide - 1) / (T / wide), j0 = tid / wide * share, j1 = min(j0 + share, n);
+            u64 place = ~0ull, w = 0ull;
+            if (mine < n) {
+                place = s.place[mine];
+                w = s.weight[mine];
+                unsigned rank = 0;
+                u64 ahead = 0;
+#pragma unroll 4
+                for (int j = j0; j < j1; ++j) {
+                    const bool before = s.place[j] < place;
+                    rank += before;
+                    ahead += before ? s.weight[j] : 0ull;
+                }
+                if (rank) {
+                    atomicAdd(&s.rank[mine], rank);
+                    atomicAdd(&s.ahead[mine], ahead);
+                }
             }
-        }
-        const int n = min(s.n_list, kList);
-        // the list in order: every token counts those before it
-        if (tid < n) {
-            const u64 own = s.place[tid];
-            int rank = 0;
-#pragma unroll 2
-            for (int j = 0; j < n; ++j) rank += s.place[j] < own;
-            s.sorted[rank] = own;
-            s.weight[rank] = sample_weight(level(sample_of_key(~(unsigned)(own >> 32))));
-        }
-        __syncthreads();
-        const u64 place = tid < n ? s.sorted[tid] : ~0ull, w = tid < n ? s.weight[tid] : 0ull;
-        unsigned none, none_of;
-        u64 sum, list_mass;
-        block_scan(s, turn ^= 1, 0u, w, none, sum, none_of, list_mass);
-        sum += before_mass;                                // of the order before this thread's token
-        if (all) {
-            n_k = min(n_k, n);                             // (tokens behind the first n_k are in the list too)
-            if (tid == n_k - 1) s.value = sum + w;
             if (tid == 0) s.kept = 0u;
             __syncthreads();
-            u64 p_target = ~0ull;
-            if (by_p) p_target = max((u64)ceil((double)how.top_p * (double)s.value), 1ull);
-            const bool ok = tid < n_k && sum < p_target && level(sample_of_key(~(unsigned)(place >> 32))) >= least;
-            const unsigned long long of_wave = __ballot(ok);
-            if ((tid & 63) == 0 && of_wave) atomicAdd(&s.kept, (unsigned)__popcll(of_wave));
+            // one thread to a token from here on: its number in the order, and the sums up to it and with it
+            const bool token = tid < n;
+            unsigned rank = 0;
+            u64 sum = 0, with = 0;
+            if (token) {
+                rank = before_count + s.rank[tid];
+                sum = s.ahead[tid];
+                with = sum + w;
+                if (!all && !counts) {
+                    sum = before_mass + scaled(bin, before_in + sum);
+                    with = before_mass + scaled(bin, before_in + with);
+                }
+            }
+            if (all) {
+                n_k = min(n_k, n);                         // (tokens behind the first n_k are in the list too)
+                rank = tid < n ? s.rank[tid] : 0u;
+                if (token && rank == (unsigned)n_k - 1u) s.value = with;
+                __syncthreads();
+                u64 p_target = ~0ull;
+                if (by_p) p_target = max((u64)ceil((double)how.top_p * (double)s.value), 1ull);
+                const bool ok = token && rank < (unsigned)n_k && sum < p_target && (!by_m || level(sample_of_place(place)) >= least);
+                const unsigned long long of_wave = __ballot(ok);
+                if ((tid & 63) == 0 && of_wave) atomicAdd(&s.kept, (unsigned)__popcll(of_wave));
+                __syncthreads();
+                const unsigned n_kept = s.kept;            // (the first of the order)
+                if (token && rank == n_kept - 1u) s.found_weight = with;
+                __syncthreads();
+                const u64 in_all = s.found_weight, at = drawn(in_all);
+                if (ok && sum < at && at <= with) answer((int)(unsigned)place, (float)((double)(with - sum) / (double)in_all), (int)n_kept);
+                return true;
+            }
+            if (token && (counts ? rank + 1u == target : sum < target && target <= with)) {
+                s.found_place = place; s.value = with; s.found_weight = with - sum; s.kept = rank + 1u;
+            }
             __syncthreads();
-            const int n_kept = (int)s.kept;                // (the first of the order)
-            if (tid == n_kept - 1) s.found_mass = sum + w;
-            __syncthreads();
-            const u64 at = drawn(s.found_mass);
-            if (sum < at && at <= sum + w && tid < n_kept) answer((int)(unsigned)place, (float)((double)w / (double)s.found_mass), n_kept);
-            return;
         }
-        if (tid < n && (counts ? before_count + tid + 1 == target : sum < target && target <= sum + w)) {
-            s.found_place = place; s.found_mass = sum + w; s.found_weight = w; s.kept = before_count + tid + 1;
-        }
-        __syncthreads();
         if (stage == kStageK) {
             k_place = s.found_place;
-            stage = by_p ? kStageP : kStageDraw;
-        } else if (stage == kStageP) {
-            kept = min(kept, s.kept);
-            mass = min(mass, s.found_mass);
+            stage = behind_k;
+        } else if (stage == kStageCut) {
+            kept = kept_m;
+            mass = mass_m;
+            if (by_list) {
+                kept = min(kept, s.kept);
+                mass = min(mass, s.value);
+            }
             cut = true;
             stage = kStageDraw;
         } else {
             if (tid == 0) answer((int)(unsigned)s.found_place, (float)((double)s.found_weight / (double)mass), (int)kept);
-            return;
+            return true;
         }
+        __syncthreads();                                   // (what was found has been read)
     }
 }
 
 template <int T, bool F16, bool FEW>
-__global__ void __launch_bounds__(T) k_sample(SampleParams P)
+__global__ void __launch_bounds__(T, 4) k_sample(SampleParams P)
 {
     __shared__ SampleShared<T> s;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, row = blockIdx.x;
+    const int tid = threadIdx.x, row = blockIdx.x;
     const SampleRow<T, F16, FEW> R{static_cast<const char *>(P.logits) + (size_t)row * P.stride * (F16 ? 2 : 4), P.vocab};
-    const SampleHow how{P.temperature ? P.temperature[row] : 1.f, P.top_p ? P.top_p[row] : 1.f, P.min_p ? P.min_p[row] : 0.f, P.uniform[row], P.top_k ? P.top_k[row] : 0};
+    SampleHow how{P.temperature ? P.temperature[row] : 1.f, P.top_p ? P.top_p[row] : 1.f, P.min_p ? P.min_p[row] : 0.f, P.uniform[row], P.top_k ? P.top_k[row] : 0};
+    int shown = -1;                                        // tokens that the filters keep, where that is known beforehand
     auto answer = [&](int token, float prob, int kept) {
         P.tokens[row] = token;
         if (P.probs) P.probs[row] = prob;
-        if (P.kept) P.kept[row] = kept;
+        if (P.kept) P.kept[row] = shown >= 0 ? shown : kept;
     };
     for (int b = tid; b < kBins; b += T) { s.count[b] = 0u; s.mass[b] = 0ull; }
-    if (tid == 0) s.first = 0x7fffffffu;
-    float most = -INFINITY;
-    R.template each<false>([&](f32x4 v, int) { most = fmaxf(fmaxf(most, fmaxf(v[0], v[1])), fmaxf(v[2], v[3])); });
-    most = wave_max(most);
-    if (lane == 0) s.wave_max[wave] = most;
-    __syncthreads();
-    most = wave_max(s.wave_max[lane & (T / 64 - 1)]);
-    if (most == -INFINITY) {                               // (uniform, as the ways out below)
-        if (tid == 0) answer(-1, 0.f, 0);
-        return;
-    }
-    if (!(how.tau > 0.f) || how.top_k == 1 || how.top_p <= 0.f) {              // the first of the order
-        R.template each<false>([&](f32x4 v, int i) {
+    if (!(how.tau > 0.f) || how.top_k == 1 || how.top_p <= 0.f) {              // (uniform) the first of the order
+        float most = -INFINITY;
+        int at = 0x7fffffff;
+        R.each([&](f32x4 v, int i) {
 #pragma unroll
             for (int c = 0; c < 4; ++c)
-                if (v[c] == most) atomicMin(&s.first, (unsigned)(i + c));
+                if (v[c] > most) { most = v[c]; at = i + c; }                  // (a thread's indexes rise)
         });
+        if (tid == 0) s.first = 0x7fffffffu;
+        const float all = block_max(s, 0, most);
+        if (most == all && at != 0x7fffffff) atomicMin(&s.first, (unsigned)at);
         __syncthreads();
-        if (tid == 0) answer((int)s.first, 1.f, 1);
+        if (tid == 0) {
+            if (s.first == 0x7fffffffu) answer(-1, 0.f, 0);
+            else answer((int)s.first, 1.f, 1);
+        }
         return;
     }
-    if (most == INFINITY) sample_row<true>(s, R, how, 0.f, answer);
-    else sample_row<false>(s, R, how, most, answer);
+    float most = -INFINITY;
+    if (sample_row<false>(s, R, how, most, answer)) return;
+    // Only the tokens that equal the largest weigh anything.  Where that is infinite the others are no part of the order; where the temperature is so low they
+    // are, and are kept where nothing cuts them off.
+    if (most < INFINITY && !(how.top_p < 1.f) && !(how.min_p > 0.f)) {         // (uniform)
+        unsigned n = 0, none, valid;
+        u64 none_of, no_sum;
+        R.each([&](f32x4 v, int) {
+#pragma unroll
+            for (int c = 0; c < 4; ++c) n += v[c] > -INFINITY;
+        });
+        block_scan(s, 0, n, 0ull, none, none_of, valid, no_sum);
+        shown = how.top_k > 0 ? min(how.top_k, (int)valid) : (int)valid;
+    }
+    __syncthreads();
+    for (int b = tid; b < kBins; b += T) { s.count[b] = 0u; s.mass[b] = 0ull; }
+    __syncthreads();
+    sample_row<true>(s, R, how, most, answer);
 }
 
 template <int T, bool F16>
