@@ -76,6 +76,12 @@ __device__ __forceinline__ V wave_scan(V v)
     return dpp_add<0x143, 0xC>(v);
 }
 __device__ __forceinline__ unsigned lane_value(unsigned v, int lane) { return (unsigned)__builtin_amdgcn_readlane((int)v, lane); }
+// a value that all lanes have, in scalar registers
+__device__ __forceinline__ unsigned uniform(unsigned v) { return (unsigned)__builtin_amdgcn_readfirstlane((int)v); }
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ float uniform(float v) { return __uint_as_float(uniform(__float_as_uint(v))); }
+__device__ __forceinline__ u64 uniform(u64 v) { return (u64)uniform((unsigned)(v >> 32)) << 32 | uniform((unsigned)v); }
+__device__ __forceinline__ double uniform(double v) { return __longlong_as_double((long long)uniform((u64)__double_as_longlong(v))); }
 __device__ __forceinline__ u64 lane_value(u64 v, int lane) { return (u64)lane_value((unsigned)(v >> 32), lane) << 32 | lane_value((unsigned)v, lane); }
 
 template <int T>
@@ -115,7 +121,7 @@ __device__ __forceinline__ float block_max(SampleShared<T> &s, int turn, float v
     v = wave_max(v);
     if ((threadIdx.x & 63) == 0) s.wave_max[turn][threadIdx.x >> 6] = v;
     __syncthreads();
-    return wave_max(s.wave_max[turn][threadIdx.x & (T / 64 - 1)]);
+    return uniform(wave_max(s.wave_max[turn][threadIdx.x & (T / 64 - 1)]));
 }
 __device__ __forceinline__ float max4(f32x4 v, float m) { return fmaxf(fmaxf(m, fmaxf(v[0], v[1])), fmaxf(v[2], v[3])); }
 
@@ -194,13 +200,13 @@ __device__ __forceinline__ bool sample_row(SampleShared<Row::kThreads> &s, const
     const int tid = threadIdx.x;
     // bins to a logit; at least so many that infinite differences stay infinite (the largest finite one is no thousandth of a bin then), at most so many that
     // none becomes NaN
-    const double slope = fmin(fmax(LEVEL ? 1.0 : 1.4426950408889634 * kBinsToOctave / (double)how.tau, 1e-42), 1e37);
-    const float slope32 = (float)slope;
+    const double slope = uniform(fmin(fmax(LEVEL ? 1.0 : 1.4426950408889634 * kBinsToOctave / (double)how.tau, 1e-42), 1e37));
+    const float slope32 = uniform((float)slope);
     float ref = 0.f;                                       // its bin is kAbove
     double shift = 0.0;
     auto refer = [&](float to) {
         ref = to;
-        shift = (double)ref * slope + ((double)kAbove - 0.5);
+        shift = uniform((double)ref * slope + ((double)kAbove - 0.5));
     };
     auto depth_of = [&](float v) { return fmaf(ref - v, slope32, kAbove); };   // (never rises with v; infinite for minus infinity)
     auto bin_of = [&](float v) { return (int)fminf(fmaxf(depth_of(v), 0.f), kBins - 1.f); };
@@ -253,7 +259,7 @@ __device__ __forceinline__ bool sample_row(SampleShared<Row::kThreads> &s, const
     bool dirty = false, known = LEVEL, cut = false;        // the histogram is to be cleared; `most` is known; top-p or min-p has cut
     unsigned kept = 0, all_count = 0;
     u64 mass = 0, all_mass = 0;                            // mass: of what is kept; all_: of all bins
-    const double least = by_m ? log2((double)fminf(how.min_p, 1.f)) : 0.0;     // of a kept token's logarithm, by min-p
+    const double least = uniform(by_m ? log2((double)fminf(how.min_p, 1.f)) : 0.0);     // of a kept token's logarithm, by min-p
     int turn = 0;
     auto clear = [&]() {
         __syncthreads();
@@ -267,7 +273,7 @@ __device__ __forceinline__ bool sample_row(SampleShared<Row::kThreads> &s, const
     auto level = [&](float v) { return ((double)v - (LEVEL ? 0.0 : (double)most)) * slope * (1.0 / kBinsToOctave); };
     if constexpr (LEVEL) {
         refer(0.f);
-        top_bin = bin_of(0.f);
+        top_bin = uniform(bin_of(0.f));
     }
     for (;;) {
         const bool counts = stage <= kStageK;
@@ -311,6 +317,7 @@ __device__ __forceinline__ bool sample_row(SampleShared<Row::kThreads> &s, const
                         const int b = (int)y;
                         const u64 w = weight_in(v[c], b);
                         if (y >= 0.f && y < (float)kBins) atomicAdd(&s.mass[b], w);
+                        if (c & 1) __builtin_amdgcn_sched_barrier(0);          // (four side by side take more registers than there are)
                     }
                 });
             };
@@ -332,7 +339,7 @@ __device__ __forceinline__ bool sample_row(SampleShared<Row::kThreads> &s, const
                         lay(std::false_type{});
                     }
                 }
-                top_bin = bin_of(most);
+                top_bin = uniform(bin_of(most));
             } else {
                 lay(std::false_type{});
             }
@@ -356,7 +363,7 @@ __device__ __forceinline__ bool sample_row(SampleShared<Row::kThreads> &s, const
                     else s.mass[EACH * tid + b] = m1 + m[b];
                 }
                 if (!counts && !cut) {
-                    mass = all_mass;
+                    mass = uniform(all_mass);
                     kept = (unsigned)n_k;
                     if (number) {
                         unsigned none;
@@ -378,6 +385,7 @@ __device__ __forceinline__ bool sample_row(SampleShared<Row::kThreads> &s, const
         u64 target = (u64)n_k;
         if (stage == kStageCut) target = by_p ? min(max((u64)ceil((double)how.top_p * (double)all_mass), 1ull), all_mass) : 1ull;
         if (stage == kStageDraw) target = drawn(mass);
+        target = uniform(target);
         if (small) {
             if (tid == 0) s.bin = kBins;
         } else {
@@ -393,9 +401,10 @@ __device__ __forceinline__ bool sample_row(SampleShared<Row::kThreads> &s, const
         if (tid == 0) { s.n_list = 0; s.lo = ~0u; s.hi = 0u; s.below = 0u; }
         if (tid < kList) { s.rank[tid] = 0u; s.ahead[tid] = 0ull; }
         __syncthreads();
-        int bin = s.bin;
-        unsigned before_count = s.before_count;
-        u64 before_mass = s.before_mass, before_in = 0;    // before_in: of the bin's own tokens, unscaled
+        const int bin = uniform(s.bin);
+        unsigned before_count = uniform(s.before_count);
+        u64 before_in = 0;
+        const u64 before_mass = uniform(s.before_mass);    // before_in: of the bin's own tokens, unscaled
         const bool all = stage == kStageAll;
         if (all && !small && s.other > kList) {            // (uniform) more tokens than the list has places for
             stage = kStageK;
@@ -456,11 +465,7 @@ __device__ __forceinline__ bool sample_row(SampleShared<Row::kThreads> &s, const
                     if (!inside(v, i)) return;
                     const int at = atomicAdd(&s.n_list, 1);
                     if (at >= kList) return;
-                    const int b = bin_of(v);
-                    u64 w = counts && !all ? 0ull : weight_in(v, b);
-                    if (all) w = depth_of(v) < (float)kBins ? scaled(b, w) : 0ull;
                     s.place[at] = sample_place(sample_key(v), i);
-                    s.weight[at] = w;
                 };
                 if (stage == kStageCut && round == 0) {    // (what stands before a token that is kept is kept)
                     unsigned below = 0;
@@ -471,7 +476,7 @@ __device__ __forceinline__ bool sample_row(SampleShared<Row::kThreads> &s, const
                     some(near, collect);
                 }
                 __syncthreads();
-                if (stage == kStageCut && round == 0) before_count = s.below;
+                if (stage == kStageCut && round == 0) before_count = uniform(s.below);
                 if (s.n_list <= kList || round == 4) break;                    // (a cut by a logit's 32 bits takes three rounds at most, by the index one)
                 // too many for the list: a histogram of what is inside
                 if (depth == 0) {
@@ -482,7 +487,7 @@ __device__ __forceinline__ bool sample_row(SampleShared<Row::kThreads> &s, const
                         atomicMax(&s.hi, key);
                     });
                     __syncthreads();
-                    k_lo = s.lo; k_hi = s.hi;
+                    k_lo = uniform(s.lo); k_hi = uniform(s.hi);
                     depth = 1;
                 }
                 if (depth == 1 && k_lo == k_hi) { depth = 2; i_lo = 0; i_hi = R.vocab - 1; }
@@ -516,9 +521,9 @@ __device__ __forceinline__ bool sample_row(SampleShared<Row::kThreads> &s, const
                 }
                 if (tid == 0) s.n_list = 0;
                 __syncthreads();
-                before_count = s.before_count;
-                before_in = s.value;
-                const unsigned b = (unsigned)s.other;
+                before_count = uniform(s.before_count);
+                before_in = uniform(s.value);
+                const unsigned b = uniform((unsigned)s.other);
                 if (depth == 1) {
                     k_hi -= b << shift_by;
                     k_lo = max(k_lo, k_hi - min(k_hi, (1u << shift_by) - 1u));
@@ -528,7 +533,15 @@ __device__ __forceinline__ bool sample_row(SampleShared<Row::kThreads> &s, const
                 }
             }
             // every token counts those before it; where there are threads enough, several for a token
-            const int n = min(s.n_list, kList);
+            const int n = uniform(min(s.n_list, kList));
+            if (tid < n && !(counts && !all)) {
+                const float v = sample_of_place(s.place[tid]);
+                const int b = bin_of(v);
+                u64 w = weight_in(v, b);
+                if (all) w = depth_of(v) < (float)kBins ? scaled(b, w) : 0ull;
+                s.weight[tid] = w;
+            }
+            __syncthreads();
             int wide = 64;
             while (wide < n) wide <<= 1;                   // (a power of two up to kList, which divides the threads)
             const int mine = tid & (wide - 1), share = (n + T / wide - 1) / (T / wide), j0 = tid / wide * share, j1 = min(j0 + share, n);
@@ -588,14 +601,14 @@ __device__ __forceinline__ bool sample_row(SampleShared<Row::kThreads> &s, const
             __syncthreads();
         }
         if (stage == kStageK) {
-            k_place = s.found_place;
+            k_place = uniform(s.found_place);
             stage = behind_k;
         } else if (stage == kStageCut) {
             kept = kept_m;
             mass = mass_m;
             if (by_list) {
-                kept = min(kept, s.kept);
-                mass = min(mass, s.value);
+                kept = uniform(min(kept, s.kept));
+                mass = uniform(min(mass, s.value));
             }
             cut = true;
             stage = kStageDraw;
