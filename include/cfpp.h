@@ -535,7 +535,7 @@ cfpp_status cfpp_stack_tree(cfpp_ctx *ctx, const void *const *packed_layers, voi
  * cfpp_tree_plan serve both kinds of pools, and a decode step of many requests is
  *   cfpp_page_tables (counts 1) -> cfpp_tree_plan (max_nodes 1, parents -1)
  *   -> per layer cfpp_page8_append -> cfpp_page8_attention -> logits -> cfpp_sample
- * Sequences with shorter pages lose nothing; no call raises the device error flag. */
+ * No call raises the device error flag. */
 #define CFPP_TYPE_F16  1
 #define CFPP_TYPE_F32  2
 #define CFPP_TYPE_INT8 3
@@ -611,6 +611,20 @@ typedef struct cfpp_sampling {
 cfpp_status cfpp_sample(const void *logits, int32_t type, int64_t row_stride, int32_t n_rows, int32_t vocab,
                         const cfpp_sampling *how, int32_t *tokens, float *probs, int32_t *kept,
                         cfpp_stream stream);
+
+/* cfpp_lm_next with a token that is drawn (one sequence): the logits of the whole head into
+ * logits_dev (DEVICE float [vocab], never NULL), then cfpp_sample's token from them -
+ * token 0 where the order has none - into tokens_dev[*pos_dev + 1], and *pos_dev += 1.
+ * how's filters are one value each; its uniform is [max_seq], the number at *pos_dev counts.
+ * EUNSUPPORTED too for a vocab over 2^18.
+ * cfpp_generate_sample_capture records embed -> stack step -> cfpp_lm_sample as
+ * cfpp_generate_capture does with cfpp_lm_next. */
+cfpp_status cfpp_lm_sample(cfpp_ctx *ctx, const cfpp_lm *lm, const void *hidden, const cfpp_sampling *how,
+                           int32_t *tokens_dev, int32_t *pos_dev, float *logits_dev, cfpp_stream stream);
+cfpp_status cfpp_generate_sample_capture(cfpp_ctx *ctx, const void *const *packed_layers, void *const *kv_layers,
+                                         const cfpp_lm *lm, const cfpp_sampling *how, int32_t *tokens_dev,
+                                         int32_t *pos_dev, void *x_buf, void *hidden_buf, float *logits_dev,
+                                         cfpp_stream stream);
 
 /* The whole-stack kernel marks the words its workgroups exchange with a 32-bit
  * epoch that every launch advances by n_layers + 1; the library counts the

@@ -13,7 +13,7 @@ from .binding import (  # noqa: F401
     cfpp_block_decode_static, cfpp_device_error, cfpp_debug_read, cfpp_debug_prefill_plan, cfpp_debug_prefill_narrow, cfpp_debug_prefill_beside, cfpp_debug_attention_plan, cfpp_debug_prefill_tiles, cfpp_debug_prefill_long, cfpp_debug_prefill_scratch, cfpp_debug_gelu, cfpp_stream_read, cfpp_stream_copy,
     Pages, TreeBatch, cfpp_validate_pages, cfpp_page_pool_bytes, cfpp_tree_plan_bytes, cfpp_page_tables, cfpp_tree_plan, cfpp_page_append,
     cfpp_tree_attention, cfpp_tree_accept, cfpp_tree_scratch_bytes, cfpp_stack_tree,
-    cfpp_page8_pool_bytes, cfpp_page8_append, cfpp_page8_read, cfpp_page8_attention, Sampling, cfpp_sample,
+    cfpp_page8_pool_bytes, cfpp_page8_append, cfpp_page8_read, cfpp_page8_attention, Sampling, cfpp_sample, cfpp_lm_sample, cfpp_generate_sample_capture,
     TYPE_F16, TYPE_F32, TYPE_INT8, TYPE_E4M3,
     Lm, cfpp_lm_embed, cfpp_lm_next, cfpp_generate_capture,
     OPT_MODE, OPT_GRID, OPT_THREADS, OPT_PROFILE_SKIP, OPT_EPOCH_LIMIT, MODE_AUTO,

@@ -414,6 +414,18 @@ def cfpp_sample(logits, type: int, n_rows: int, vocab: int, how: Sampling, token
         _check(st, "cfpp_sample")
 
 
+def cfpp_lm_sample(ctx: int, lm: Lm, hidden, how: Sampling, tokens_dev, pos_dev, logits_dev, stream=None):
+    _check(lib().cfpp_lm_sample(C.c_void_p(ctx), C.byref(lm), _ptr(hidden), C.byref(how), _ptr(tokens_dev), _ptr(pos_dev), _ptr(logits_dev),
+                                _ptr(stream)), "cfpp_lm_sample")
+
+
+def cfpp_generate_sample_capture(ctx: int, packed_layers, kv_layers, lm: Lm, how: Sampling, tokens_dev, pos_dev, x_buf, hidden_buf, logits_dev,
+                                 stream):
+    _check(lib().cfpp_generate_sample_capture(C.c_void_p(ctx), _ptr_array(packed_layers), _ptr_array(kv_layers), C.byref(lm), C.byref(how),
+                                              _ptr(tokens_dev), _ptr(pos_dev), _ptr(x_buf), _ptr(hidden_buf), _ptr(logits_dev),
+                                              _ptr(stream)), "cfpp_generate_sample_capture")
+
+
 def cfpp_tree_scratch_bytes(cfg: Config, max_rows: int) -> int:
     return int(lib().cfpp_tree_scratch_bytes(C.byref(cfg), C.c_int32(max_rows)))
 

@@ -68,6 +68,7 @@ extern "C" const char *cfpp_last_error(void) { return g_err; }
 
 // ---- config -------------------------------------------------------------------
 static bool aligned16(const void *p) { return p && (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+static bool aligned4(const void *p) { return p && (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 
 extern "C" cfpp_status cfpp_validate_config(const cfpp_config *c)
 {
@@ -981,9 +982,43 @@ extern "C" cfpp_status cfpp_lm_next(cfpp_ctx *ctx, const cfpp_lm *lm, const void
     return CFPP_OK;
 }
 
-extern "C" cfpp_status cfpp_generate_capture(cfpp_ctx *ctx, const void *const *packed_layers,
-                                             void *const *kv_layers, const cfpp_lm *lm, int32_t *tokens_dev,
-                                             int32_t *pos_dev, void *x_buf, void *hidden_buf, cfpp_stream stream)
+static cfpp_status check_sampling(const cfpp_sampling *how);
+// the sampling of a generation loop's row
+static cfpp_status make_loop_sampling(const LmParams &L, const cfpp_sampling *how, float *logits_dev, SampleParams *P)
+{
+    const cfpp_status st = check_sampling(how);
+    if (st != CFPP_OK) return st;
+    if (!logits_dev || (reinterpret_cast<uintptr_t>(logits_dev) & 3u)) return fail(CFPP_EINVAL, "logits_dev is NULL or misaligned");
+    if (L.vocab > kSampleMaxVocab) return fail(CFPP_EUNSUPPORTED, "vocab %d > %d", L.vocab, kSampleMaxVocab);
+    std::memset(P, 0, sizeof *P);
+    P->logits = logits_dev; P->stride = P->vocab = L.vocab;
+    P->temperature = how->temperature; P->top_k = how->top_k; P->top_p = how->top_p; P->min_p = how->min_p; P->uniform = how->uniform;
+    P->tokens = L.tokens_out; P->pos = L.pos_out; P->max_seq = L.max_seq;
+    return CFPP_OK;
+}
+
+extern "C" cfpp_status cfpp_lm_sample(cfpp_ctx *ctx, const cfpp_lm *lm, const void *hidden, const cfpp_sampling *how, int32_t *tokens_dev,
+                                      int32_t *pos_dev, float *logits_dev, cfpp_stream stream)
+{
+    Shape sh;
+    LmParams L;
+    SampleParams P;
+    cfpp_status st = make_lm_params(ctx, lm, tokens_dev, pos_dev, &sh, &L);
+    if (st != CFPP_OK) return st;
+    if (!aligned16(hidden)) return fail(CFPP_EINVAL, "hidden is NULL or not 16-byte aligned");
+    if ((st = make_loop_sampling(L, how, logits_dev, &P)) != CFPP_OK) return st;
+    if ((st = prepare_lm(ctx)) != CFPP_OK) return st;
+    L.hidden = static_cast<const __half *>(hidden);
+    L.logits = logits_dev;
+    L.sampled = true;
+    HIP_OK(launch_lm_head(L, sh.grid, sh.threads, static_cast<hipStream_t>(stream)));
+    HIP_OK(launch_sample(P, CFPP_TYPE_F32, 1, static_cast<hipStream_t>(stream)));
+    return CFPP_OK;
+}
+
+// how: null for the largest logit
+static cfpp_status capture_generation(cfpp_ctx *ctx, const void *const *packed_layers, void *const *kv_layers, const cfpp_lm *lm, const cfpp_sampling *how,
+                                      int32_t *tokens_dev, int32_t *pos_dev, void *x_buf, void *hidden_buf, float *logits_dev, cfpp_stream stream)
 {
     if (!ctx) return fail(CFPP_EINVAL, "ctx is NULL");
     hipStream_t s = static_cast<hipStream_t>(stream);
@@ -995,6 +1030,12 @@ extern "C" cfpp_status cfpp_generate_capture(cfpp_ctx *ctx, const void *const *p
     if (!aligned16(x_buf) || !aligned16(hidden_buf)) return fail(CFPP_EINVAL, "x_buf or hidden_buf is NULL or not 16-byte aligned");
     L.x = static_cast<__half *>(x_buf);
     L.hidden = static_cast<const __half *>(hidden_buf);
+    SampleParams P;
+    if (how) {
+        if ((st = make_loop_sampling(L, how, logits_dev, &P)) != CFPP_OK) return st;
+        L.logits = logits_dev;
+        L.sampled = true;
+    }
     if ((st = prepare(ctx)) != CFPP_OK) return st;
     if ((st = prepare_lm(ctx)) != CFPP_OK) return st;
     if (ctx->exec) { (void)hipGraphExecDestroy(ctx->exec); ctx->exec = nullptr; }
@@ -1008,6 +1049,7 @@ extern "C" cfpp_status cfpp_generate_capture(cfpp_ctx *ctx, const void *const *p
     if (e == hipSuccess) {
         st = enqueue_stack(ctx, packed_layers, kv_layers, x_buf, pos_dev, 1, hidden_buf, s, false, true);
         if (st == CFPP_OK) e = launch_lm_head(L, sh.grid, sh.threads, s);
+        if (st == CFPP_OK && e == hipSuccess && how) e = launch_sample(P, CFPP_TYPE_F32, 1, s);
     }
     hipGraph_t graph = nullptr;
     const hipError_t e2 = hipStreamEndCapture(s, &graph);
@@ -1023,6 +1065,21 @@ extern "C" cfpp_status cfpp_generate_capture(cfpp_ctx *ctx, const void *const *p
         return fail(CFPP_EHIP, "hipGraphInstantiate failed: %s", hipGetErrorString(e));
     }
     return CFPP_OK;
+}
+
+extern "C" cfpp_status cfpp_generate_capture(cfpp_ctx *ctx, const void *const *packed_layers,
+                                             void *const *kv_layers, const cfpp_lm *lm, int32_t *tokens_dev,
+                                             int32_t *pos_dev, void *x_buf, void *hidden_buf, cfpp_stream stream)
+{
+    return capture_generation(ctx, packed_layers, kv_layers, lm, nullptr, tokens_dev, pos_dev, x_buf, hidden_buf, nullptr, stream);
+}
+
+extern "C" cfpp_status cfpp_generate_sample_capture(cfpp_ctx *ctx, const void *const *packed_layers, void *const *kv_layers, const cfpp_lm *lm,
+                                                    const cfpp_sampling *how, int32_t *tokens_dev, int32_t *pos_dev, void *x_buf, void *hidden_buf,
+                                                    float *logits_dev, cfpp_stream stream)
+{
+    if (!how) return fail(CFPP_EINVAL, "how is NULL");
+    return capture_generation(ctx, packed_layers, kv_layers, lm, how, tokens_dev, pos_dev, x_buf, hidden_buf, logits_dev, stream);
 }
 
 extern "C" cfpp_status cfpp_device_error(cfpp_ctx *ctx, cfpp_stream stream)
@@ -1045,7 +1102,6 @@ extern "C" cfpp_status cfpp_device_error(cfpp_ctx *ctx, cfpp_stream stream)
 }
 
 // ---- drafted trees over a paged cache -------------------------------------------------------
-static bool aligned4(const void *p) { return p && (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 static bool overlap(const void *a, size_t na, const void *b, size_t nb)
 {
     const char *x = static_cast<const char *>(a), *y = static_cast<const char *>(b);
@@ -1312,22 +1368,32 @@ extern "C" cfpp_status cfpp_page8_attention(const cfpp_pages *pages, int32_t typ
 }
 
 // ---- sampling ----------------------------------------------------------------------------------
+static cfpp_status check_sampling(const cfpp_sampling *how)
+{
+    if (!how) return fail(CFPP_EINVAL, "how is NULL");
+    if (!aligned4(how->uniform)) return fail(CFPP_EINVAL, "uniform is NULL or misaligned");
+    for (const void *p : {static_cast<const void *>(how->temperature), static_cast<const void *>(how->top_k), static_cast<const void *>(how->top_p),
+                          static_cast<const void *>(how->min_p)})
+        if (p && !aligned4(p)) return fail(CFPP_EINVAL, "temperature, top_k, top_p or min_p is misaligned");
+    return CFPP_OK;
+}
+
 extern "C" cfpp_status cfpp_sample(const void *logits, int32_t type, int64_t row_stride, int32_t n_rows, int32_t vocab, const cfpp_sampling *how,
                                    int32_t *tokens, float *probs, int32_t *kept, cfpp_stream stream)
 {
     if (type != CFPP_TYPE_F32 && type != CFPP_TYPE_F16) return fail(CFPP_EINVAL, "type %d: CFPP_TYPE_F32 or CFPP_TYPE_F16", type);
     if (!logits || (reinterpret_cast<uintptr_t>(logits) & (type == CFPP_TYPE_F32 ? 3u : 1u))) return fail(CFPP_EINVAL, "logits is NULL or misaligned");
-    if (!how) return fail(CFPP_EINVAL, "how is NULL");
     if (n_rows < 0 || n_rows > kTreeMaxRows) return fail(CFPP_EINVAL, "n_rows %d outside [0, %d]", n_rows, kTreeMaxRows);
     if (vocab < 1) return fail(CFPP_EINVAL, "vocab %d < 1", vocab);
     if (vocab > kSampleMaxVocab) return fail(CFPP_EUNSUPPORTED, "vocab %d > %d", vocab, kSampleMaxVocab);
     if (row_stride < vocab || row_stride > (1ll << 32)) return fail(CFPP_EINVAL, "row_stride %lld: at least vocab and at most 2^32", (long long)row_stride);
-    if (!aligned4(how->uniform) || !aligned4(tokens)) return fail(CFPP_EINVAL, "uniform or tokens is NULL or misaligned");
-    for (const void *p : {static_cast<const void *>(how->temperature), static_cast<const void *>(how->top_k), static_cast<const void *>(how->top_p),
-                          static_cast<const void *>(how->min_p), static_cast<const void *>(probs), static_cast<const void *>(kept)})
-        if (p && !aligned4(p)) return fail(CFPP_EINVAL, "temperature, top_k, top_p, min_p, probs or kept is misaligned");
+    const cfpp_status st = check_sampling(how);
+    if (st != CFPP_OK) return st;
+    if (!aligned4(tokens)) return fail(CFPP_EINVAL, "tokens is NULL or misaligned");
+    if ((probs && !aligned4(probs)) || (kept && !aligned4(kept))) return fail(CFPP_EINVAL, "probs or kept is misaligned");
     if (n_rows == 0) return CFPP_OK;
     SampleParams P;
+    std::memset(&P, 0, sizeof P);
     P.logits = logits; P.stride = row_stride; P.vocab = vocab;
     P.temperature = how->temperature; P.top_k = how->top_k; P.top_p = how->top_p; P.min_p = how->min_p; P.uniform = how->uniform;
     P.tokens = tokens; P.probs = probs; P.kept = kept;

@@ -231,6 +231,7 @@ __global__ void __launch_bounds__(64 * kLmWaves, 2) k_lm_ring(LmParams L)
         if (L.logits) L.logits[r0 + t] = lg;
         if (lm_better(lg, r0 + t, best, bi)) { best = lg; bi = r0 + t; }
     }
+    if (L.sampled) return;                                 // (uniform over the grid)
     lm_wave_best(best, bi);
     if (lane == 0) { last[2 * wave] = best; last[2 * wave + 1] = __int_as_float(bi); }
     __syncthreads();
@@ -285,7 +286,7 @@ hipError_t launch_lm_head(const LmParams &L, int grid, int threads, hipStream_t 
     }
     hipLaunchKernelGGL(k_lm_head, dim3(grid), dim3(threads), lm_head_lds_bytes(L, threads), s, L);
     hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
+    if (e != hipSuccess || L.sampled) return e;
     hipLaunchKernelGGL(k_lm_pick, dim3(1), dim3(64), 0, s, L, grid);
     return hipGetLastError();
 }

@@ -24,6 +24,7 @@ struct LmParams {
     float *best;                     // [grid][2]: (logit, row) of every workgroup
     unsigned *sync;
     int rows;                        // LM-head rows per workgroup
+    bool sampled;                    // logits only: the token is drawn from them (sample_kernels.hip)
 };
 
 hipError_t launch_lm_embed(const LmParams &L, hipStream_t s);

@@ -625,10 +625,20 @@ __global__ void __launch_bounds__(T, 4) k_sample(SampleParams P)
 {
     __shared__ SampleShared<T> s;
     const int tid = threadIdx.x, row = blockIdx.x;
+    int at = row;
+    if (P.pos) {                                           // (uniform)
+        at = *P.pos;
+        if (at < 0 || at >= P.max_seq) return;
+    }
     const SampleRow<T, F16, FEW> R{static_cast<const char *>(P.logits) + (size_t)row * P.stride * (F16 ? 2 : 4), P.vocab};
-    SampleHow how{P.temperature ? P.temperature[row] : 1.f, P.top_p ? P.top_p[row] : 1.f, P.min_p ? P.min_p[row] : 0.f, P.uniform[row], P.top_k ? P.top_k[row] : 0};
+    SampleHow how{P.temperature ? P.temperature[row] : 1.f, P.top_p ? P.top_p[row] : 1.f, P.min_p ? P.min_p[row] : 0.f, P.uniform[at], P.top_k ? P.top_k[row] : 0};
     int shown = -1;                                        // tokens that the filters keep, where that is known beforehand
     auto answer = [&](int token, float prob, int kept) {
+        if (P.pos) {
+            P.tokens[at + 1] = max(token, 0);
+            *P.pos = at + 1;
+            return;
+        }
         P.tokens[row] = token;
         if (P.probs) P.probs[row] = prob;
         if (P.kept) P.kept[row] = shown >= 0 ? shown : kept;
@@ -636,15 +646,15 @@ __global__ void __launch_bounds__(T, 4) k_sample(SampleParams P)
     for (int b = tid; b < kBins; b += T) { s.count[b] = 0u; s.mass[b] = 0ull; }
     if (!(how.tau > 0.f) || how.top_k == 1 || how.top_p <= 0.f) {              // (uniform) the first of the order
         float most = -INFINITY;
-        int at = 0x7fffffff;
+        int first = 0x7fffffff;
         R.each([&](f32x4 v, int i) {
 #pragma unroll
             for (int c = 0; c < 4; ++c)
-                if (v[c] > most) { most = v[c]; at = i + c; }                  // (a thread's indexes rise)
+                if (v[c] > most) { most = v[c]; first = i + c; }               // (a thread's indexes rise)
         });
         if (tid == 0) s.first = 0x7fffffffu;
         const float all = block_max(s, 0, most);
-        if (most == all && at != 0x7fffffff) atomicMin(&s.first, (unsigned)at);
+        if (most == all && first != 0x7fffffff) atomicMin(&s.first, (unsigned)first);
         __syncthreads();
         if (tid == 0) {
             if (s.first == 0x7fffffffu) answer(-1, 0.f, 0);

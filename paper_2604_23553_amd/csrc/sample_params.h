@@ -19,6 +19,9 @@ struct SampleParams {
     int *tokens;
     float *probs;                    // or null
     int *kept;                       // or null
+    // a generation loop's row, or null: uniform is that of the position, the token goes to tokens[position + 1] (0 where there is none) and the position advances
+    int *pos;
+    int max_seq;
 };
 
 hipError_t launch_sample(const SampleParams &P, int type, int n_rows, hipStream_t s);

@@ -194,3 +194,165 @@ def test_outputs_that_are_not_wanted_and_replays():
         cf.cfpp_sample(gx, cf.TYPE_F32, n, vocab, how, tokens, stream=stream())
         assert torch.equal(tokens, again) and not torch.equal(tokens, first)
         gu.copy_(f32(u))
+
+
+# ---- the generation loop -----------------------------------------------------------------------------
+def test_generation_with_sampling():
+    """The captured loop against its calls one by one, and every token against the plain form on the logits that the step left"""
+    import synth
+    from tests.test_gpu_generate import SHAPE, VOCAB, _device, _world
+    S, steps = 21, 24
+    cap, layers, kv, head, embed, tokens = _world(99, S, steps)
+    rng = np.random.default_rng(12)
+    u = rng.random(cap, dtype=np.float32)
+    g = dict(uniform=f32(u), temperature=f32([0.8]), top_k=i32([200]), top_p=f32([0.9]), min_p=f32([0.001]))
+    how = cf.Sampling.of(**g)
+    runs = []
+    for graph in (True, False):
+        ds = _device(cap, layers, kv, head, embed, S, 2 if graph else 0)
+        try:
+            ds.set_tokens(tokens, S)
+            if graph:
+                cf.cfpp_generate_sample_capture(ds.ctx, ds.packed, ds.kv, ds.lm, how, ds.tokens, ds.pos, ds.x, ds.out, ds.logits, ds.s)
+            out = []
+            for step in range(steps):
+                if graph:
+                    ds.replay()
+                else:
+                    cf.cfpp_lm_embed(ds.ctx, ds.lm, ds.tokens, ds.pos, ds.x, ds.s)
+                    cf.cfpp_stack_decode(ds.ctx, ds.packed, ds.kv, ds.x, ds.pos, 1, ds.out, ds.s)
+                    cf.cfpp_lm_sample(ds.ctx, ds.lm, ds.out, how, ds.tokens, ds.pos, ds.logits, ds.s)
+                ds.stream.synchronize()
+                assert int(ds.pos[0].item()) == S + step + 1
+                token, logits = int(ds.tokens[S + step + 1].item()), ds.logits.cpu().numpy().copy()
+                r = page8_ref.sample(logits, temperature=0.8, top_k=200, top_p=0.9, min_p=0.001, uniform=u[S + step])
+                at = int(np.nonzero(r["order"] == token)[0][0])
+                before, off = r["sums"][at - 1] if at else 0.0, 2 * (r["sums"][-1] * 2.0 ** -40 + VOCAB * 2.0 ** -46)
+                assert at < r["kept"] and before <= r["target"] + off and r["sums"][at] >= r["target"] - off
+                out.append((token, logits))
+            ds.check()
+            runs.append(out)
+            # past the end nothing is drawn
+            ds.pos[:1].fill_(cap)
+            torch.cuda.synchronize()
+            was = ds.tokens.clone()
+            cf.cfpp_lm_sample(ds.ctx, ds.lm, ds.out, how, ds.tokens, ds.pos, ds.logits, ds.s)
+            ds.stream.synchronize()
+            assert torch.equal(was, ds.tokens) and int(ds.pos[0].item()) == cap
+        finally:
+            ds.close()
+    assert len({t for t, _ in runs[0]}) > 3
+    # the head alone leaves the same logits whether the token is drawn or picked
+    ds = _device(cap, layers, kv, head, embed, S, 0)
+    try:
+        ds.set_tokens(tokens, S)
+        ds.generate_step(want_logits=True)
+        ds.stream.synchronize()
+        assert np.array_equal(ds.logits.cpu().numpy(), runs[1][0][1])
+        greedy = int(ds.tokens[S + 1].item())
+        ds.set_tokens(tokens, S)
+        cold = cf.Sampling.of(uniform=g["uniform"], temperature=f32([0.0]))
+        cf.cfpp_lm_sample(ds.ctx, ds.lm, ds.out, cold, ds.tokens, ds.pos, ds.logits, ds.s)
+        ds.stream.synchronize()
+        assert int(ds.tokens[S + 1].item()) == greedy
+        for bad in (dict(logits_dev=0), dict(how=cf.Sampling.of(uniform=0))):
+            with pytest.raises(cf.CfppError) as e:
+                cf.cfpp_lm_sample(ds.ctx, ds.lm, ds.out, bad.get("how", cold), ds.tokens, ds.pos, bad.get("logits_dev", ds.logits), ds.s)
+            assert e.value.status == -1
+    finally:
+        ds.close()
+
+
+# ---- a server's step ----------------------------------------------------------------------------------
+@pytest.mark.parametrize("type", [page8_ref.INT8, page8_ref.E4M3])
+def test_a_servers_steps(type):
+    """Tables, plan, append and attention of two layers, logits and sampling, captured once and replayed: requests grow over page borders, one ends and begins
+    anew, one has no row.  Every operator's result against the plain form on what the step before it left."""
+    from tests import tree_ref
+    rng = np.random.default_rng(type)
+    R, H, kv, d, page, vocab, layers, stride = 5, 4, 2, 64, 16, 999, 2, 6
+    h, n_pages = H * d, 24
+    lens = [14, 0, 31, 60, 7]
+    alloc = tree_ref.Allocator(n_pages, page, R, stride, rng)
+    pools = [page8_ref.Pool(n_pages, page, kv, d, type) for _ in range(layers)]
+    # what the requests have cached before
+    alloc.step([0] * R, lens, sum(lens))
+    for pool in pools:
+        for r in range(R):
+            for t in range(lens[r]):
+                pool.put(alloc.tables[r][t // page] * page + t % page, *rng.standard_normal((2, kv, d)).astype(np.float16))
+    half = lambda *n: dev((rng.standard_normal(n) / np.sqrt(n[0])).astype(np.float16))  # noqa: E731
+    embed, w_out = dev(rng.standard_normal((vocab, h)).astype(np.float16)), half(h, vocab)
+    w = [(half(h, h), half(h, kv * d), half(h, kv * d), half(h, h)) for _ in range(layers)]
+    table = np.full((R, stride), -1, dtype=np.int32)
+    for r, t in enumerate(alloc.tables):
+        table[r, :len(t)] = t
+    free = np.full(n_pages, -1, dtype=np.int32)
+    free[:len(alloc.free)] = alloc.free
+    g = dict(lens=i32(lens), counts=i32([1] * R), table=i32(table), held=i32([len(t) for t in alloc.tables]), free=i32(free), free_count=i32([len(alloc.free)]),
+             granted=i32([0] * R), row_start=i32([0] * (R + 1)), slots=i32([0] * R), parents=i32([-1] * R), masks=i32([[0]] * R), positions=i32([0] * R),
+             tokens=i32(rng.integers(0, vocab, R)), kept=i32([0] * R), uniform=f32(np.zeros(R)), top_p=f32([0.9] * R), top_k=i32([0, 40, 0, 40, 0]),
+             temperature=f32([1.0, 0.7, 0.0, 1.5, 1.0]), probs=f32([0] * R))
+    P = cf.Pages(n_pages, page, kv, d)
+    plan = torch.empty(cf.cfpp_tree_plan_bytes(P, H, R, R, 1), dtype=torch.uint8, device="cuda")
+    batch = cf.TreeBatch.of(1, g["lens"], g["row_start"], g["table"], g["slots"], g["parents"], g["masks"], g["positions"], plan)
+    how = cf.Sampling.of(uniform=g["uniform"], temperature=g["temperature"], top_k=g["top_k"], top_p=g["top_p"])
+    g_pools = [dev(p.bytes) for p in pools]
+    q, k, v, o = (torch.zeros((layers, R, n), dtype=torch.float16, device="cuda") for n in (h, kv * d, kv * d, h))
+    logits = torch.zeros((R, vocab), dtype=torch.float32, device="cuda")
+
+    def step():
+        s = stream()
+        cf.cfpp_page_tables(P, batch, g["counts"], g["held"], g["free"], g["free_count"], g["granted"], s)
+        cf.cfpp_tree_plan(P, batch, H, s)
+        x = embed[g["tokens"].long()]
+        for l in range(layers):
+            for to, by in zip((q, k, v), w[l]):
+                torch.matmul(x, by, out=to[l])
+            cf.cfpp_page8_append(P, type, g_pools[l], k[l], v[l], g["slots"], R, stream=s)
+            cf.cfpp_page8_attention(P, type, g_pools[l], batch, q[l], H, o[l], stream=s)
+            x = x + torch.matmul(o[l], w[l][3])
+        logits.copy_(torch.matmul(x, w_out))
+        cf.cfpp_sample(logits, cf.TYPE_F32, R, vocab, how, g["tokens"], g["probs"], g["kept"], stream=s)
+
+    # (the first call of a library product may not be captured)
+    torch.matmul(embed[:R], w[0][0])
+    torch.matmul(embed[:R], w[0][1])
+    torch.matmul(embed[:R], w_out)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        step()
+    counts = [1] * R
+    for n in range(12):
+        if n == 5:
+            lens[2] = 0                                     # a request ends, another begins in its place
+        counts[4] = 0 if n in (3, 4) else 1                # the last one pauses
+        u = rng.random(R, dtype=np.float32)
+        g["lens"].copy_(i32(lens))
+        g["counts"].copy_(i32(counts))
+        g["uniform"].copy_(f32(u))
+        o.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        granted, starts, slots = alloc.step(lens, counts, R)
+        assert granted == [1] * R and np.array_equal(g["slots"].cpu().numpy(), slots) and g["row_start"].cpu().tolist() == starts
+        for l in range(layers):
+            kk, vv, qq, got = (t[l].cpu().numpy() for t in (k, v, q, o))
+            for r in range(R):
+                if not counts[r]:
+                    assert (got[r] == 7.0).all()           # (the last row is nobody's then)
+                    continue
+                pools[l].put(int(slots[r]), kk[r].reshape(kv, d), vv[r].reshape(kv, d))
+                rows = np.stack([pools[l].get(alloc.tables[r][t // page] * page + t % page) for t in range(lens[r] + 1)], 1)
+                want, off = page8_ref.attend(qq[r].astype(np.float64).reshape(1, H, d), rows[0], rows[1], np.ones((1, lens[r] + 1), dtype=bool))
+                limit = np.abs(want) * 2.0 ** -11 + 2.0 ** -25 + off * (1 + 2.0 ** -11)
+                assert (np.abs(got[r].astype(np.float64).reshape(1, H, d) - want) <= limit).all(), f"step {n}, layer {l}, request {r}"
+        x, tokens, probs, kept = (t.cpu().numpy() for t in (logits, g["tokens"], g["probs"], g["kept"]))
+        for r in range(R):
+            page8_ref.check_sample(x[r], (int(tokens[r]), float(probs[r]), int(kept[r])), uniform=float(u[r]), temperature=[1.0, 0.7, 0.0, 1.5, 1.0][r],
+                                   top_k=[0, 40, 0, 40, 0][r], top_p=0.9)
+        for r in range(R):
+            lens[r] += counts[r]

@@ -85,6 +85,14 @@ def test_refusals_of_sampling():
     cf.cfpp_sample(x + 2, cf.TYPE_F16, 0, 100, cf.Sampling.of(uniform=x), x)
 
 
+def test_the_loop_without_a_context():
+    x, how = 65536, cf.Sampling.of(uniform=65536)
+    lm = cf.Lm.of(x, x, x, x, 100)
+    assert refused(cf.cfpp_lm_sample, 0, lm, x, how, x, x, x) == -1
+    assert refused(cf.cfpp_generate_sample_capture, 0, [x], [x], lm, how, x, x, x, x, x, x) == -1
+    assert cf.lib().cfpp_generate_sample_capture(None, None, None, None, None, None, None, None, None, None, None) == -1
+
+
 # ---- the plain forms -------------------------------------------------------------------------
 def test_e4m3_by_hand():
     v = page8_ref.E4M3_VALUES
