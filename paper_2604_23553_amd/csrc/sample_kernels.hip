@@ -138,7 +138,8 @@ struct SampleRow {
         typedef L L4 __attribute__((ext_vector_type(4), aligned(sizeof(L))));
         const CFPP_GLOBAL L *p = (const CFPP_GLOBAL L *)at;
         if constexpr (FEW) {
-            return f32x4{(float)p[0], (float)p[min(1, vocab - 1)], (float)p[vocab - 1], 0.f};
+            const float last = (float)p[vocab - 1];
+            return f32x4{(float)p[0], (float)p[min(1, vocab - 1)], last, last};         // (the histogram's reference is one of the row's)
         } else {
             const L4 x = *(const CFPP_GLOBAL L4 *)(p + min(i, vocab - 4));
             return f32x4{(float)x[0], (float)x[1], (float)x[2], (float)x[3]};

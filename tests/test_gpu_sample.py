@@ -145,6 +145,17 @@ def test_logits_that_are_no_numbers_or_infinite(dtype):
         assert got[2] == got[3] == (-1, 0.0, 0) and got[6][0] == vocab - 1
 
 
+@pytest.mark.parametrize("dtype", [np.float32, np.float16])
+@pytest.mark.parametrize("vocab", [1, 2, 3, 4, 5])
+def test_few_logits_far_from_zero(vocab, dtype):
+    rng = np.random.default_rng(vocab)
+    n = 24
+    x = (np.repeat([-1e4, -100.0, -30.0, 30.0, 100.0, 1e4], 4)[:, None] + np.round(2 * rng.standard_normal((n, vocab)), 1)).astype(dtype)
+    u = rng.random(n, dtype=np.float32)
+    for how in (dict(), dict(temperature=3.0), dict(top_k=2), dict(top_p=0.7), dict(min_p=0.2), dict(top_k=2, top_p=0.9, min_p=0.01)):
+        check(x, uniform=u, **how)
+
+
 def test_random_numbers_out_of_range():
     rng = np.random.default_rng(8)
     x = model_logits(rng, 6, 700)
