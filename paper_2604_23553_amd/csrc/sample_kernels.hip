@@ -8,8 +8,8 @@
 // bin's tokens - some hundred of them for a usual row - are collected, and each finds its own place among them.  A bin of more than kList is cut again by the
 // bits of its logits, and equal logits by their index, until few are left.  Two or three passes over the row, the first from memory.
 //
-// The histogram is laid from the largest of the row's first logits, which is known before the others have arrived; only where a later one stands more than
-// 2^16 above it, or where the first are all masked, is it laid again.
+// The histogram is laid from the largest of the row's first logits, which is known before the others have arrived; only where a later one's weight is more than
+// 2^16 times its own, or where the first are all masked and the others stand below zero, is it laid again.
 //
 // Sums are exact: a bin's tokens add 2^(their place in the bin), which is near 1, as whole multiples of 2^-44 with a relative error of 2^-43, and the bin's sum, or
 // that of the first of its tokens, is scaled by 2^(-bin / 32) once, by a product of whole numbers that is cut off.  Whole numbers add up to the same
@@ -19,9 +19,6 @@
 #include <hip/hip_fp16.h>
 #include "sample_params.h"
 #include "device_utils.h"
-
-// A token's weight is worked out in several places and has to be the same number in all of them: no product joins a sum but where fma() says so.
-#pragma clang fp contract(off)
 
 // A token's bin and its place in it are worked out in several places and have to be the same numbers in all of them: no product joins a sum but where
 // fma() says so.
@@ -332,7 +329,8 @@ __device__ __forceinline__ bool sample_row(SampleShared<Row::kThreads> &s, const
                 }
                 // infinite, or so steep that only what equals it has a weight: one step of the largest number is more bins than there are
                 if (most == INFINITY || (double)fabsf(most) * slope > 0x1p40) return false;
-                if (depth_of(most) < 0.f) {                // (uniform) out of reach: the histogram from the largest on
+                // (uniform) out of reach, or below the zero that stands in for first logits that are all masked: the histogram from the largest on
+                if (depth_of(most) < 0.f || depth_of(most) > kAbove) {
                     refer(most);
                     if (!small) {
                         n = 0;

@@ -156,6 +156,21 @@ def test_few_logits_far_from_zero(vocab, dtype):
         check(x, uniform=u, **how)
 
 
+@pytest.mark.parametrize("dtype", [np.float32, np.float16])
+@pytest.mark.parametrize("first", [-np.inf, np.nan, -3e4, -60.0])
+def test_a_beginning_that_is_masked_or_far_below(first, dtype):
+    """The first 17000 logits, and all but the last 300, in rows whose others stand about a value from far below zero to far above it"""
+    rng = np.random.default_rng(31)
+    n, vocab = 24, 20000
+    about = np.repeat([-2000.0, -100.0, -18.0, -0.5, 25.0, 1000.0], 4)
+    x = (about[:, None] + 2.0 * rng.standard_normal((n, vocab))).astype(dtype)
+    for r in range(n):
+        x[r, :17000 if r % 2 else vocab - 300] = first
+    u = rng.random(n, dtype=np.float32)
+    for how in (dict(), dict(top_k=40), dict(top_k=600), dict(top_p=0.9), dict(min_p=0.05), dict(top_k=600, top_p=0.8, min_p=0.01), dict(temperature=0.3), dict(temperature=4.0)):
+        check(x, uniform=u, **how)
+
+
 def test_random_numbers_out_of_range():
     rng = np.random.default_rng(8)
     x = model_logits(rng, 6, 700)
