@@ -420,7 +420,8 @@ __device__ __forceinline__ bool sample_row(SampleShared<Row::kThreads> &s, const
             const int m_lo = (int)fmin(fmax(at - 0.01, 0.0), (double)kBins), m_hi = (int)fmin(fmax(at + 0.01, 0.0), (double)kBins);
             by_list = by_p && bin <= m_hi;
             if (!by_p || bin >= m_lo) {                    // (uniform)
-                const float from = m_lo < kBins ? (float)m_lo : (float)at, to = m_lo < kBins ? (float)(m_hi + 1) : from;
+                // (behind the last bin nothing has a weight that counts, but it does as a token kept)
+                const float from = m_lo < kBins ? (float)m_lo : (float)(at - 0.01), to = m_lo < kBins ? (float)(m_hi + 1) : (float)(at + 0.01);
                 unsigned n = 0;
                 u64 in[2] = {0, 0};
                 some([&](float v) {
@@ -437,6 +438,7 @@ __device__ __forceinline__ bool sample_row(SampleShared<Row::kThreads> &s, const
                 u64 none_of;
                 block_scan(s, turn ^= 1, n, in[0], none, none_of, kept_m, in[0]);
                 block_scan(s, turn ^= 1, 0u, in[1], none, none_of, n, in[1]);
+                kept_m = min(kept_m, (unsigned)n_k);       // (those before the bins are numbered wherever top-k ends)
                 mass_m = m_lo < kBins ? s.mass[m_lo] : all_mass;
                 if (m_lo < kBins && in[0]) mass_m = s.mass[m_lo] + scaled(m_lo, in[0]);
                 if (m_hi < kBins && m_hi > m_lo && in[1]) mass_m = s.mass[m_hi] + scaled(m_hi, in[1]);

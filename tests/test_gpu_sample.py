@@ -171,6 +171,19 @@ def test_a_beginning_that_is_masked_or_far_below(first, dtype):
         check(x, uniform=u, **how)
 
 
+@pytest.mark.parametrize("min_p", [1e-40, 2.0 ** -70, 1e-15, 2.0 ** -47.5, 1e-6, 0.01, 0.3, 0.9])
+def test_min_p_with_the_others(min_p):
+    """Least weights from below what a sum notices to near the largest, before and behind the place where top-k or top-p ends"""
+    rng = np.random.default_rng(41)
+    n, vocab = 24, 30000
+    x = model_logits(rng, n, vocab)
+    x[8:16] *= 12.0                                        # weights down to 2^-150 of the largest
+    x[16:] = np.round(x[16:])
+    u = rng.random(n, dtype=np.float32)
+    for how in (dict(), dict(top_k=600), dict(top_k=25000), dict(top_p=0.6), dict(top_p=1 - 2.0 ** -24), dict(top_k=600, top_p=0.99), dict(top_k=100), dict(temperature=0.2)):
+        check(x, uniform=u, min_p=min_p, **how)
+
+
 def test_random_numbers_out_of_range():
     rng = np.random.default_rng(8)
     x = model_logits(rng, 6, 700)
