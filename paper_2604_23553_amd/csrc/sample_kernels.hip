@@ -4,17 +4,21 @@
 // order - k tokens; as many as reach p of those k tokens' sum; those of at least min_p times the largest weight - and the token drawn is the first whose running sum
 // passes u times the sum of what is kept.  So all of it is the same question: where, in the order, does a running count or a running sum reach a target?
 //
-// Nothing is sorted.  A histogram over the logits in steps of 2^(1/32) of a weight, 2048 bins of counts or of sums in LDS, says in which bin that is; the
+// Nothing is sorted.  A histogram over the logits in steps of 2^(1/32) of a weight, 4096 bins of counts or of sums in LDS, says in which bin that is; the
 // bin's tokens - some hundred of them for a usual row - are collected, and each finds its own place among them.  A bin of more than kList is cut again by the
 // bits of its logits, and equal logits by their index, until few are left.  Two or three passes over the row, the first from memory.
 //
 // The histogram is laid from the largest of the row's first logits, which is known before the others have arrived; only where a later one's weight is more than
-// 2^16 times its own, or where the first are all masked and the others stand below zero, is it laid again.
+// 2^64 times its own, or where the first are all masked and the others stand below zero, is it laid again.
 //
 // Sums are exact: a bin's tokens add 2^(their place in the bin), which is near 1, as whole multiples of 2^-44 with a relative error of 2^-43, and the bin's sum, or
 // that of the first of its tokens, is scaled by 2^(-bin / 32) once, by a product of whole numbers that is cut off.  Whole numbers add up to the same
 // whichever wavefront comes first, and a border between two tokens is where 64-bit arithmetic has it but for 2^-40 of the sum.  With weights in fp32 it would
 // be up to 2^-24 off, which is another token once in some hundred thousand rows.
+//
+// Bound by one CU's instructions and by the way of a pass's first logits, not by memory: of a row's 27 us the pass that lays sums takes 12, 4 of them the weights, the
+// sums over the bins 2, each pass that collects 4.  50304 logits in fp32, top-p: one row 28.0 us; 64 rows, top-k of 50, top-p and min-p 19.4 us; 512 rows of
+// different settings 65 to 70 us, 1.5 TB/s.  A row's logits do not fit its registers, and a row on more than one CU would need a workspace of the caller's.
 #include <hip/hip_runtime.h>
 #include <hip/hip_fp16.h>
 #include "sample_params.h"
@@ -28,9 +32,11 @@ namespace cfpp {
 
 typedef unsigned long long u64;
 
-constexpr int kBins = 2048, kList = 512, kBinsToOctave = 32;
-constexpr float kAbove = 512.f;                            // bins above the reference
-// Rows up to which a row has a CU's 1024 threads; more, and two rows share it
+constexpr int kBins = 4096, kCut = 2048, kList = 512, kBinsToOctave = 32;     // kCut: bins of a bin's own histogram
+// Bins above the reference; as many below it.  (512 of 2048: 0.4 us less, but where the histogram of one of 64 rows is laid again 59.3 us for 35.0.)
+constexpr float kAbove = 2048.f;
+// Rows up to which a row has a CU's 1024 threads; more, and two rows share it.  (One row 27.5 us, with 512 threads 30.4; 64 rows 19.0 and 21.9; 512 rows, each with
+// 1024 threads, 78.7 and 70.7.)
 constexpr int kSampleOneEach = 256;
 
 // larger logits have larger keys (no NaN)
@@ -84,8 +90,9 @@ __device__ __forceinline__ u64 lane_value(u64 v, int lane) { return (u64)lane_va
 template <int T>
 struct SampleShared {
     static constexpr int kWaves = T / 64;
-    u64 mass[kBins];                                       // sums of the bins, then those of all bins before
-    unsigned count[kBins];
+    // sums of the bins, then those of all bins before; or the same of counts, behind the first half; or kCut of both
+    u64 mass[kBins];
+    __device__ __forceinline__ unsigned &count(int b) { return reinterpret_cast<unsigned *>(mass + kCut)[b]; }
     u64 place[kList], weight[kList], ahead[kList];         // the list's tokens; their weights; the sum of those before, of the same bin
     unsigned rank[kList];
     u64 wave_mass[2][kWaves];
@@ -125,7 +132,7 @@ __device__ __forceinline__ float max4(f32x4 v, float m) { return fmaxf(fmaxf(m, 
 // A row's logits, four to a thread that follow one another; what lies behind the row as minus infinity, a NaN stays one.  FEW: of less than four
 template <int T, bool F16, bool FEW>
 struct SampleRow {
-    static constexpr int kThreads = T, STEP = 4 * T, AT = FEW ? 1 : 4;         // four vectors are on their way while four others are looked at
+    static constexpr int kThreads = T, STEP = 4 * T, AT = FEW ? 1 : 2;         // two vectors are on their way while two others are looked at (four as fast, and registers spilled; one 20.7 us for 18.9 with 64 rows)
     const void *at;
     int vocab;
     // (the last ones of the row in place of those behind it; rows may begin at any logit)
@@ -190,11 +197,11 @@ struct SampleRow {
 struct SampleHow { float tau, top_p, min_p, uniform; int top_k; };
 
 // The token of a row.  LEVEL: the tokens that equal `most` weigh one and all others nothing; otherwise `most` is found here.  false: the weights are like
-// that, `most` is set and nothing is answered.  s.mass and s.count are zero.
+// that, `most` is set and nothing is answered.  s.mass is zero.
 template <bool LEVEL, class Row, class Answer>
 __device__ __forceinline__ bool sample_row(SampleShared<Row::kThreads> &s, const Row &R, const SampleHow &how, float &most, Answer answer)
 {
-    constexpr int T = Row::kThreads, EACH = kBins / T;
+    constexpr int T = Row::kThreads, EACH = kBins / T, EACH_CUT = kCut / T;
     const int tid = threadIdx.x;
     // bins to a logit; at least so many that infinite differences stay infinite (the largest finite one is no thousandth of a bin then), at most so many that
     // none becomes NaN
@@ -247,11 +254,11 @@ __device__ __forceinline__ bool sample_row(SampleShared<Row::kThreads> &s, const
     int n_k = by_k ? how.top_k : R.vocab;                  // (at most so many: minus infinities are found later)
     u64 k_place = ~0ull;                                   // of the last token that top-k keeps
 
-    // kStageAll: the few tokens that top-k leaves, and some more, are in the list: all filters there.  Otherwise the places where top-k ends, where top-p or min-p
-    // does, whichever comes first, and of the draw, one after the other
+    // kStageAll: the few tokens that top-k leaves, and some more, are in the list: all filters there (64 rows of 50304 18.9 us with a k of 50 and 38.2 with 480; 40.0 and 41.6
+    // otherwise).  Otherwise the places where top-k ends, where top-p or min-p does, whichever comes first, and of the draw, one after the other
     enum { kStageAll, kStageK, kStageCut, kStageDraw };
     const int behind_k = by_p || by_m ? kStageCut : kStageDraw;
-    int stage = small || (by_k && n_k <= kList / 2) ? kStageAll : by_k ? kStageK : behind_k;
+    int stage = small || (by_k && n_k <= kList) ? kStageAll : by_k ? kStageK : behind_k;
     enum { kNone, kCounts, kMasses };
     int built = kNone;                                     // what the histogram holds: running numbers or sums of the bins before
     bool dirty = false, known = LEVEL, cut = false;        // the histogram is to be cleared; `most` is known; top-p or min-p has cut
@@ -261,7 +268,7 @@ __device__ __forceinline__ bool sample_row(SampleShared<Row::kThreads> &s, const
     int turn = 0;
     auto clear = [&]() {
         __syncthreads();
-        for (int b = tid; b < kBins; b += T) { s.count[b] = 0u; s.mass[b] = 0ull; }
+        for (int b = tid; b < kBins; b += T) s.mass[b] = 0ull;
         __syncthreads();
     };
     auto drawn = [&](u64 sum) {
@@ -299,7 +306,7 @@ __device__ __forceinline__ bool sample_row(SampleShared<Row::kThreads> &s, const
                     if (counts) {                          // (uniform)
 #pragma unroll
                         for (int c = 0; c < 4; ++c)
-                            if (v[c] > -INFINITY) atomicAdd(&s.count[bin_of(v[c])], 1u);
+                            if (v[c] > -INFINITY) atomicAdd(&s.count(bin_of(v[c])), 1u);
                         return;
                     }
                     if (by_k) {                            // (uniform)
@@ -350,15 +357,15 @@ __device__ __forceinline__ bool sample_row(SampleShared<Row::kThreads> &s, const
                 for (int b = 0; b < EACH; ++b) {
                     c[b] = c0;
                     m[b] = m0;
-                    if (counts) c0 += s.count[EACH * tid + b];
-                    else m0 += scaled(EACH * tid + b, s.mass[EACH * tid + b]);
+                    if (counts) c0 += s.count(EACH * tid + b);
+                    else if (const u64 in = s.mass[EACH * tid + b]) m0 += scaled(EACH * tid + b, in);       // (most of the bins have nothing)
                 }
                 unsigned c1;
                 u64 m1;
                 block_scan(s, turn ^= 1, c0, m0, c1, m1, all_count, all_mass);
 #pragma unroll
                 for (int b = 0; b < EACH; ++b) {
-                    if (counts) s.count[EACH * tid + b] = c1 + c[b];
+                    if (counts) s.count(EACH * tid + b) = c1 + c[b];
                     else s.mass[EACH * tid + b] = m1 + m[b];
                 }
                 if (!counts && !cut) {
@@ -391,7 +398,7 @@ __device__ __forceinline__ bool sample_row(SampleShared<Row::kThreads> &s, const
 #pragma unroll
             for (int k = 0; k < EACH; ++k) {
                 const int b = EACH * tid + k;
-                const u64 from = counts ? s.count[b] : s.mass[b], to = b + 1 < kBins ? (counts ? s.count[b + 1] : s.mass[b + 1]) : counts ? all_count : all_mass;
+                const u64 from = counts ? s.count(b) : s.mass[b], to = b + 1 < kBins ? (counts ? s.count(b + 1) : s.mass[b + 1]) : counts ? all_count : all_mass;
                 if (from < target && target <= to) {
                     s.bin = b; s.other = (int)min(to, (u64)kBins); s.before_count = (unsigned)from; s.before_mass = from;
                 }
@@ -494,29 +501,29 @@ __device__ __forceinline__ bool sample_row(SampleShared<Row::kThreads> &s, const
                 if (depth == 1 && k_lo == k_hi) { depth = 2; i_lo = 0; i_hi = R.vocab - 1; }
                 const unsigned span = depth == 1 ? k_hi - k_lo : (unsigned)(i_hi - i_lo);
                 int shift_by = 0;
-                while (span >> shift_by >= (unsigned)kBins) ++shift_by;
+                while (span >> shift_by >= (unsigned)kCut) ++shift_by;
                 clear();
                 built = kNone;
                 some(near, [&](float v, int i) {
                     if (!inside(v, i)) return;
                     const unsigned b = (depth == 1 ? k_hi - sample_key(v) : (unsigned)(i - i_lo)) >> shift_by;
-                    atomicAdd(&s.count[b], 1u);
+                    atomicAdd(&s.count((int)b), 1u);
                     if (!counts) atomicAdd(&s.mass[b], weight_in(v, bin));
                 });
                 __syncthreads();
                 unsigned c = 0, none;
                 u64 m = 0, none_of;
 #pragma unroll
-                for (int k = 0; k < EACH; ++k) { c += s.count[EACH * tid + k]; m += s.mass[EACH * tid + k]; }
+                for (int k = 0; k < EACH_CUT; ++k) { c += s.count(EACH_CUT * tid + k); m += s.mass[EACH_CUT * tid + k]; }
                 block_scan(s, turn ^= 1, c, m, c, m, none, none_of);
                 c += before_count;
                 m += before_in;
 #pragma unroll
-                for (int k = 0; k < EACH; ++k) {
-                    const unsigned cb = s.count[EACH * tid + k];
-                    const u64 mb = s.mass[EACH * tid + k];
+                for (int k = 0; k < EACH_CUT; ++k) {
+                    const unsigned cb = s.count(EACH_CUT * tid + k);
+                    const u64 mb = s.mass[EACH_CUT * tid + k];
                     if (counts ? c < target && target <= c + cb : before_mass + scaled(bin, m) < target && target <= before_mass + scaled(bin, m + mb)) {
-                        s.other = EACH * tid + k; s.before_count = c; s.value = m;
+                        s.other = EACH_CUT * tid + k; s.before_count = c; s.value = m;
                     }
                     c += cb; m += mb;
                 }
@@ -644,7 +651,7 @@ __global__ void __launch_bounds__(T, 4) k_sample(SampleParams P)
         if (P.probs) P.probs[row] = prob;
         if (P.kept) P.kept[row] = shown >= 0 ? shown : kept;
     };
-    for (int b = tid; b < kBins; b += T) { s.count[b] = 0u; s.mass[b] = 0ull; }
+    for (int b = tid; b < kBins; b += T) s.mass[b] = 0ull;
     if (!(how.tau > 0.f) || how.top_k == 1 || how.top_p <= 0.f) {              // (uniform) the first of the order
         float most = -INFINITY;
         int first = 0x7fffffff;
@@ -678,7 +685,7 @@ __global__ void __launch_bounds__(T, 4) k_sample(SampleParams P)
         shown = how.top_k > 0 ? min(how.top_k, (int)valid) : (int)valid;
     }
     __syncthreads();
-    for (int b = tid; b < kBins; b += T) { s.count[b] = 0u; s.mass[b] = 0ull; }
+    for (int b = tid; b < kBins; b += T) s.mass[b] = 0ull;
     __syncthreads();
     sample_row<true>(s, R, how, most, answer);
 }
