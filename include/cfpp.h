@@ -589,8 +589,9 @@ cfpp_status cfpp_page8_attention(const cfpp_pages *pages, int32_t type, const vo
  *                 whose running sum is above uniform times the sum of what is kept is
  *                 drawn (below 0 or NaN count as 0; from 1 on: the last that has a weight)
  * Logits that are minus infinity or NaN are no part of the order.  Where the largest is plus
- * infinity, those that are weigh 1 and all others 0.  Weights are rounded to multiples of 2^-45 of
- * the largest and added exactly: the token does not depend on how the sum is split. */
+ * infinity, those that are weigh 1 and all others 0.  Weights are whole multiples of a small number
+ * and are added exactly: a token does not depend on how a sum is split, and a border between two
+ * tokens is off by at most 2^-40 of the sum and 2^-44 of the largest weight for each token. */
 typedef struct cfpp_sampling {
     const float *temperature;
     const int32_t *top_k;

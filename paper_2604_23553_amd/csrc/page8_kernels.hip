@@ -8,6 +8,9 @@
 // V lies by dimension, 16 positions to 16 bytes, so what can be written at once are rows whose slots follow one another inside of a granule:
 // a run.  A workgroup has the runs that begin in 16 rows of the call - up to 31 rows - for a few heads of K or of V; V's codes meet in LDS.  A single row to a
 // run, as in a decode step, writes its V codes byte by byte.
+//
+// Bound by memory where there are many rows (append of 4096 rows of 32 heads of 128, 101 MB: 23.7 us, 4.3 TB/s), by launch and one way to memory and back where there are
+// few (64 rows in pages of their own 5.1 us).
 #include <hip/hip_runtime.h>
 #include <hip/hip_fp16.h>
 #include "tree_params.h"
@@ -195,7 +198,7 @@ __device__ __forceinline__ unsigned p8_read(unsigned c, float a0, float a1)
 }
 
 // V: a thread has two dimensions of a head and all positions of a run, which it writes one after the other, 256 bytes of a row to a wavefront; nothing
-// goes through LDS (16384 rows of 8 heads of 128 27.7 us through it, 23.1 so).
+// goes through LDS (16384 rows of 8 heads of 128, 101 MB: 27.7 us through it, 24.1 so, 4.2 TB/s; a large copy has 4.6).
 template <int D, bool INT8, bool FEW>
 __global__ void __launch_bounds__(256) k_page8_read(Page8Rows P)
 {
@@ -258,7 +261,8 @@ __global__ void __launch_bounds__(256) k_page8_read(Page8Rows P)
 }
 
 // Up to so many workgroups of many heads there are some of few: 64 rows of 32 heads of 80, each in a page of its own, are 48 of six heads or 256 of one
-// (append 16.4 and 8.6 us, read of 77 rows 7.4 and 7.3); 4096 rows of hidden 4096 would take 24.0 and 27.4.
+// (kernel alone: append 13.8 and 5.1 us; read of 77 rows 7.6 and 5.3).  Of few always, an append of 4096 rows of 32 heads of 128 takes 32.4 us for 23.7, a read of 16384
+// rows of 8 heads 35.6 for 24.1.
 constexpr int kP8Few = 256;
 template <int D, bool INT8, bool FEW>
 static hipError_t launch_of(const Page8Rows &P, bool append, hipStream_t s)

@@ -235,6 +235,38 @@ def test_outputs_that_are_not_wanted_and_replays():
         gu.copy_(f32(u))
 
 
+@pytest.mark.parametrize("dtype", [np.float32, np.float16])
+def test_rows_that_lie_far_apart(dtype):
+    """row_stride of 2^32 values, its most"""
+    rng = np.random.default_rng(51)
+    vocab, stride = 1001, 1 << 32
+    x, u = model_logits(rng, 2, vocab, dtype), rng.random(2, dtype=np.float32)
+    g = torch.empty(stride + vocab, dtype=torch.float16 if dtype == np.float16 else torch.float32, device="cuda")
+    g[:vocab].copy_(dev(x[0]))
+    g[stride:].copy_(dev(x[1]))
+    tokens, kept, probs = i32([-7] * 2), i32([-7] * 2), f32([-7] * 2)
+    gu = f32(u)
+    cf.cfpp_sample(g, cf.TYPE_F16 if dtype == np.float16 else cf.TYPE_F32, 2, vocab, cf.Sampling.of(uniform=gu), tokens, probs, kept, stride, stream())
+    torch.cuda.synchronize()
+    for r in range(2):
+        page8_ref.check_sample(x[r], (int(tokens[r]), float(probs[r]), int(kept[r])), uniform=float(u[r]))
+
+
+def test_two_streams_at_once():
+    rng = np.random.default_rng(52)
+    x, u = [model_logits(rng, 40, 50304) for _ in range(2)], rng.random(40, dtype=np.float32)
+    want = [[t for t, _, _ in draw(a, uniform=u, top_p=0.9)] for a in x]
+    g, gu, p = [dev(a) for a in x], f32(u), f32([0.9] * 40)
+    how = cf.Sampling.of(uniform=gu, top_p=p)
+    tokens, streams = [i32([-7] * 40) for _ in range(2)], [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for i in range(2):
+            cf.cfpp_sample(g[i], cf.TYPE_F32, 40, 50304, how, tokens[i], stream=streams[i].cuda_stream)
+    torch.cuda.synchronize()
+    assert [t.cpu().numpy().tolist() for t in tokens] == want
+
+
 # ---- the generation loop -----------------------------------------------------------------------------
 def test_generation_with_sampling():
     """The captured loop against its calls one by one, and every token against the plain form on the logits that the step left"""
@@ -298,6 +330,37 @@ def test_generation_with_sampling():
             with pytest.raises(cf.CfppError) as e:
                 cf.cfpp_lm_sample(ds.ctx, ds.lm, ds.out, bad.get("how", cold), ds.tokens, ds.pos, bad.get("logits_dev", ds.logits), ds.s)
             assert e.value.status == -1
+    finally:
+        ds.close()
+
+
+@pytest.mark.parametrize("heads,d,vocab,threads", [(2, 64, 300, 512), (1, 80, 500, 512), (8, 64, 900, 256), (2, 64, 3, 512)])
+def test_a_token_behind_both_kernels_of_the_head(heads, d, vocab, threads):
+    """Twice from the same position: nothing is left behind for the pick of cfpp_lm_next, which follows"""
+    import synth
+    from paper_2604_23553_amd.harness import DeviceStack
+    shape = synth.ModelShape(heads * d, heads, d, 16, 512, n_layers=1, name=f"lm-h{heads * d}")
+    ds = DeviceStack(shape, 8, 1, 1)
+    try:
+        ds.set_options(threads=threads)
+        ds.load_lm(synth.lm_head(shape, 15, vocab=vocab), synth.embedding(shape, 15, vocab=vocab))
+        ds.out[:1].copy_(torch.from_numpy(synth.x_input(shape, 15)))
+        u = np.float32([0.9, 0.37, 0.2, 0.1, 0.0, 0.0, 0.0, 0.0])
+        g = dict(uniform=f32(u), temperature=f32([0.5]))
+        for step in range(2):
+            ds.set_tokens([0, 0], 1)
+            cf.cfpp_lm_sample(ds.ctx, ds.lm, ds.out, cf.Sampling.of(**g), ds.tokens, ds.pos, ds.logits, ds.s)
+            ds.check()
+            logits = ds.logits.cpu().numpy()
+            r = page8_ref.sample(logits, temperature=0.5, uniform=float(u[1]))
+            at = int(np.nonzero(r["order"] == int(ds.tokens[2].item()))[0][0])
+            off = 2 * (r["sums"][-1] * 2.0 ** -40 + vocab * 2.0 ** -46)
+            assert (r["sums"][at - 1] if at else 0.0) <= r["target"] + off and r["sums"][at] >= r["target"] - off
+            assert int(ds.pos[0].item()) == 2
+        ds.set_tokens([0, 0], 1)
+        cf.cfpp_lm_next(ds.ctx, ds.lm, ds.out, ds.tokens, ds.pos, ds.logits, ds.s)
+        ds.check()
+        assert np.array_equal(ds.logits.cpu().numpy(), logits) and int(ds.tokens[2].item()) == int(np.argmax(logits))
     finally:
         ds.close()
 
