@@ -14,7 +14,7 @@
 //
 // Bound by the way of the codes from memory once there are many (32 requests behind 3000 to 8191 of 32 heads of 128: 1.55 GB in 250 us, 6.2 TB/s of the 7.0
 // that reads reach), and by launch, first loads and the join of the pieces where there are few: about 9 us that no split made shorter (one token behind 128 positions of 8
-// heads of 64 6.0 us, behind 4096 of 32 heads of 80 11.5, behind 131072 of one head of 128 with 8 query heads 16.6; 64 requests of up to 3000 positions and 8 heads 48, of
+// heads of 64 6.0 us, behind 4096 of 32 heads of 80 11.5, behind 131072 of two heads of 64 with 8 query heads each 16.6; 64 requests of up to 3000 positions and 8 heads 48, of
 // which 9 and 38 at 6.4 TB/s).  More pieces: 768 to 2048 workgroups 52 to 56 us for the 64 requests; workgroups of 8 wavefronts 54; a third
 // workgroup to a CU needs 20 more registers than head_dim 128 leaves.
 //
@@ -103,7 +103,7 @@ __device__ __forceinline__ float p8_sum4(float v)
 
 // The pieces of a tile of up to 16 query rows, added in order.  Up to kP8Join by the last workgroup that ends, more by the last ones of groups of about as many
 // as there are groups, whose sums the last of these adds: 128 pieces one after the other would be eleven trips to memory of a single workgroup
-// (one token of 8 query heads behind 131072 positions 24.6 -> 16.6 us); 16 are one trip.
+// (one token of two heads of 64 behind 131072 positions 24.6 -> 16.6 us); 16 are one trip.
 constexpr int kP8Join = 16;
 template <int D>
 __device__ __forceinline__ void p8_join(const TreeAttention &P, const TreePlanLayout &L, char *plan, const TreeItem &it, int H, int head, int rows, int *last_one)

@@ -16,9 +16,9 @@
 // whichever wavefront comes first, and a border between two tokens is where 64-bit arithmetic has it but for 2^-40 of the sum.  With weights in fp32 it would
 // be up to 2^-24 off, which is another token once in some hundred thousand rows.
 //
-// Bound by one CU's instructions and by the way of a pass's first logits, not by memory: of a row's 27 us the pass that lays sums takes 12, 4 of them the weights, the
-// sums over the bins 2, each pass that collects 4.  50304 logits in fp32, top-p: one row 28.0 us; 64 rows, top-k of 50, top-p and min-p 19.4 us; 512 rows of
-// different settings 65 to 70 us, 1.5 TB/s.  A row's logits do not fit its registers, and a row on more than one CU would need a workspace of the caller's.
+// Bound by one CU's instructions - the vector units are busy two thirds of a lone row's time - and by the way of a pass's first logits, not by memory: of a row's 27 us the
+// pass that lays sums takes 11, the sums over the bins 2, each pass that collects 4.  50304 logits in fp32: one row, top-p 27.0 us; 64 rows, top-k of 50, top-p and min-p
+// 19.4 us; 512 rows of different settings 63 us, 1.6 TB/s.  A row's logits do not fit its registers, and a row on more than one CU would need a workspace of the caller's.
 #include <hip/hip_runtime.h>
 #include <hip/hip_fp16.h>
 #include "sample_params.h"
@@ -90,9 +90,8 @@ __device__ __forceinline__ u64 lane_value(u64 v, int lane) { return (u64)lane_va
 template <int T>
 struct SampleShared {
     static constexpr int kWaves = T / 64;
-    // sums of the bins, then those of all bins before; or the same of counts, behind the first half; or kCut of both
-    u64 mass[kBins];
-    __device__ __forceinline__ unsigned &count(int b) { return reinterpret_cast<unsigned *>(mass + kCut)[b]; }
+    u64 mass[kBins];                                       // sums of the bins, then those of all bins before
+    unsigned count[kBins];
     u64 place[kList], weight[kList], ahead[kList];         // the list's tokens; their weights; the sum of those before, of the same bin
     unsigned rank[kList];
     u64 wave_mass[2][kWaves];
@@ -127,6 +126,13 @@ __device__ __forceinline__ float block_max(SampleShared<T> &s, int turn, float v
     __syncthreads();
     return uniform(wave_max(s.wave_max[turn][threadIdx.x & (T / 64 - 1)]));
 }
+// a b + c, with c in registers that stay as they are (the compiler copies a constant for every sum that it may overwrite)
+__device__ __forceinline__ double fma_keep(double a, double b, double c)
+{
+    double r;
+    asm("v_fma_f64 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+}
 __device__ __forceinline__ float max4(f32x4 v, float m) { return fmaxf(fmaxf(m, fmaxf(v[0], v[1])), fmaxf(v[2], v[3])); }
 
 // A row's logits, four to a thread that follow one another; what lies behind the row as minus infinity, a NaN stays one.  FEW: of less than four
@@ -140,12 +146,12 @@ struct SampleRow {
     {
         typedef std::conditional_t<F16, _Float16, float> L;
         typedef L L4 __attribute__((ext_vector_type(4), aligned(sizeof(L))));
-        const CFPP_GLOBAL L *p = (const CFPP_GLOBAL L *)at;
         if constexpr (FEW) {
+            const CFPP_GLOBAL L *p = (const CFPP_GLOBAL L *)at;
             const float last = (float)p[vocab - 1];
             return f32x4{(float)p[0], (float)p[min(1, vocab - 1)], last, last};         // (the histogram's reference is one of the row's)
         } else {
-            const L4 x = *(const CFPP_GLOBAL L4 *)(p + min(i, vocab - 4));
+            const L4 x = *(const CFPP_GLOBAL L4 *)((const CFPP_GLOBAL char *)at + (unsigned)min(i, vocab - 4) * (unsigned)sizeof(L));
             return f32x4{(float)x[0], (float)x[1], (float)x[2], (float)x[3]};
         }
     }
@@ -197,7 +203,7 @@ struct SampleRow {
 struct SampleHow { float tau, top_p, min_p, uniform; int top_k; };
 
 // The token of a row.  LEVEL: the tokens that equal `most` weigh one and all others nothing; otherwise `most` is found here.  false: the weights are like
-// that, `most` is set and nothing is answered.  s.mass is zero.
+// that, `most` is set and nothing is answered.  s.mass and s.count are zero.
 template <bool LEVEL, class Row, class Answer>
 __device__ __forceinline__ bool sample_row(SampleShared<Row::kThreads> &s, const Row &R, const SampleHow &how, float &most, Answer answer)
 {
@@ -214,15 +220,15 @@ __device__ __forceinline__ bool sample_row(SampleShared<Row::kThreads> &s, const
         shift = uniform((double)ref * slope + ((double)kAbove - 0.5));
     };
     auto depth_of = [&](float v) { return fmaf(ref - v, slope32, kAbove); };   // (never rises with v; infinite for minus infinity)
-    auto bin_of = [&](float v) { return (int)fminf(fmaxf(depth_of(v), 0.f), kBins - 1.f); };
+    auto bin_of = [&](float v) { return (int)__builtin_amdgcn_fmed3f(depth_of(v), 0.f, kBins - 1.f); };          // (no NaN)
+    auto in_bins = [](float depth) { return __float_as_uint(depth) < __float_as_uint((float)kBins); };            // (neither less than zero nor NaN)
     // 2^(-f / 32) in multiples of 2^-44, f the token's place in its bin from its middle: -1/2 to 1/2
     auto weight_in = [&](float v, int bin) {
         const double f = fma((double)v, -slope, shift) - (double)bin;
-        double p = 161364.9745385843;                      // (fitted to the least relative error, 2^-43.5)
-        p = fma(p, f, -29798760.585014474);
-        p = fma(p, f, 4127059964.301119);
-        p = fma(p, f, -381061692379.1814);
-        p = fma(p, f, 17592186044416.0);
+        double p = fma_keep(161364.9745385843, f, -29798760.585014474);        // (fitted to the least relative error, 2^-43.5)
+        p = fma_keep(p, f, 4127059964.301119);
+        p = fma_keep(p, f, -381061692379.1814);
+        p = fma_keep(p, f, 17592186044416.0);
         return (u64)__double_as_longlong(p + 4503599627370496.0) - 0x4330000000000000ull;      // (2^52 more, and the last bits are the number)
     };
     int top_bin = 0;                                       // the largest logit's
@@ -254,12 +260,12 @@ __device__ __forceinline__ bool sample_row(SampleShared<Row::kThreads> &s, const
     int n_k = by_k ? how.top_k : R.vocab;                  // (at most so many: minus infinities are found later)
     u64 k_place = ~0ull;                                   // of the last token that top-k keeps
 
-    // kStageAll: the few tokens that top-k leaves, and some more, are in the list: all filters there (64 rows of 50304 18.9 us with a k of 50 and 38.2 with 480; 40.0 and 41.6
-    // otherwise).  Otherwise the places where top-k ends, where top-p or min-p does, whichever comes first, and of the draw, one after the other
+    // kStageAll: the few tokens that top-k leaves, and some more, are in the list: all filters there (64 rows of 50304, here / the other way: a k of 50 19.0 / 36.5 us, 400 35.5 / 37.0,
+    // 480 38.8 / 37.0).  Otherwise the places where top-k ends, where top-p or min-p does, whichever comes first, and of the draw, one after the other
     enum { kStageAll, kStageK, kStageCut, kStageDraw };
     const int behind_k = by_p || by_m ? kStageCut : kStageDraw;
-    int stage = small || (by_k && n_k <= kList) ? kStageAll : by_k ? kStageK : behind_k;
-    enum { kNone, kCounts, kMasses };
+    int stage = small || (by_k && n_k <= kList * 7 / 8) ? kStageAll : by_k ? kStageK : behind_k;
+    enum { kNone, kCounts, kMasses, kBoth };
     int built = kNone;                                     // what the histogram holds: running numbers or sums of the bins before
     bool dirty = false, known = LEVEL, cut = false;        // the histogram is to be cleared; `most` is known; top-p or min-p has cut
     unsigned kept = 0, all_count = 0;
@@ -268,7 +274,7 @@ __device__ __forceinline__ bool sample_row(SampleShared<Row::kThreads> &s, const
     int turn = 0;
     auto clear = [&]() {
         __syncthreads();
-        for (int b = tid; b < kBins; b += T) s.mass[b] = 0ull;
+        for (int b = tid; b < kBins; b += T) { s.count[b] = 0u; s.mass[b] = 0ull; }
         __syncthreads();
     };
     auto drawn = [&](u64 sum) {
@@ -282,7 +288,10 @@ __device__ __forceinline__ bool sample_row(SampleShared<Row::kThreads> &s, const
     }
     for (;;) {
         const bool counts = stage <= kStageK;
-        if (built != (counts ? kCounts : kMasses) && !(small && known)) {
+        if ((counts ? built != kCounts && built != kBoth : built != kMasses) && !(small && known)) {
+            // Where top-k ends among many the sums are laid along with the numbers, so that no second pass has to lay those of the tokens it keeps: all bins behind the one where it ends
+            // have the same sum then, that of what is kept (a k of 600: 64 rows of 50304 41.8 -> 37.0 us, 512 rows 88.4 -> 76.5).
+            const bool both = stage == kStageK;
             if (dirty) clear();
             dirty = true;
             float seen = -INFINITY;
@@ -306,10 +315,9 @@ __device__ __forceinline__ bool sample_row(SampleShared<Row::kThreads> &s, const
                     if (counts) {                          // (uniform)
 #pragma unroll
                         for (int c = 0; c < 4; ++c)
-                            if (v[c] > -INFINITY) atomicAdd(&s.count(bin_of(v[c])), 1u);
-                        return;
-                    }
-                    if (by_k) {                            // (uniform)
+                            if (v[c] > -INFINITY) atomicAdd(&s.count[bin_of(v[c])], 1u);
+                        if (!both) return;
+                    } else if (by_k) {                     // (uniform)
 #pragma unroll
                         for (int c = 0; c < 4; ++c) v[c] = sample_place(sample_key(v[c]), i + c) > k_place ? -INFINITY : v[c];
                     }
@@ -321,7 +329,7 @@ __device__ __forceinline__ bool sample_row(SampleShared<Row::kThreads> &s, const
                         const float y = depth_of(v[c]);
                         const int b = (int)y;
                         const u64 w = weight_in(v[c], b);
-                        if (y >= 0.f && y < (float)kBins) atomicAdd(&s.mass[b], w);
+                        if (in_bins(y)) atomicAdd(&s.mass[b], w);
                         if (c & 1) __builtin_amdgcn_sched_barrier(0);          // (four side by side take more registers than there are)
                     }
                 });
@@ -351,26 +359,28 @@ __device__ __forceinline__ bool sample_row(SampleShared<Row::kThreads> &s, const
             }
             __syncthreads();
             if (!small) {
-                unsigned c[EACH], c0 = 0;
-                u64 m[EACH], m0 = 0;
+                const bool masses = !counts || both;
+                unsigned c[EACH], c0 = 0, c1;
+                u64 m[EACH], m0 = 0, m1;
 #pragma unroll
-                for (int b = 0; b < EACH; ++b) {
-                    c[b] = c0;
-                    m[b] = m0;
-                    if (counts) c0 += s.count(EACH * tid + b);
-                    else if (const u64 in = s.mass[EACH * tid + b]) m0 += scaled(EACH * tid + b, in);       // (most of the bins have nothing)
+                for (int k = 0; k < EACH; ++k) {
+                    const int b = EACH * tid + k;
+                    c[k] = c0;
+                    m[k] = m0;
+                    if (counts) c0 += s.count[b];
+                    if (!masses) continue;
+                    if (const u64 in = s.mass[b]) m0 += scaled(b, in);         // (most of the bins have nothing)
                 }
-                unsigned c1;
-                u64 m1;
                 block_scan(s, turn ^= 1, c0, m0, c1, m1, all_count, all_mass);
 #pragma unroll
-                for (int b = 0; b < EACH; ++b) {
-                    if (counts) s.count(EACH * tid + b) = c1 + c[b];
-                    else s.mass[EACH * tid + b] = m1 + m[b];
+                for (int k = 0; k < EACH; ++k) {
+                    if (counts) s.count[EACH * tid + k] = c1 + c[k];
+                    if (masses) s.mass[EACH * tid + k] = m1 + m[k];
                 }
-                if (!counts && !cut) {
-                    mass = uniform(all_mass);
-                    kept = (unsigned)n_k;
+                if (masses) all_mass = uniform(all_mass);
+                if (masses && !cut) {
+                    mass = all_mass;
+                    kept = both ? min((unsigned)n_k, all_count) : (unsigned)n_k;
                     if (number) {
                         unsigned none;
                         u64 none_of, no_sum;
@@ -378,11 +388,15 @@ __device__ __forceinline__ bool sample_row(SampleShared<Row::kThreads> &s, const
                     }
                 }
                 __syncthreads();
-                built = counts ? kCounts : kMasses;
+                built = both ? kBoth : counts ? kCounts : kMasses;
                 if (counts && all_count <= (unsigned)n_k) {                    // (uniform) top-k keeps all that there is
                     n_k = (int)all_count;
                     by_k = false;
-                    if (all_count > (unsigned)kList) { stage = behind_k; continue; }
+                    if (all_count > (unsigned)kList) {
+                        stage = behind_k;
+                        if (both) built = kMasses;
+                        continue;
+                    }
                     stage = kStageAll;
                 }
             }
@@ -398,7 +412,7 @@ __device__ __forceinline__ bool sample_row(SampleShared<Row::kThreads> &s, const
 #pragma unroll
             for (int k = 0; k < EACH; ++k) {
                 const int b = EACH * tid + k;
-                const u64 from = counts ? s.count(b) : s.mass[b], to = b + 1 < kBins ? (counts ? s.count(b + 1) : s.mass[b + 1]) : counts ? all_count : all_mass;
+                const u64 from = counts ? s.count[b] : s.mass[b], to = counts ? (b + 1 < kBins ? s.count[b + 1] : all_count) : b + 1 < kBins ? min(s.mass[b + 1], all_mass) : all_mass;
                 if (from < target && target <= to) {
                     s.bin = b; s.other = (int)min(to, (u64)kBins); s.before_count = (unsigned)from; s.before_mass = from;
                 }
@@ -449,6 +463,7 @@ __device__ __forceinline__ bool sample_row(SampleShared<Row::kThreads> &s, const
                 mass_m = m_lo < kBins ? s.mass[m_lo] : all_mass;
                 if (m_lo < kBins && in[0]) mass_m = s.mass[m_lo] + scaled(m_lo, in[0]);
                 if (m_hi < kBins && m_hi > m_lo && in[1]) mass_m = s.mass[m_hi] + scaled(m_hi, in[1]);
+                mass_m = min(mass_m, all_mass);            // (what top-k keeps)
             }
         }
         if (by_list) {
@@ -457,11 +472,16 @@ __device__ __forceinline__ bool sample_row(SampleShared<Row::kThreads> &s, const
             unsigned k_lo = 0, k_hi = 0;
             // (where numbers are asked for the first and last bins have all that lies outside of them)
             const float from = all || (counts && bin == 0) ? -INFINITY : (float)bin, to = counts && bin >= kBins - 1 ? NAN : (float)(bin + 1);
-            auto near = [&](float v) {
+            // what is near lies between two logits, which two comparisons tell for nearly all others: the bounds are a hundredth of a bin further than fp32 puts anything
+            auto logit_at = [&](double depth) { return uniform((float)((double)ref - (depth - (double)kAbove) / slope)); };
+            const float v_lo = to == to ? logit_at((double)to + 0.01) : -INFINITY, v_hi = from > -INFINITY ? logit_at((double)from - 0.01) : INFINITY;
+            auto near = [&](float v) { return v >= v_lo && v <= v_hi; };
+            auto is_near = [&](float v) {
                 const float y = depth_of(v);
                 return y >= from && !(y >= to);
             };
             auto inside = [&](float v, int i) {
+                if (!is_near(v)) return false;
                 if (depth > 0) {
                     const unsigned key = sample_key(v);
                     if (key < k_lo || key > k_hi || (depth == 2 && (i < i_lo || i > i_hi))) return false;
@@ -477,7 +497,10 @@ __device__ __forceinline__ bool sample_row(SampleShared<Row::kThreads> &s, const
                 };
                 if (stage == kStageCut && round == 0) {    // (what stands before a token that is kept is kept)
                     unsigned below = 0;
-                    some([&](float v) { below += depth_of(v) < from; return near(v); }, collect);
+                    some([&](float v) { below += v > v_hi; return near(v); }, [&](float v, int i) {
+                        below += depth_of(v) < from;
+                        collect(v, i);
+                    });
                     below = wave_scan(below);
                     if ((tid & 63) == 63 && below) atomicAdd(&s.below, below);
                 } else {
@@ -507,20 +530,20 @@ __device__ __forceinline__ bool sample_row(SampleShared<Row::kThreads> &s, const
                 some(near, [&](float v, int i) {
                     if (!inside(v, i)) return;
                     const unsigned b = (depth == 1 ? k_hi - sample_key(v) : (unsigned)(i - i_lo)) >> shift_by;
-                    atomicAdd(&s.count((int)b), 1u);
+                    atomicAdd(&s.count[b], 1u);
                     if (!counts) atomicAdd(&s.mass[b], weight_in(v, bin));
                 });
                 __syncthreads();
                 unsigned c = 0, none;
                 u64 m = 0, none_of;
 #pragma unroll
-                for (int k = 0; k < EACH_CUT; ++k) { c += s.count(EACH_CUT * tid + k); m += s.mass[EACH_CUT * tid + k]; }
+                for (int k = 0; k < EACH_CUT; ++k) { c += s.count[EACH_CUT * tid + k]; m += s.mass[EACH_CUT * tid + k]; }
                 block_scan(s, turn ^= 1, c, m, c, m, none, none_of);
                 c += before_count;
                 m += before_in;
 #pragma unroll
                 for (int k = 0; k < EACH_CUT; ++k) {
-                    const unsigned cb = s.count(EACH_CUT * tid + k);
+                    const unsigned cb = s.count[EACH_CUT * tid + k];
                     const u64 mb = s.mass[EACH_CUT * tid + k];
                     if (counts ? c < target && target <= c + cb : before_mass + scaled(bin, m) < target && target <= before_mass + scaled(bin, m + mb)) {
                         s.other = EACH_CUT * tid + k; s.before_count = c; s.value = m;
@@ -542,11 +565,12 @@ __device__ __forceinline__ bool sample_row(SampleShared<Row::kThreads> &s, const
             }
             // every token counts those before it; where there are threads enough, several for a token
             const int n = uniform(min(s.n_list, kList));
-            if (tid < n && !(counts && !all)) {
+            if (tid < n) {
                 const float v = sample_of_place(s.place[tid]);
                 const int b = bin_of(v);
                 u64 w = weight_in(v, b);
-                if (all) w = depth_of(v) < (float)kBins ? scaled(b, w) : 0ull;
+                if (counts && !(depth_of(v) < (float)kBins)) w = 0ull;         // (the last bin has all that lies behind it)
+                if (all) w = scaled(b, w);
                 s.weight[tid] = w;
             }
             __syncthreads();
@@ -604,12 +628,18 @@ __device__ __forceinline__ bool sample_row(SampleShared<Row::kThreads> &s, const
                 return true;
             }
             if (token && (counts ? rank + 1u == target : sum < target && target <= with)) {
+                if (built == kBoth) with = s.mass[bin] + scaled(bin, with);
                 s.found_place = place; s.value = with; s.found_weight = with - sum; s.kept = rank + 1u;
             }
             __syncthreads();
         }
         if (stage == kStageK) {
             k_place = uniform(s.found_place);
+            if (built == kBoth) {                          // (otherwise laid anew)
+                mass = all_mass = uniform(s.value);
+                kept = (unsigned)n_k;
+                built = kMasses;
+            }
             stage = behind_k;
         } else if (stage == kStageCut) {
             kept = kept_m;
@@ -651,7 +681,7 @@ __global__ void __launch_bounds__(T, 4) k_sample(SampleParams P)
         if (P.probs) P.probs[row] = prob;
         if (P.kept) P.kept[row] = shown >= 0 ? shown : kept;
     };
-    for (int b = tid; b < kBins; b += T) s.mass[b] = 0ull;
+    for (int b = tid; b < kBins; b += T) { s.count[b] = 0u; s.mass[b] = 0ull; }
     if (!(how.tau > 0.f) || how.top_k == 1 || how.top_p <= 0.f) {              // (uniform) the first of the order
         float most = -INFINITY;
         int first = 0x7fffffff;
@@ -685,7 +715,7 @@ __global__ void __launch_bounds__(T, 4) k_sample(SampleParams P)
         shown = how.top_k > 0 ? min(how.top_k, (int)valid) : (int)valid;
     }
     __syncthreads();
-    for (int b = tid; b < kBins; b += T) s.mass[b] = 0ull;
+    for (int b = tid; b < kBins; b += T) { s.count[b] = 0u; s.mass[b] = 0ull; }
     __syncthreads();
     sample_row<true>(s, R, how, most, answer);
 }

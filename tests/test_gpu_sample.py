@@ -184,6 +184,22 @@ def test_min_p_with_the_others(min_p):
         check(x, uniform=u, min_p=min_p, **how)
 
 
+@pytest.mark.parametrize("left", [100, 511, 600, 5000])
+def test_top_k_of_about_as_many_as_there_are(left):
+    """k below, at and above the number of logits that are numbers; ties where it ends"""
+    rng = np.random.default_rng(left)
+    n, vocab = 16, 9000
+    x = np.full((n, vocab), -np.inf, dtype=np.float32)
+    for r in range(n):
+        at = rng.permutation(vocab)[:left]
+        x[r, at] = np.round(3.0 * rng.standard_normal(left), 1 if r % 2 else 4)
+        x[r, rng.permutation(vocab)[:50]] = np.nan
+    u = rng.random(n, dtype=np.float32)
+    for k in (left - 80, left - 51, left, left + 1, 448, 449, 512, 513):
+        for how in (dict(), dict(top_p=0.8), dict(min_p=0.01), dict(top_p=0.999, min_p=1e-4)):
+            check(x, uniform=u, top_k=k, **how)
+
+
 def test_random_numbers_out_of_range():
     rng = np.random.default_rng(8)
     x = model_logits(rng, 6, 700)
