@@ -39,6 +39,14 @@ constexpr float kAbove = 2048.f;
 // 1024 threads, 78.7 and 70.7.)
 constexpr int kSampleOneEach = 256;
 
+// 2^(63 - k / 32), to the nearest
+__constant__ const u64 kOctave[kBinsToOctave] = {
+    0x8000000000000000ull, 0x7d41d96db915019dull, 0x7a92be8a92436616ull, 0x77f25ccdee6d7ae6ull, 0x75606373ee921c97ull, 0x72dc8373be41a454ull, 0x70666f76154a7089ull,
+    0x6dfddbcbed791babull, 0x6ba27e656b4eb57aull, 0x69540ec8f895722dull, 0x6712460a8fc24072ull, 0x64dcdec3371793d1ull, 0x62b39508aa836d6full, 0x6096266533384a2bull,
+    0x5e8451cfac061b5full, 0x5c7dd7a3b17dcf75ull, 0x5a827999fcef3242ull, 0x5891fac0e95612c8ull, 0x56ac1f752150a563ull, 0x54d0ad5a753e077cull, 0x52ff6b54d8a89c75ull,
+    0x513821818624b40cull, 0x4f7a993048d088d7ull, 0x4dc69cdceaa72a9cull, 0x4c1bf828c6dc54b8ull, 0x4a7a77d47f7b84b1ull, 0x48e1e9b9d588e19bull, 0x47521cc5a2e6a9e0ull,
+    0x45cae0f1f545eb73ull, 0x444c0740496d4294ull, 0x42d561b3e6243d8aull, 0x4166c34c5615d0ecull};
+
 // larger logits have larger keys (no NaN)
 __device__ __forceinline__ unsigned sample_key(float v)
 {
@@ -100,6 +108,7 @@ struct SampleShared {
     int n_list, bin, other;
     unsigned below, before_count, lo, hi, kept, first;
     u64 before_mass, value, found_place, found_weight;
+    u64 octave[kBinsToOctave];                             // kOctave
 };
 
 // Sums of a value over the workgroup: those of the threads before this one, and of all.  `turn` alternates, so that a second call need not wait for the first one's readers.
@@ -233,8 +242,8 @@ __device__ __forceinline__ bool sample_row(SampleShared<Row::kThreads> &s, const
     };
     int top_bin = 0;                                       // the largest logit's
     auto scaled = [&](int bin, u64 sum) {                  // sum 2^((top_bin - bin) / 32), cut off
-        const u64 by = (u64)ldexp(exp2((double)(top_bin - bin) * (1.0 / kBinsToOctave)), 63);
-        return __umul64hi(sum << 1, by);
+        const int below = bin - top_bin;                   // (of a bin that has something, not less than zero)
+        return __umul64hi(sum << 1, s.octave[below & (kBinsToOctave - 1)]) >> min((unsigned)below / kBinsToOctave, 63u);
     };
     auto fit = [&](f32x4 v) {
         if constexpr (LEVEL)
@@ -682,6 +691,7 @@ __global__ void __launch_bounds__(T, 4) k_sample(SampleParams P)
         if (P.kept) P.kept[row] = shown >= 0 ? shown : kept;
     };
     for (int b = tid; b < kBins; b += T) { s.count[b] = 0u; s.mass[b] = 0ull; }
+    if (tid < kBinsToOctave) s.octave[tid] = kOctave[tid];
     if (!(how.tau > 0.f) || how.top_k == 1 || how.top_p <= 0.f) {              // (uniform) the first of the order
         float most = -INFINITY;
         int first = 0x7fffffff;
