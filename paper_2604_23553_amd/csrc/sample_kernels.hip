@@ -16,9 +16,9 @@
 // whichever wavefront comes first, and a border between two tokens is where 64-bit arithmetic has it but for 2^-40 of the sum.  With weights in fp32 it would
 // be up to 2^-24 off, which is another token once in some hundred thousand rows.
 //
-// Bound by one CU's instructions - the vector units are busy two thirds of a lone row's time - and by the way of a pass's first logits, not by memory: of a row's 27 us the
-// pass that lays sums takes 11, the sums over the bins 2, each pass that collects 4.  50304 logits in fp32: one row, top-p 27.0 us; 64 rows, top-k of 50, top-p and min-p
-// 19.4 us; 512 rows of different settings 63 us, 1.6 TB/s.  A row's logits do not fit its registers, and a row on more than one CU would need a workspace of the caller's.
+// Bound by one CU's instructions - the vector units are busy two thirds of a lone row's time - and by the way of a pass's first logits, not by memory: of a row's 26 us the
+// pass that lays sums takes 11, the sums over the bins 1, each pass that collects 4.  50304 logits in fp32: one row, top-p 25.2 us; 64 rows, top-k of 50, top-p and min-p
+// 18.3 us; 512 rows of different settings 61 us, 1.7 TB/s.  A row's logits do not fit its registers, and a row on more than one CU would need a workspace of the caller's.
 #include <hip/hip_runtime.h>
 #include <hip/hip_fp16.h>
 #include "sample_params.h"
@@ -35,8 +35,8 @@ typedef unsigned long long u64;
 constexpr int kBins = 4096, kCut = 2048, kList = 512, kBinsToOctave = 32;     // kCut: bins of a bin's own histogram
 // Bins above the reference; as many below it.  (512 of 2048: 0.4 us less, but where the histogram of one of 64 rows is laid again 59.3 us for 35.0.)
 constexpr float kAbove = 2048.f;
-// Rows up to which a row has a CU's 1024 threads; more, and two rows share it.  (One row 27.5 us, with 512 threads 30.4; 64 rows 19.0 and 21.9; 512 rows, each with
-// 1024 threads, 78.7 and 70.7.)
+// Rows up to which a row has a CU's 1024 threads; more, and two rows share it.  (No filter: one row 25.6 us, with 512 threads 29.9; 64 rows 27.7 and 33.4; 512 rows, each
+// with 1024 threads, 65.7, with 512 51.3.)
 constexpr int kSampleOneEach = 256;
 
 // 2^(63 - k / 32), to the nearest
@@ -147,7 +147,7 @@ __device__ __forceinline__ float max4(f32x4 v, float m) { return fmaxf(fmaxf(m, 
 // A row's logits, four to a thread that follow one another; what lies behind the row as minus infinity, a NaN stays one.  FEW: of less than four
 template <int T, bool F16, bool FEW>
 struct SampleRow {
-    static constexpr int kThreads = T, STEP = 4 * T, AT = FEW ? 1 : 2;         // two vectors are on their way while two others are looked at (four as fast, and registers spilled; one 20.7 us for 18.9 with 64 rows)
+    static constexpr int kThreads = T, STEP = 4 * T;
     const void *at;
     int vocab;
     // (the last ones of the row in place of those behind it; rows may begin at any logit)
@@ -164,42 +164,34 @@ struct SampleRow {
             return f32x4{(float)x[0], (float)x[1], (float)x[2], (float)x[3]};
         }
     }
-    // first(the first vectors, which may hold logits twice or stand for ones behind the row), then f(four logits, index of the first) for all; all threads of the workgroup together
+    // first(the first vector, which may hold logits twice or stand for ones behind the row), then f(four logits, index of the first) for all; all threads of the workgroup
+    // together.  One vector is on its way while another is looked at: two or four of each are no faster (one row 25.6 and 25.7 us for 24.8, 64 rows with a top-k of 50 18.5 and
+    // 18.4 for 17.8; 512 rows 51.3 and 58.2 for 53.0, with a top-k of 50 39.6 and 42.7 for 36.7)
     template <class First, class Fn>
     __device__ __forceinline__ void each(First first, Fn f) const
     {
         int own = 4 * (int)threadIdx.x;
         asm volatile("" : "+v"(own));                      // (so that no pass keeps its addresses in registers for the next one)
-        f32x4 next[AT];
-#pragma unroll
-        for (int j = 0; j < AT; ++j) next[j] = raw(own + j * STEP);
+        f32x4 next = raw(own);
         first(next);
 #pragma unroll 1
-        for (int base = 0; base < vocab; base += AT * STEP) {
-            f32x4 x[AT];
+        for (int at = 0; at < vocab; at += STEP) {
+            const int i = at + own;
+            f32x4 v = next;
+            next = raw(i + STEP);                          // (past the end: the last ones again)
+            if (at + STEP > vocab) {                       // (uniform) the row's end: what was loaded is `off` logits too early
+                const int off = FEW ? 0 : max(i - (vocab - 4), 0);
+                const f32x4 y = v;
 #pragma unroll
-            for (int j = 0; j < AT; ++j) x[j] = next[j];
+                for (int c = 0; c < 4; ++c) {
+                    float z = y[c];
 #pragma unroll
-            for (int j = 0; j < AT; ++j) next[j] = raw(own + base + (AT + j) * STEP);          // (past the end: the last ones again)
-#pragma unroll
-            for (int j = 0; j < AT; ++j) {
-                const int at = base + j * STEP, i = at + own;
-                if (at >= vocab) break;                    // (uniform)
-                f32x4 v = x[j];
-                if (at + STEP > vocab) {                   // (uniform) the row's end: what was loaded is `off` logits too early
-                    const int off = FEW ? 0 : max(i - (vocab - 4), 0);
-                    const f32x4 y = v;
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        float z = y[c];
-#pragma unroll
-                        for (int k = c + 1; k < 4; ++k) z = off == k - c ? y[k] : z;
-                        v[c] = i + c < vocab ? z : -INFINITY;
-                    }
+                    for (int k = c + 1; k < 4; ++k) z = off == k - c ? y[k] : z;
+                    v[c] = i + c < vocab ? z : -INFINITY;
                 }
-                f(v, i);
-                __builtin_amdgcn_sched_barrier(0);
             }
+            f(v, i);
+            __builtin_amdgcn_sched_barrier(0);
         }
     }
     template <class Fn>
@@ -269,11 +261,11 @@ __device__ __forceinline__ bool sample_row(SampleShared<Row::kThreads> &s, const
     int n_k = by_k ? how.top_k : R.vocab;                  // (at most so many: minus infinities are found later)
     u64 k_place = ~0ull;                                   // of the last token that top-k keeps
 
-    // kStageAll: the few tokens that top-k leaves, and some more, are in the list: all filters there (64 rows of 50304, here / the other way: a k of 50 19.0 / 36.5 us, 400 35.5 / 37.0,
-    // 480 38.8 / 37.0).  Otherwise the places where top-k ends, where top-p or min-p does, whichever comes first, and of the draw, one after the other
+    // kStageAll: the few tokens that top-k leaves, and some more, are in the list: all filters there (64 rows of 50304, here / the other way: a k of 50 18.4 / 34.9 us, 320 32.0 / 35.4,
+    // 400 35.0 / 35.3, 480 38.1 / 35.4).  Otherwise the places where top-k ends, where top-p or min-p does, whichever comes first, and of the draw, one after the other
     enum { kStageAll, kStageK, kStageCut, kStageDraw };
     const int behind_k = by_p || by_m ? kStageCut : kStageDraw;
-    int stage = small || (by_k && n_k <= kList * 7 / 8) ? kStageAll : by_k ? kStageK : behind_k;
+    int stage = small || (by_k && n_k <= kList * 3 / 4) ? kStageAll : by_k ? kStageK : behind_k;
     enum { kNone, kCounts, kMasses, kBoth };
     int built = kNone;                                     // what the histogram holds: running numbers or sums of the bins before
     bool dirty = false, known = LEVEL, cut = false;        // the histogram is to be cleared; `most` is known; top-p or min-p has cut
@@ -310,11 +302,7 @@ __device__ __forceinline__ bool sample_row(SampleShared<Row::kThreads> &s, const
             auto lay = [&](auto first) {
                 R.each([&](auto &x) {
                     if constexpr (decltype(first)::value) {
-                        float m = -INFINITY;
-#pragma unroll
-                        for (int j = 0; j < Row::AT; ++j)
-                            if (j * Row::STEP + 4 * tid < R.vocab) m = max4(x[j], m);
-                        m = block_max(s, 0, m);
+                        const float m = block_max(s, 0, 4 * tid < R.vocab ? max4(x, -INFINITY) : -INFINITY);
                         refer(fabsf(m) < INFINITY ? m : 0.f);
                     }
                 }, [&](f32x4 x, int i) {
