@@ -107,7 +107,7 @@ struct SampleShared {
     float wave_max[2][kWaves];
     int n_list, bin, other;
     unsigned below, before_count, lo, hi, kept, first;
-    u64 before_mass, value, found_place, found_weight;
+    u64 before_mass, value, found_place, sum_of_kept;
     u64 octave[kBinsToOctave];                             // kOctave
 };
 
@@ -236,6 +236,12 @@ __device__ __forceinline__ bool sample_row(SampleShared<Row::kThreads> &s, const
     auto scaled = [&](int bin, u64 sum) {                  // sum 2^((top_bin - bin) / 32), cut off
         const int below = bin - top_bin;                   // (of a bin that has something, not less than zero)
         return __umul64hi(sum << 1, s.octave[below & (kBinsToOctave - 1)]) >> min((unsigned)below / kBinsToOctave, 63u);
+    };
+    // a token's weight over a sum (its own, not the difference of two sums that are cut off)
+    auto part_of = [&](u64 place, u64 of) {
+        const float v = sample_of_place(place);
+        const int bin = bin_of(v), below = bin - top_bin;
+        return (float)(ldexp((double)weight_in(v, bin) * (double)s.octave[below & (kBinsToOctave - 1)], -63 - below / kBinsToOctave) / (double)of);
     };
     auto fit = [&](f32x4 v) {
         if constexpr (LEVEL)
@@ -618,15 +624,15 @@ __device__ __forceinline__ bool sample_row(SampleShared<Row::kThreads> &s, const
                 if ((tid & 63) == 0 && of_wave) atomicAdd(&s.kept, (unsigned)__popcll(of_wave));
                 __syncthreads();
                 const unsigned n_kept = s.kept;            // (the first of the order)
-                if (token && rank == n_kept - 1u) s.found_weight = with;
+                if (token && rank == n_kept - 1u) s.sum_of_kept = with;
                 __syncthreads();
-                const u64 in_all = s.found_weight, at = drawn(in_all);
-                if (ok && sum < at && at <= with) answer((int)(unsigned)place, (float)((double)(with - sum) / (double)in_all), (int)n_kept);
+                const u64 in_all = s.sum_of_kept, at = drawn(in_all);
+                if (ok && sum < at && at <= with) answer((int)(unsigned)place, part_of(place, in_all), (int)n_kept);
                 return true;
             }
             if (token && (counts ? rank + 1u == target : sum < target && target <= with)) {
                 if (built == kBoth) with = s.mass[bin] + scaled(bin, with);
-                s.found_place = place; s.value = with; s.found_weight = with - sum; s.kept = rank + 1u;
+                s.found_place = place; s.value = with; s.kept = rank + 1u;
             }
             __syncthreads();
         }
@@ -648,7 +654,7 @@ __device__ __forceinline__ bool sample_row(SampleShared<Row::kThreads> &s, const
             cut = true;
             stage = kStageDraw;
         } else {
-            if (tid == 0) answer((int)(unsigned)s.found_place, (float)((double)s.found_weight / (double)mass), (int)kept);
+            if (tid == 0) answer((int)(unsigned)s.found_place, part_of(s.found_place, mass), (int)kept);
             return true;
         }
         __syncthreads();                                   // (what was found has been read)

@@ -200,6 +200,24 @@ def test_top_k_of_about_as_many_as_there_are(left):
             check(x, uniform=u, top_k=k, **how)
 
 
+@pytest.mark.parametrize("how", [dict(), dict(top_k=300), dict(top_k=4000), dict(top_p=1 - 2.0 ** -24)])
+def test_probabilities_of_rare_tokens(how):
+    """Drawn by random numbers next to 1 behind a few tokens that have nearly all of the weight: they are as precise as those of the likely ones"""
+    rng = np.random.default_rng(61)
+    n, vocab = 30, 19253
+    x = (2.0 * rng.standard_normal((n, vocab))).astype(np.float32)
+    x[:, 5000] = np.linspace(10, 25, n)
+    got = check(x, uniform=1 - 2.0 ** -24, **how)
+    for r, (token, prob, kept) in enumerate(got):
+        p = page8_ref.sample(x[r], **how)
+        at = int(np.nonzero(p["order"] == token)[0][0])
+        # the weight 2^-41 off, the sum 2^-39, the quotient rounded to fp32
+        want = p["w"][at] / p["sums"][kept - 1]
+        assert abs(prob - want) <= want * (2.0 ** -24 + 2.0 ** -38), (r, prob, want)
+    # (that the inputs are what the test is about: the 300th of so many is near 2 * 2.16, and exp(4.3 - 25) is 2^-29.9)
+    assert min(g[1] for g in got) < 2.0 ** -29
+
+
 def test_random_numbers_out_of_range():
     rng = np.random.default_rng(8)
     x = model_logits(rng, 6, 700)
