@@ -332,7 +332,7 @@ def test_generation_with_sampling():
                 token, logits = int(ds.tokens[S + step + 1].item()), ds.logits.cpu().numpy().copy()
                 r = page8_ref.sample(logits, temperature=0.8, top_k=200, top_p=0.9, min_p=0.001, uniform=u[S + step])
                 at = int(np.nonzero(r["order"] == token)[0][0])
-                before, off = r["sums"][at - 1] if at else 0.0, 2 * (r["sums"][-1] * 2.0 ** -40 + VOCAB * 2.0 ** -46)
+                before, off = r["sums"][at - 1] if at else 0.0, page8_ref.sample_off(r)
                 assert at < r["kept"] and before <= r["target"] + off and r["sums"][at] >= r["target"] - off
                 out.append((token, logits))
             ds.check()
@@ -388,7 +388,7 @@ def test_a_token_behind_both_kernels_of_the_head(heads, d, vocab, threads):
             logits = ds.logits.cpu().numpy()
             r = page8_ref.sample(logits, temperature=0.5, uniform=float(u[1]))
             at = int(np.nonzero(r["order"] == int(ds.tokens[2].item()))[0][0])
-            off = 2 * (r["sums"][-1] * 2.0 ** -40 + vocab * 2.0 ** -46)
+            off = page8_ref.sample_off(r)
             assert (r["sums"][at - 1] if at else 0.0) <= r["target"] + off and r["sums"][at] >= r["target"] - off
             assert int(ds.pos[0].item()) == 2
         ds.set_tokens([0, 0], 1)
