@@ -323,17 +323,13 @@ __global__ void __launch_bounds__(kTaThreads, 2) k_page8_attention(TreeAttention
             hi[j >> 2][j & 3] = __builtin_bit_cast(unsigned, a);
             lo[j >> 2][j & 3] = __builtin_bit_cast(unsigned, b);
         }
-        unsigned keep[4] = {~0u, ~0u, ~0u, ~0u};
-        if (!INT8 && masked) {                             // (bytes past the last position may be none of e4m3's numbers)
-            const int left = it.t1 - (base + 16 * kg);
-#pragma unroll
-            for (int w = 0; w < 4; ++w) keep[w] = left >= 4 * w + 4 ? ~0u : left <= 4 * w ? 0u : (1u << 8 * (left - 4 * w)) - 1u;
-        }
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
+            // Bytes 0x7f and 0xff are none of e4m3's numbers and are never written; where nothing was, in positions that no row sees, behind the last or in a page that an
+            // entry outside the pool is read as, they may lie, and a weight of zero times NaN is NaN for all rows.  One bit less and they are finite.
             if (!INT8 && masked)
 #pragma unroll
-                for (int w = 0; w < 4; ++w) r.v[t][w] &= keep[w];
+                for (int w = 0; w < 4; ++w) r.v[t][w] &= ~((((r.v[t][w] & 0x7f7f7f7fu) + 0x01010101u) >> 7) & 0x01010101u);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const ta_f16x8 v = p8_values8<INT8>(r.v[t][2 * h], r.v[t][2 * h + 1]);

@@ -386,3 +386,63 @@ def test_two_batches_on_two_streams():
         b.attention8(two.cuda_stream)
     a.check(a.result())
     b.check(b.result())
+
+
+# ---- what lies in positions that a row does not see ------------------------------------------------------
+def unwritten(s, r, node):
+    """A node's slot holds what a pool begins with"""
+    t = s.lens[r] + node
+    s.pool[0][:, s.table[r, t // s.page], :, :, t % s.page] = np.full(1, NAN16, dtype=np.uint16).view(np.float16)
+
+
+@pytest.mark.parametrize("poison", [0x7F, 0xFF])
+@pytest.mark.parametrize("type", TYPES)
+@pytest.mark.parametrize("sizes,lens,heads,page", [
+    ([4, 1, 6], [0, 33, 100], (2, 2, 64), 16),               # 16 query rows at most
+    ([11, 3, 9], [70, 250, 16], (4, 2, 80), 16),             # 64
+    ([6, 16], [45, 300], (4, 4, 128), 32),
+    ([64, 40], [500, 31], (2, 1, 128), 48),                  # 128, masks of several words
+])
+def test_unseen_positions_that_were_never_written(type, poison, sizes, lens, heads, page):
+    """Nodes that no mask shows need no K and V: codes and scales that are no numbers change nothing for the rows of their tile"""
+    rng = np.random.default_rng(len(sizes) + page)
+    hidden = [rng.random(n) < 0.4 for n in sizes]
+    hidden[0][0] = hidden[-1][-1] = True
+
+    def change(s):
+        for r, h in enumerate(hidden):
+            for node in np.nonzero(h)[0]:
+                unwritten(s, r, int(node))
+    s = Step8(lens, trees_of(rng, sizes), heads, page=page, seed=31, type=type, change=change).to_gpu()
+    s.pool8.bytes[s.pool8.bytes == 0x7F] = poison
+    s.g_pool8.copy_(dev(s.pool8.bytes))
+    s.run_plan()
+    up = [(rng.random((n, n)) < 0.6) & ~h for n, h in zip(sizes, hidden)]
+    words = np.concatenate([tree_ref.mask_words(u, s.words) for u in up] + [np.zeros((s.max_rows - s.rows, s.words), np.int32)])
+    s.g_masks.copy_(dev(words.astype(np.int32)))
+    s.attention8()
+    s.check(s.result(), up=up)
+
+
+@pytest.mark.parametrize("bad", [-1, 10 ** 6])
+@pytest.mark.parametrize("type", TYPES)
+def test_a_bad_entry_that_some_rows_see(type, bad):
+    """The rows that see one of its positions are NaN, the others have their answer, whatever the pool's last page holds"""
+    tree = [-1, 0, 1, 0, 3, 4, 1]                           # nodes 2 .. 6 lie in the second page; 0 and 1 see nothing of it
+    def change(s):
+        last = np.full((1, 2, 1) + s.pool.shape[3:], NAN16, dtype=np.uint16).view(np.float16)
+        s.pool = np.concatenate([s.pool, last], axis=2)
+        s.n_pages += 1
+    s = Step8([14, 62, 30], [tree, tree, tree], (4, 2, 64), seed=32, type=type, change=change).to_gpu()
+    for r in range(2):
+        s.g["table"][r, (s.lens[r] + 2) // s.page] = bad
+    s.run_plan().attention8()
+    got = s.result()
+    s.check(got, requests=[2])
+    for r in range(2):
+        e, off = s.plain(r, s.up[r])
+        g = got[s.starts[r]:s.starts[r] + 7, :256].astype(np.float64).reshape(e.shape)
+        sees = s.up[r][:7, 2:7].any(-1)
+        assert sees.tolist() == [False, False, True, True, True, True, True]
+        assert np.isnan(g[sees]).all()
+        assert (np.abs(g[~sees] - e[~sees]) <= np.abs(e[~sees]) * 2.0 ** -11 + 2.0 ** -25 + off[~sees] * (1 + 2.0 ** -11)).all()
