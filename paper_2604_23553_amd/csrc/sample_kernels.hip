@@ -213,14 +213,16 @@ __device__ __forceinline__ bool sample_row(SampleShared<Row::kThreads> &s, const
     // bins to a logit; at least so many that infinite differences stay infinite (the largest finite one is no thousandth of a bin then), at most so many that
     // none becomes NaN
     const double slope = uniform(fmin(fmax(LEVEL ? 1.0 : 1.4426950408889634 * kBinsToOctave / (double)how.tau, 1e-42), 1e37));
-    const float slope32 = uniform((float)slope);
-    float ref = 0.f;                                       // its bin is kAbove
+    // Differences of logits are halved: two finite logits may be further apart than the type reaches.  (What the smallest numbers lose is 2^-150 of the slope.)
+    const float slope_of_half = uniform((float)(2.0 * slope));
+    float ref = 0.f, half_ref = 0.f;                       // its bin is kAbove
     double shift = 0.0;
     auto refer = [&](float to) {
         ref = to;
+        half_ref = uniform(0.5f * ref);
         shift = uniform((double)ref * slope + ((double)kAbove - 0.5));
     };
-    auto depth_of = [&](float v) { return fmaf(ref - v, slope32, kAbove); };   // (never rises with v; infinite for minus infinity)
+    auto depth_of = [&](float v) { return fmaf(fmaf(v, -0.5f, half_ref), slope_of_half, kAbove); };            // (never rises with v; infinite for minus infinity)
     auto bin_of = [&](float v) { return (int)__builtin_amdgcn_fmed3f(depth_of(v), 0.f, kBins - 1.f); };          // (no NaN)
     auto in_bins = [](float depth) { return __float_as_uint(depth) < __float_as_uint((float)kBins); };            // (neither less than zero nor NaN)
     // 2^(-f / 32) in multiples of 2^-44, f the token's place in its bin from its middle: -1/2 to 1/2

@@ -218,6 +218,25 @@ def test_probabilities_of_rare_tokens(how):
     assert min(g[1] for g in got) < 2.0 ** -29
 
 
+FILTERS = [dict(), dict(top_k=30), dict(top_k=600), dict(top_p=0.8), dict(min_p=0.03), dict(top_k=600, top_p=0.9, min_p=0.01)]
+
+
+@pytest.mark.parametrize("temperature", [1e37, 1e38, np.finfo(np.float32).max])
+@pytest.mark.parametrize("vocab", [2, 300, 20000])
+def test_logits_further_apart_than_their_largest(vocab, temperature):
+    """Finite logits whose difference is beyond the type's range weigh what the temperature says"""
+    rng = np.random.default_rng(vocab)
+    n, most = 24, np.finfo(np.float32).max
+    x = (np.float64(most) * rng.uniform(-1, 1, (n, vocab))).astype(np.float32)
+    x[:8] = np.where(rng.random((8, vocab)) < 0.5, most, -most)
+    x[8:12, :vocab * 4 // 5] = -most
+    x[12:16, ::2] = -np.inf
+    x[16] = [most, -most] * (vocab // 2)
+    u = rng.random(n, dtype=np.float32)
+    for how in FILTERS:
+        check(x, uniform=u, temperature=np.float32(temperature), **how)
+
+
 def test_random_numbers_out_of_range():
     rng = np.random.default_rng(8)
     x = model_logits(rng, 6, 700)
