@@ -210,11 +210,11 @@ __device__ __forceinline__ bool sample_row(SampleShared<Row::kThreads> &s, const
 {
     constexpr int T = Row::kThreads, EACH = kBins / T, EACH_CUT = kCut / T;
     const int tid = threadIdx.x;
-    // bins to a logit; at least so many that infinite differences stay infinite (the largest finite one is no thousandth of a bin then), at most so many that
-    // none becomes NaN
-    const double slope = uniform(fmin(fmax(LEVEL ? 1.0 : 1.4426950408889634 * kBinsToOctave / (double)how.tau, 1e-42), 1e37));
+    // bins to a logit; for fp32 at least so many that infinite differences stay infinite (the largest finite one is no thousandth of a bin then), at most so many that
+    // none becomes NaN.  None at an infinite temperature: all logits weigh the same.
+    const double bounded = uniform(fmin(fmax(LEVEL ? 1.0 : 1.4426950408889634 * kBinsToOctave / (double)how.tau, 1e-42), 1e37)), slope = LEVEL || how.tau < INFINITY ? bounded : 0.0;
     // Differences of logits are halved: two finite logits may be further apart than the type reaches.  (What the smallest numbers lose is 2^-150 of the slope.)
-    const float slope_of_half = uniform((float)(2.0 * slope));
+    const float slope_of_half = uniform((float)(2.0 * bounded));
     float ref = 0.f, half_ref = 0.f;                       // its bin is kAbove
     double shift = 0.0;
     auto refer = [&](float to) {

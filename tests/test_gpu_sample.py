@@ -237,6 +237,20 @@ def test_logits_further_apart_than_their_largest(vocab, temperature):
         check(x, uniform=u, temperature=np.float32(temperature), **how)
 
 
+@pytest.mark.parametrize("vocab", [2, 300, 20000])
+def test_an_infinite_temperature(vocab):
+    """All finite logits weigh one, however far apart they are; min-p of 1 keeps them all"""
+    rng = np.random.default_rng(vocab)
+    n, most = 24, np.finfo(np.float32).max
+    x = (np.float64(most) * rng.uniform(-1, 1, (n, vocab))).astype(np.float32)
+    x[:8] = rng.standard_normal((8, vocab)).astype(np.float32)
+    x[8:12, :vocab * 4 // 5] = -most
+    x[12:16, 1::2] = -np.inf
+    u = rng.random(n, dtype=np.float32)
+    for how in FILTERS + [dict(min_p=1.0), dict(top_k=600, min_p=1.0)]:
+        check(x, uniform=u, temperature=np.float32(np.inf), **how)
+
+
 def test_random_numbers_out_of_range():
     rng = np.random.default_rng(8)
     x = model_logits(rng, 6, 700)
