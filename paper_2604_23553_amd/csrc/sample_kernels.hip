@@ -201,18 +201,29 @@ struct SampleRow {
     }
 };
 
-struct SampleHow { float tau, top_p, min_p, uniform; int top_k; };
+struct SampleHow {
+    float tau, top_p, min_p, uniform;
+    int top_k;
+    __device__ __forceinline__ double slope() const { return 1.4426950408889634 * kBinsToOctave / (double)tau; }       // bins to a logit
+};
 
-// The token of a row.  LEVEL: the tokens that equal `most` weigh one and all others nothing; otherwise `most` is found here.  false: the weights are like
-// that, `most` is set and nothing is answered.  s.mass and s.count are zero.
-template <bool LEVEL, class Row, class Answer>
-__device__ __forceinline__ bool sample_row(SampleShared<Row::kThreads> &s, const Row &R, const SampleHow &how, float &most, Answer answer)
+// Whether only the tokens that equal the largest weigh anything: it is infinite, or one step of the largest number is more bins than there are
+__device__ __forceinline__ bool sample_level(const SampleHow &how, float most) { return most == INFINITY || (double)fabsf(most) * how.slope() > 0x1p40; }
+
+// Below this temperature, where a bin is less than 2^-100 of a logit, a row is taken kUnsteep times as large, logits and temperature: 32 bits do not reach the slope.
+// Tokens that weigh anything are so close to a largest one so small that this is exact; others may become minus infinity.
+constexpr float kSteep = 0x1p-95f, kUnsteep = 0x1p64f;
+
+// The token of a row.  !KNOWN: `most`, the largest logit, is found here.  false: only the tokens that equal it weigh anything, or the row is a steep one; nothing
+// is answered then.  KNOWN: the logits are fit_one() of the row's, and `most` is the largest of them.  s.mass and s.count are zero.
+template <bool KNOWN, class Row, class Fit, class Answer>
+__device__ __forceinline__ bool sample_row(SampleShared<Row::kThreads> &s, const Row &R, const SampleHow &how, Fit fit_one, float &most, Answer answer)
 {
     constexpr int T = Row::kThreads, EACH = kBins / T, EACH_CUT = kCut / T;
     const int tid = threadIdx.x;
-    // bins to a logit; for fp32 at least so many that infinite differences stay infinite (the largest finite one is no thousandth of a bin then), at most so many that
-    // none becomes NaN.  None at an infinite temperature: all logits weigh the same.
-    const double bounded = uniform(fmin(fmax(LEVEL ? 1.0 : 1.4426950408889634 * kBinsToOctave / (double)how.tau, 1e-42), 1e37)), slope = LEVEL || how.tau < INFINITY ? bounded : 0.0;
+    // for fp32 at least so many bins that infinite differences stay infinite (the largest finite one is no thousandth of a bin then), at most so many, of a steep row,
+    // that none becomes NaN
+    const double bounded = uniform(fmin(fmax(how.slope(), 1e-42), 1e37)), slope = how.tau < INFINITY ? bounded : 0.0;     // (none: all logits weigh the same)
     // Differences of logits are halved: two finite logits may be further apart than the type reaches.  (What the smallest numbers lose is 2^-150 of the slope.)
     const float slope_of_half = uniform((float)(2.0 * bounded));
     float ref = 0.f, half_ref = 0.f;                       // its bin is kAbove
@@ -246,9 +257,9 @@ __device__ __forceinline__ bool sample_row(SampleShared<Row::kThreads> &s, const
         return (float)(ldexp((double)weight_in(v, bin) * (double)s.octave[below & (kBinsToOctave - 1)], -63 - below / kBinsToOctave) / (double)of);
     };
     auto fit = [&](f32x4 v) {
-        if constexpr (LEVEL)
+        if constexpr (KNOWN)
 #pragma unroll
-            for (int c = 0; c < 4; ++c) v[c] = v[c] == most ? 0.f : -INFINITY;
+            for (int c = 0; c < 4; ++c) v[c] = fit_one(v[c]);
         return v;
     };
     // f of the tokens that pick() is true of; a vector of four without any costs nothing more
@@ -276,7 +287,7 @@ __device__ __forceinline__ bool sample_row(SampleShared<Row::kThreads> &s, const
     int stage = small || (by_k && n_k <= kList * 3 / 4) ? kStageAll : by_k ? kStageK : behind_k;
     enum { kNone, kCounts, kMasses, kBoth };
     int built = kNone;                                     // what the histogram holds: running numbers or sums of the bins before
-    bool dirty = false, known = LEVEL, cut = false;        // the histogram is to be cleared; `most` is known; top-p or min-p has cut
+    bool dirty = false, known = KNOWN, cut = false;        // the histogram is to be cleared; `most` is known; top-p or min-p has cut
     unsigned kept = 0, all_count = 0;
     u64 mass = 0, all_mass = 0;                            // mass: of what is kept; all_: of all bins
     const double least = uniform(by_m ? log2((double)fminf(how.min_p, 1.f)) : 0.0);     // of a kept token's logarithm, by min-p
@@ -290,10 +301,10 @@ __device__ __forceinline__ bool sample_row(SampleShared<Row::kThreads> &s, const
         const double u = how.uniform;
         return min((u64)floor(fmin(u > 0.0 ? u : 0.0, 1.0) * (double)sum) + 1ull, sum);
     };
-    auto level = [&](float v) { return ((double)v - (LEVEL ? 0.0 : (double)most)) * slope * (1.0 / kBinsToOctave); };
-    if constexpr (LEVEL) {
-        refer(0.f);
-        top_bin = uniform(bin_of(0.f));
+    auto level = [&](float v) { return ((double)v - (double)most) * slope * (1.0 / kBinsToOctave); };
+    if constexpr (KNOWN) {
+        refer(most);
+        top_bin = uniform(bin_of(most));
     }
     for (;;) {
         const bool counts = stage <= kStageK;
@@ -347,8 +358,7 @@ __device__ __forceinline__ bool sample_row(SampleShared<Row::kThreads> &s, const
                     if (tid == 0) answer(-1, 0.f, 0);
                     return true;
                 }
-                // infinite, or so steep that only what equals it has a weight: one step of the largest number is more bins than there are
-                if (most == INFINITY || (double)fabsf(most) * slope > 0x1p40) return false;
+                if (how.tau < kSteep || sample_level(how, most)) return false;
                 // (uniform) out of reach, or below the zero that stands in for first logits that are all masked: the histogram from the largest on
                 if (depth_of(most) < 0.f || depth_of(most) > kAbove) {
                     refer(most);
@@ -442,7 +452,7 @@ __device__ __forceinline__ bool sample_row(SampleShared<Row::kThreads> &s, const
         if (stage == kStageCut && by_m) {
             // min-p ends in one of the bins m_lo .. m_hi (fp32 and fp64 may put a logit on either side of a border).  Where top-p ends in a bin before them, min-p
             // keeps more; otherwise the tokens before and in them are numbered and added up.
-            const double at = ((double)ref - (LEVEL ? 0.0 : (double)most)) * slope + (double)kAbove - least * kBinsToOctave;
+            const double at = ((double)ref - (double)most) * slope + (double)kAbove - least * kBinsToOctave;
             const int m_lo = (int)fmin(fmax(at - 0.01, 0.0), (double)kBins), m_hi = (int)fmin(fmax(at + 0.01, 0.0), (double)kBins);
             by_list = by_p && bin <= m_hi;
             if (!by_p || bin >= m_lo) {                    // (uniform)
@@ -707,9 +717,9 @@ __global__ void __launch_bounds__(T, 4) k_sample(SampleParams P)
         return;
     }
     float most = -INFINITY;
-    if (sample_row<false>(s, R, how, most, answer)) return;
-    // Only the tokens that equal the largest weigh anything.  Where that is infinite the others are no part of the order; where the temperature is so low they
-    // are, and are kept where nothing cuts them off.
+    if (sample_row<false>(s, R, how, [](float v) { return v; }, most, answer)) return;
+    // Either the row is steep, or only the tokens that equal the largest weigh anything.  Where that is infinite the others are no part of the order; where the temperature is
+    // so low they are, and are kept where nothing cuts them off.
     if (most < INFINITY && !(how.top_p < 1.f) && !(how.min_p > 0.f)) {         // (uniform)
         unsigned n = 0, none, valid;
         u64 none_of, no_sum;
@@ -723,7 +733,11 @@ __global__ void __launch_bounds__(T, 4) k_sample(SampleParams P)
     __syncthreads();
     for (int b = tid; b < kBins; b += T) { s.count[b] = 0u; s.mass[b] = 0ull; }
     __syncthreads();
-    sample_row<true>(s, R, how, most, answer);
+    const bool steep = !sample_level(how, most);
+    const float top = most;
+    how.tau = steep ? how.tau * kUnsteep : 1.f;
+    most = steep ? most * kUnsteep : 0.f;
+    sample_row<true>(s, R, how, [=](float v) { return steep ? v * kUnsteep : v == top ? 0.f : -INFINITY; }, most, answer);
 }
 
 template <int T, bool F16>

@@ -221,6 +221,23 @@ def test_probabilities_of_rare_tokens(how):
 FILTERS = [dict(), dict(top_k=30), dict(top_k=600), dict(top_p=0.8), dict(min_p=0.03), dict(top_k=600, top_p=0.9, min_p=0.01)]
 
 
+@pytest.mark.parametrize("temperature", [4e-36, 1e-37, 1e-40, 2.0 ** -149])
+@pytest.mark.parametrize("vocab", [3, 300, 20000])
+def test_temperatures_next_to_zero(vocab, temperature):
+    """Logits as far apart as the temperature is large, down to the smallest positive number, alone and behind others that are far below"""
+    rng = np.random.default_rng(vocab)
+    n = 24
+    t = np.float32(temperature)
+    x = (3.0 * rng.standard_normal((n, vocab)) * np.float64(t)).astype(np.float32)
+    x[8:] -= x[8:].max(-1, keepdims=True)                   # the largest is 0
+    x[12:16, :vocab * 4 // 5] = -1e30
+    x[16:20, :vocab * 4 // 5] = np.finfo(np.float32).min
+    x[20:, ::2] = -np.inf
+    u = rng.random(n, dtype=np.float32)
+    for how in FILTERS:
+        check(x, uniform=u, temperature=t, **how)
+
+
 @pytest.mark.parametrize("temperature", [1e37, 1e38, np.finfo(np.float32).max])
 @pytest.mark.parametrize("vocab", [2, 300, 20000])
 def test_logits_further_apart_than_their_largest(vocab, temperature):
