@@ -388,6 +388,58 @@ def test_two_batches_on_two_streams():
     b.check(b.result())
 
 
+@pytest.mark.parametrize("type", TYPES)
+def test_many_pieces_behind_one_plan(type):
+    """Requests of 31 and 20 pieces, whose sums are joined in two steps: every layer's call finds the plan as the one before it did, one over an fp16 pool among them"""
+    s = Step8([3950, 900, 2500], ones(3), (4, 2, 80), seed=41, type=type).to_gpu()
+    s.run_plan()
+    first = s.attention8().result().copy()
+    s.check(first)
+    half = s.attention().copy()
+    for _ in range(3):
+        s.g_out.fill_(7.0)
+        assert np.array_equal(bits(s.attention8().result()), bits(first))
+        s.g_out.fill_(7.0)
+        assert np.array_equal(bits(s.attention()), bits(half))
+    s.q = -s.q                                              # other queries: no sum is that of the call before
+    s.g_q.copy_(dev(s.q))
+    s.check(s.attention8().result())
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    one = torch.zeros_like(s.g_out)
+    with torch.cuda.graph(graph, stream=side):
+        cf.cfpp_tree_plan(s.pages, s.batch, s.H, stream())
+        s.attention8()
+        one.copy_(s.g_out)
+        s.attention8()
+    for r, n in ((0, 3950), (1, 3000), (0, 2049), (2, 64)):
+        s.g["lens"][r] = s.lens[r] = min(n, s.lens[r])
+        s.g_out.fill_(7.0)
+        graph.replay()
+        replayed = s.result().copy()
+        assert np.array_equal(bits(replayed), bits(one.cpu().numpy()))
+        s.g_out.fill_(7.0)
+        s.run_plan().attention8()
+        assert np.array_equal(bits(s.result()), bits(replayed))
+        s.check(replayed)
+
+
+def test_many_pieces_on_two_streams():
+    """Each batch with a plan of its own, over and over"""
+    a = Step8([3950, 90], ones(2), (8, 2, 64), seed=42).to_gpu()
+    b = Step8([3500, 90], ones(2), (4, 2, 128), seed=43, type=page8_ref.E4M3).to_gpu()
+    a.run_plan()
+    b.run_plan()
+    torch.cuda.synchronize()
+    one, two = torch.cuda.Stream(), torch.cuda.Stream()
+    for _ in range(5):
+        a.attention8(one.cuda_stream)
+        b.attention8(two.cuda_stream)
+    a.check(a.result())
+    b.check(b.result())
+
+
 # ---- what lies in positions that a row does not see ------------------------------------------------------
 def unwritten(s, r, node):
     """A node's slot holds what a pool begins with"""

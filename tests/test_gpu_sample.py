@@ -336,6 +336,23 @@ def test_rows_that_lie_far_apart(dtype):
         page8_ref.check_sample(x[r], (int(tokens[r]), float(probs[r]), int(kept[r])), uniform=float(u[r]))
 
 
+@pytest.mark.parametrize("dtype", [np.float32, np.float16])
+def test_as_many_logits_as_there_may_be(dtype):
+    """2^18 of them: equal ones, whose sum is the largest there is, and such as a model has"""
+    rng = np.random.default_rng(53)
+    n, vocab = 6, 1 << 18
+    x = model_logits(rng, n, vocab, dtype)
+    x[:2] = [[-1.25], [3.5]]
+    x[4] = np.round(x[4])
+    x[5, :-200] = -np.inf
+    u = rng.random(n, dtype=np.float32)
+    for how in (dict(), dict(top_k=200000), dict(top_p=0.37), dict(min_p=0.5), dict(top_k=600, top_p=0.9), dict(temperature=1e-3), dict(temperature=50.0, top_p=0.999)):
+        got = check(x, uniform=u, **how)
+        kept = 200000 if "top_k" in how and "top_p" not in how else vocab
+        if "top_p" not in how:
+            assert [t for t, _, _ in got[:2]] == [int(np.floor(float(v) * kept)) for v in u[:2]]
+
+
 def test_two_streams_at_once():
     rng = np.random.default_rng(52)
     x, u = [model_logits(rng, 40, 50304) for _ in range(2)], rng.random(40, dtype=np.float32)
