@@ -569,8 +569,9 @@ cfpp_status cfpp_page8_read(const cfpp_pages *pages, int32_t type, const void *k
 /* cfpp_tree_attention over a pool of 8-bit codes: the same batch, plan, masks, arguments
  * and rules, with the codes' values, unrounded, for K and V.  Fastest where a request's nodes
  * times the query heads of a key head are at most 16, above all one new token to a
- * request: more are taken 16 at a time, each time with the cache read again.  Positions
- * that a row sees have to have been written by cfpp_page8_append. */
+ * request: more are taken 16 at a time, each time with the cache read again, and from 33
+ * on an fp16 pool is the faster one.  Positions that a row sees have to have been written
+ * by cfpp_page8_append. */
 cfpp_status cfpp_page8_attention(const cfpp_pages *pages, int32_t type, const void *kv_pool,
                                  const cfpp_tree_batch *batch, const void *q, int64_t q_stride,
                                  int32_t n_heads, void *out, int64_t out_stride, cfpp_stream stream);
@@ -579,7 +580,8 @@ cfpp_status cfpp_page8_attention(const cfpp_pages *pages, int32_t type, const vo
  * Filters of each row (HOST struct of DEVICE pointers, 4-byte aligned, each [n_rows] or NULL).
  * A row's order is larger logit first, lower index among equals; its weights are
  * w = exp((logit - largest logit) / temperature).  In turn:
- *   temperature : NULL: 1.  Not above 0: the first of the order, whatever the rest
+ *   temperature : NULL: 1.  Not above 0: the first of the order, whatever the rest.  Infinite: all
+ *                 that are in the order weigh the same
  *   top_k       : the first k of the order are kept; NULL, 0 or less, or as many as there are: all
  *   top_p       : of these as many, from the first on, as it takes for their sum to reach
  *                 top_p times the sum of all of these; one at least; NULL, 1 or more, NaN: all

@@ -12,11 +12,14 @@
 // dimension, it loads.  P needs no exchange, V no transposition: the granule holds V by dimension and K in the tiles' order, and every load
 // is a run of at least 256 bytes.  Nothing goes through LDS but the wavefronts' sums at the end.
 //
-// Bound by the way of the codes from memory once there are many (32 requests behind 3000 to 8191 of 32 heads of 128: 1.55 GB in 250 us, 6.2 TB/s of the 7.0
-// that reads reach), and by launch, first loads and the join of the pieces where there are few: about 9 us that no split made shorter (one token behind 128 positions of 8
-// heads of 64 6.0 us, behind 4096 of 32 heads of 80 11.5, behind 131072 of two heads of 64 with 8 query heads each 16.6; 64 requests of up to 3000 positions and 8 heads 48, of
-// which 9 and 38 at 6.4 TB/s).  More pieces: 768 to 2048 workgroups 52 to 56 us for the 64 requests; workgroups of 8 wavefronts 54; a third
-// workgroup to a CU needs 20 more registers than head_dim 128 leaves.
+// Bound by the way of the codes from memory once there are many (32 requests behind 3000 to 8191 of 32 heads of 128: 1.55 GB in 251 us, 6.2 TB/s of the 7.0
+// that reads reach; 64 requests of up to 3000 positions and 8 heads of 128: 222 MB in 47.5, 4.7).  Where there are few it is bound by launch and first loads (one token
+// behind 128 positions of 8 heads of 64, a piece to each head, 6.2 us) and by the pieces' way to each other through memory, which no split made shorter (behind 4096 of 32
+// heads of 80, 16 pieces, 12.2; behind 131072 of two heads of 64 with 8 query heads each 16.9).  More pieces: 768 to 2048 workgroups 52 to 56 us for the 64 requests;
+// workgroups of 8 wavefronts 54; a third workgroup to a CU needs 20 more registers than head_dim 128 leaves.
+//
+// More than 16 query rows to a request are taken 16 at a time, each time with the codes read again: simple, and right for a few drafted nodes, but from 33 rows on an fp16 pool is
+// the faster one (64 requests of up to 3000 positions of hidden 2560, fp16 / int8: 9 nodes 163 / 107 us, 36 nodes 181 / 298; 8 requests of 32 nodes 92 / 88, of 64 113 / 159).
 //
 // What enters the second product is fp16, head cut off and exact remainder cut off, 2^-21 of it.  a_V may be anything from 2^-24 to 2^16, so the
 // reference of the running maximum is that of s_t + e_t with a_V = f_t 2^(e_t): the largest *contribution* is near 2^9 whatever the scales are, and the weight
@@ -264,7 +267,9 @@ __global__ void __launch_bounds__(kTaThreads, 2) k_page8_attention(TreeAttention
                 S[T] = __builtin_amdgcn_mfma_f32_16x16x32_f16(p8_values8<INT8>(r.k[T][b][0], r.k[T][b][1]), q[b][0], S[T], 0, 0, 0);
                 S[T] = __builtin_amdgcn_mfma_f32_16x16x32_f16(p8_values8<INT8>(r.k[T][b][2], r.k[T][b][3]), q[b][1], S[T], 0, 0, 0);
             }
-            // (four dimensions of a lane's eight; the instruction of half the depth, behind the others into the same sums, left two of them wrong)
+            // Four dimensions of a lane's eight.  Not the instruction of half the depth (v_mfma_f32_16x16x16_f16): the compiler lets a vector instruction overwrite the registers
+            // of its third operand three or four places behind it, which is too soon while it still waits for that operand from an instruction of the other depth.  Two of the
+            // four sums were wrong; with wait states ahead of it or behind it they were right.  In a chain of one instruction that distance is enough.
             if constexpr (ODD) {
                 const ta_u32x2 x = p8_values<INT8>(r.kt[T]);
                 S[T] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(ta_f16x8, u32x4{x[0], x[1], 0u, 0u}), qt, S[T], 0, 0, 0);

@@ -9,8 +9,8 @@
 // a run.  A workgroup has the runs that begin in 16 rows of the call - up to 31 rows - for a few heads of K or of V; V's codes meet in LDS.  A single row to a
 // run, as in a decode step, writes its V codes byte by byte.
 //
-// Bound by memory where there are many rows (append of 4096 rows of 32 heads of 128, 101 MB: 23.7 us, 4.3 TB/s), by launch and one way to memory and back where there are
-// few (64 rows in pages of their own 5.1 us).
+// Bound by memory where there are many rows (append of 4096 rows of 32 heads of 128, 101 MB: 24.9 us, 4.0 TB/s; a large copy has 4.6), by launch and one way to memory and
+// back where there are few (64 rows in pages of their own 5.0 us).
 #include <hip/hip_runtime.h>
 #include <hip/hip_fp16.h>
 #include "tree_params.h"
@@ -260,9 +260,16 @@ __global__ void __launch_bounds__(256) k_page8_read(Page8Rows P)
     }
 }
 
-// Up to so many workgroups of many heads there are some of few: 64 rows of 32 heads of 80, each in a page of its own, are 48 of six heads or 256 of one
-// (kernel alone: append 13.8 and 5.1 us; read of 77 rows 7.6 and 5.3).  Of few always, an append of 4096 rows of 32 heads of 128 takes 32.4 us for 23.7, a read of 16384
-// rows of 8 heads 35.6 for 24.1.
+// Up to so many workgroups of many heads there are some of few: 64 rows of 32 heads of 80, each in a page of its own, are 48 of six heads or 256 of one.
+// us a call in a graph, few / many, by the workgroups of many heads:
+//     rows apart, 32 heads of 80     48     180    240    264    360    540            rows that follow one another     48     240    264    360    540    768
+//     append                         4.4    7.1    8.5    8.9   10.5   17.4                                             4.2    5.3    5.6    6.2    7.7   10.9
+//                                  / 11.0  12.9   13.4   13.6   15.2   16.3                                          / 10.2   10.4   10.5   11.0   11.5   14.4
+//     read                          10.6   11.3   12.1   13.2   13.6   19.5                                             5.2    6.1    6.3    6.8    8.2    8.9
+//                                  / 10.5  11.0   11.4   12.5   13.3   15.2                                           / 7.4    7.7    7.7    7.8    8.1    8.4
+// An append turns at about 500 of them where rows lie apart, behind 1000 where they follow one another, a read of rows that follow at about 500; one of rows that lie apart never gains.
+// 32 heads of 128 and 8 heads of 64 or of 128 do the same.  Of few always, an append of 4096 rows of 32 heads of 128 takes 32.4 us for 23.7, a read of 16384 rows of 8 heads 35.6
+// for 24.1.
 constexpr int kP8Few = 256;
 template <int D, bool INT8, bool FEW>
 static hipError_t launch_of(const Page8Rows &P, bool append, hipStream_t s)

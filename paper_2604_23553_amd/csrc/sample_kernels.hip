@@ -16,9 +16,10 @@
 // whichever wavefront comes first, and a border between two tokens is where 64-bit arithmetic has it but for 2^-40 of the sum.  With weights in fp32 it would
 // be up to 2^-24 off, which is another token once in some hundred thousand rows.
 //
-// Bound by one CU's instructions - the vector units are busy two thirds of a lone row's time - and by the way of a pass's first logits, not by memory: of a row's 26 us the
-// pass that lays sums takes 11, the sums over the bins 1, each pass that collects 4.  50304 logits in fp32: one row, top-p 25.2 us; 64 rows, top-k of 50, top-p and min-p
-// 18.3 us; 512 rows of different settings 61 us, 1.7 TB/s.  A row's logits do not fit its registers, and a row on more than one CU would need a workspace of the caller's.
+// Bound by one CU's instructions - the vector units are busy 63 % of a lone row's time - and by the way of a pass's first logits, not by memory: of a row's 26 us in an earlier
+// build the pass that lays sums took 11, the sums over the bins 1, each pass that collects 4.  50304 logits in fp32: one row, top-p 24.8 us; 64 rows, top-k of 50, top-p and
+// min-p 18.2 us, with fp16 logits 18.0; 512 rows of different settings 61 us, 1.7 TB/s.  A row's logits do not fit its registers, and a row on more than one CU would
+// need a workspace of the caller's.
 #include <hip/hip_runtime.h>
 #include <hip/hip_fp16.h>
 #include "sample_params.h"

@@ -65,7 +65,7 @@ __device__ __forceinline__ float ta_max4(float v)
 }
 constexpr float kTaUp = 9.f, kTaSlack = 6.f;               // (together at most 2^15, of fp16's 2^16)
 
-// 32 bits of "sees position t .. t + 31" of a node: cached positions, then its words; t a multiple of 32, its request's last position behind it or not
+// 32 bits of "sees position t .. t + 31" of a node: cached positions, then its words; any t, its request's last position behind it or not
 __device__ __forceinline__ unsigned ta_window(const unsigned *words, int n_words, int t, int len, int nodes)
 {
     const int rel = t - len;                               // node number of the first bit
